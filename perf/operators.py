@@ -426,12 +426,14 @@ def _plain(s):
     if case.get("lse") or kind == "wtrain":
         res["lse"] = torch.stack([o[1] for o in outs])
     if kind == "wtrain":
-        res["dq"] = torch.stack([o[2] for o in outs])
+        # bf16 gradients, as bf16 training takes them
+        res["dq"] = torch.stack([o[2] for o in outs]).to(torch.bfloat16)
         for i, name in ((1, "dk"), (2, "dv")):
-            res[name] = torch.zeros(s["k"].shape, dtype=torch.float32, device=DEV)
+            total = torch.zeros(s["k"].shape, dtype=torch.float32, device=DEV)
             for b, o in enumerate(outs):
                 for part in o[3]:
-                    res[name][b].index_add_(0, part[0], part[i])
+                    total[b].index_add_(0, part[0], part[i])
+            res[name] = total.to(torch.bfloat16)
     return res
 
 
@@ -470,7 +472,8 @@ def run(s):
                                       want_lse=case["lse"], **win)
         return {"out": got[0], "lse": got[1]} if case["lse"] else {"out": got}
     out, lse = ws.block_causal_prefill(s["q"], s["k"], s["v"], s["offsets"], want_lse=True, **win)
-    dq, dk, dv = ws.block_causal_prefill_bwd(s["q"], s["k"], s["v"], out, s["dout"], lse, s["offsets"], **win)
+    dq, dk, dv = ws.block_causal_prefill_bwd(s["q"], s["k"], s["v"], out, s["dout"], lse, s["offsets"],
+                                             grad_dtype=torch.bfloat16, **win)
     return {"out": out, "lse": lse, "dq": dq, "dk": dk, "dv": dv}
 
 
@@ -504,8 +507,8 @@ def work(case):
     if kind == "wprefill":
         lse = 4.0 * b * length * hq if case["lse"] else 0.0
         return {"bytes": 2 * q + 2 * kv + q * (4 if case["f32"] else 2) + lse, "flops": 4.0 * d * hq * pairs}
-    # forward (q, k, v -> out, lse) and gradients (dout -> f32 dq, dk, dv)
-    return {"bytes": 2 * q + 2 * kv + 2 * q + 2 * q + 4 * q + 4 * kv + 4.0 * b * length * hq,
+    # forward (q, k, v -> out, lse) and gradients (dout -> dq, dk, dv)
+    return {"bytes": 2 * q + 2 * kv + 2 * q + 2 * q + 2 * q + 2 * kv + 4.0 * b * length * hq,
             "flops": 14.0 * d * hq * pairs}
 
 
