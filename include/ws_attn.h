@@ -36,6 +36,19 @@
  * lengths, padded to a common new_len.  Padding tokens are never keys and
  * are never committed; the outputs of their rows are unspecified.
  *
+ * Sliding windows (the *_window entry points).  A session that runs for hours
+ * cannot attend to, or keep, all of its history.  With a window of `window`
+ * tokens and `sinks` first tokens that stay visible, a token sees the first
+ * `sinks` tokens, the `window` tokens before its anchor and, of its own block,
+ * what it sees without a window from the window on.  The anchor of a token in a
+ * token-causal segment is the token itself, of any other token the start of its
+ * block: token i of the block [s, e) with segment start tau (tau = e: none) sees
+ * the keys
+ *   j < max(tau, i + 1)  with  j < sinks  or  j >= (i >= tau ? i : s) - window.
+ * So a block's observations keep seeing their whole block, and a token-causal
+ * token sees the same keys whether it is decoded as a block of one token or
+ * stands in a longer segment.  Every token sees itself.
+ *
  * Conventions for every entry point
  * ---------------------------------
  * - Token tensors are 4-d [batch][tokens][heads][head_dim] described by
@@ -398,6 +411,86 @@ int ws_block_causal_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_ten
                                 int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                 float scale, ws_tensor4 dq, ws_tensor4 dk, ws_tensor4 dv,
                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * ws_block_causal_attn_fwd_window -- a streaming step through a sliding window
+ * with sinks (see the top).  Same arguments and errors as
+ * ws_block_causal_attn_fwd_varlen, but new_lens and text_starts may each be
+ * NULL on host and device (every block holds new_len tokens; no segment), plus
+ *   sinks, window: both >= 0 (WS_ERR_SHAPE otherwise)
+ * Of the cache only positions [0, sinks) and [cache_lens[b] - window,
+ * cache_lens[b]) are read, and only their pages have to exist: the page table
+ * entries of the pages between may hold anything, so a caller can free or
+ * reuse those pages (WS_FUSE_APPEND also needs the new tokens' pages).
+ * f32 outputs hold f32 accuracy here (the softmax weights enter the product
+ * with V as the sum of two bf16 values).  workspace: at least
+ * ws_step_workspace_bytes_window(...) bytes for the same arguments.
+ */
+int ws_block_causal_attn_fwd_window(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new,
+                                    const ws_paged_kv *kv,
+                                    const int32_t *cache_lens_host, const int32_t *cache_lens_dev,
+                                    const int32_t *new_lens_host, const int32_t *new_lens_dev,
+                                    const int32_t *text_starts_host, const int32_t *text_starts_dev,
+                                    int32_t batch, int32_t new_len, int32_t num_q_heads,
+                                    int32_t sinks, int32_t window, float scale, int32_t flags,
+                                    ws_tensor4 out, float *lse,
+                                    void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * ws_step_workspace_bytes_window -- device workspace bytes of
+ * ws_block_causal_attn_fwd_window for these host arrays (int32 [batch] each;
+ * new_lens_host may be NULL), planned for the current device.  0 when none is
+ * needed, an argument is invalid or no device is available.
+ */
+size_t ws_step_workspace_bytes_window(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                      int32_t new_len, const int32_t *cache_lens_host,
+                                      const int32_t *new_lens_host, int32_t sinks, int32_t window);
+
+/*
+ * ws_block_causal_prefill_window -- whole sequences through a sliding window
+ * with sinks.  Same arguments and errors as ws_block_causal_prefill_text, but
+ * text_starts may be NULL on host and device (no segments), plus
+ *   sinks, window: both >= 0 (WS_ERR_SHAPE otherwise)
+ * f32 outputs hold f32 accuracy (as in the step above).
+ */
+int ws_block_causal_prefill_window(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v,
+                                   const ws_paged_kv *kv_or_null,
+                                   const int32_t *block_offsets_host, const int32_t *block_offsets_dev,
+                                   const int32_t *text_starts_host, const int32_t *text_starts_dev,
+                                   int32_t batch, int32_t seq_len, int32_t num_blocks,
+                                   int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                   int32_t sinks, int32_t window, float scale,
+                                   ws_tensor4 out, float *lse, void *stream);
+
+/*
+ * ws_block_causal_prefill_window_bwd -- gradients of
+ * ws_block_causal_prefill_window (contiguous keys).  Same arguments and errors
+ * as ws_block_causal_prefill_bwd, with P_ij = 0 for the keys a window hides, plus
+ *   sinks, window: as the forward's
+ *   dq, dk, dv:    all f32, or all bf16 (the f32 sums rounded once: what bf16
+ *                  training keeps); mixed dtypes give WS_ERR_UNSUPPORTED
+ *   workspace:     ws_prefill_window_bwd_workspace_bytes(...) bytes, 16-byte
+ *                  aligned; 8 * batch * num_q_heads * seq_len bytes (rounded
+ *                  up to 256) + 8 * batch * seq_len are enough to run, unsplit
+ * Deterministic, as ws_block_causal_prefill_bwd.
+ */
+int ws_block_causal_prefill_window_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 o,
+                                       ws_tensor4 dout, const float *lse,
+                                       const int32_t *block_offsets_host, const int32_t *block_offsets_dev,
+                                       const int32_t *text_starts_host, const int32_t *text_starts_dev,
+                                       int32_t batch, int32_t seq_len, int32_t num_blocks,
+                                       int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                       int32_t sinks, int32_t window, float scale,
+                                       ws_tensor4 dq, ws_tensor4 dk, ws_tensor4 dv,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Workspace bytes of ws_block_causal_prefill_window_bwd, with room for the
+ * sums it would split on a whole chip (host arithmetic: no device is asked).
+ * 0 for invalid arguments.
+ */
+size_t ws_prefill_window_bwd_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                             int32_t seq_len, int32_t sinks, int32_t window);
 
 /*
  * Workspace bytes ws_block_causal_attn_fwd (and its _text variant) needs

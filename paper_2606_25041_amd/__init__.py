@@ -17,12 +17,15 @@ Entry points (same names as the C ABI, without the ``ws_`` prefix):
 segment; with new_lens: the *_varlen entry points, new blocks of different
 lengths padded to a common one)
   block_causal_prefill_bwd(q, k, v, o, dout, lse, block_offsets, ...)
+(with window and sinks: the *_window entry points, attention to the first tokens
+and a sliding window of the latest)
   workspace_bytes(op, batch, num_q_heads, num_kv_heads, max_q, max_k)
   step_workspace_bytes_varlen(batch, num_q_heads, num_kv_heads, new_len, cache_lens, new_lens)
   step_plan(batch, num_q_heads, num_kv_heads, new_len, cache_lens, new_lens=None, num_cus=0)
 """
 import ctypes
 import math
+import operator
 import os
 
 import torch  # loads the HIP runtime that libwsattn.so then shares
@@ -120,6 +123,22 @@ def library():
         lib.ws_step_plan.restype = ctypes.c_int
         lib.ws_step_plan.argtypes = [I32, I32, I32, I32, I32, P, P, ctypes.POINTER(I32),
                                      ctypes.POINTER(ctypes.c_size_t)]
+        lib.ws_block_causal_attn_fwd_window.restype = ctypes.c_int
+        lib.ws_block_causal_attn_fwd_window.argtypes = [
+            Tensor4, Tensor4, Tensor4, ctypes.POINTER(PagedKVDesc), P, P, P, P, P, P, I32, I32, I32, I32, I32, F, I32,
+            Tensor4, P, P, ctypes.c_size_t, P]
+        lib.ws_step_workspace_bytes_window.restype = ctypes.c_size_t
+        lib.ws_step_workspace_bytes_window.argtypes = [I32, I32, I32, I32, P, P, I32, I32]
+        lib.ws_block_causal_prefill_window.restype = ctypes.c_int
+        lib.ws_block_causal_prefill_window.argtypes = [
+            Tensor4, Tensor4, Tensor4, ctypes.POINTER(PagedKVDesc), P, P, P, P, I32, I32, I32, I32, I32, I32, I32,
+            I32, F, Tensor4, P, P]
+        lib.ws_block_causal_prefill_window_bwd.restype = ctypes.c_int
+        lib.ws_block_causal_prefill_window_bwd.argtypes = [
+            Tensor4, Tensor4, Tensor4, Tensor4, Tensor4, P, P, P, P, P, I32, I32, I32, I32, I32, I32, I32, I32, F,
+            Tensor4, Tensor4, Tensor4, P, ctypes.c_size_t, P]
+        lib.ws_prefill_window_bwd_workspace_bytes.restype = ctypes.c_size_t
+        lib.ws_prefill_window_bwd_workspace_bytes.argtypes = [I32, I32, I32, I32, I32, I32]
         if lib.ws_abi_version() != 5:
             raise RuntimeError("libwsattn.so ABI version mismatch")
         _bind_native(lib)
@@ -140,6 +159,9 @@ def _bind_native(lib):
         "ws_block_causal_attn_fwd_varlen", "ws_block_causal_attn_fwd_noalloc", "ws_block_causal_prefill",
         "ws_block_causal_prefill_text", "ws_block_causal_prefill_bwd", "ws_workspace_bytes",
         "ws_step_workspace_bytes_varlen")))
+    _NATIVE.bind_window(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
+        "ws_block_causal_attn_fwd_window", "ws_step_workspace_bytes_window", "ws_block_causal_prefill_window",
+        "ws_block_causal_prefill_window_bwd", "ws_prefill_window_bwd_workspace_bytes")))
 
 
 def _native():
@@ -291,6 +313,18 @@ def kv_append(cache, cache_lens, k_new, v_new, new_lens=None):
                                              _stream()))
 
 
+def _window(window, sinks):
+    """The window's arguments as ints (window None: no window, and no sinks)."""
+    window = None if window is None else operator.index(window)
+    sinks = operator.index(sinks)
+    if window is None and sinks:
+        raise ValueError("sinks need a window")
+    for name, x in (("window", window), ("sinks", sinks)):
+        if x is not None and not 0 <= x < 2 ** 31:
+            raise ValueError(f"{name} must be in [0, 2^31)")
+    return window, sinks
+
+
 def _int32_pair(x, shape, device):
     """(host, device) int32 tensors of the given shape from an array-like or
     a (host, device) pair."""
@@ -308,7 +342,7 @@ def _int32_pair(x, shape, device):
 
 def block_causal_attn_fwd(q, k_new, v_new, cache, cache_lens, scale=None, fuse_append=False,
                           out=None, out_dtype=torch.bfloat16, want_lse=False, lse=None,
-                          workspace=None, text_starts=None, new_lens=None):
+                          workspace=None, text_starts=None, new_lens=None, window=None, sinks=0):
     """One streaming step: q [B][Lq][Hq][d] of the new block attends to
     cache tokens [0, cache_lens[b]) and to its own block (k_new/v_new).
     text_starts (optional, [B]): the new block ends in a token-causal segment
@@ -317,9 +351,16 @@ def block_causal_attn_fwd(q, k_new, v_new, cache, cache_lens, scale=None, fuse_a
     new_lens (optional, [B], 1..Lq): stream b's block is its first
     new_lens[b] tokens; the rest is padding, never a key and never committed,
     and its rows' out and lse are unspecified.
+    window, sinks (optional): a token sees the first ``sinks`` tokens and, of
+    the rest, those from ``window`` tokens before its block on (a token of a
+    token-causal segment: before itself).  Only the pages of cache positions
+    [0, sinks) and [cache_lens[b] - window, cache_lens[b]) are then read; the
+    table's other entries may hold anything.
     Returns out (and lse [B][Hq][Lq] f32 when want_lse)."""
-    got = _native().step(q, k_new, v_new, cache, cache_lens, scale, fuse_append, out, out_dtype, want_lse, lse,
-                         workspace, text_starts, new_lens, False)
+    window, sinks = _window(window, sinks)
+    args = (q, k_new, v_new, cache, cache_lens, scale, fuse_append, out, out_dtype, want_lse, lse, workspace,
+            text_starts, new_lens, False)
+    got = _native().step(*args) if window is None else _native().step_window(*args, window, sinks)
     if got is not None:
         rc, out, lse = got
         if rc:
@@ -344,6 +385,9 @@ def block_causal_attn_fwd(q, k_new, v_new, cache, cache_lens, scale=None, fuse_a
     nl = None if new_lens is None else _int32_pair(new_lens, (B,), q.device)
     if B == 0 or Lq == 0:
         need = 0
+    elif window is not None:
+        need = library().ws_step_workspace_bytes_window(B, Hq, cache.num_kv_heads, Lq, host.data_ptr(),
+                                                        None if nl is None else nl[0].data_ptr(), sinks, window)
     elif nl is None:
         need = workspace_bytes(WS_OP_STEP, B, Hq, cache.num_kv_heads, Lq, int(host.max().item()) + Lq)
     else:
@@ -354,7 +398,14 @@ def block_causal_attn_fwd(q, k_new, v_new, cache, cache_lens, scale=None, fuse_a
     ws_len = workspace.numel() if workspace is not None else 0
     desc = cache.desc()
     flags = WS_FUSE_APPEND if fuse_append else 0
-    if nl is not None:
+    if window is not None:
+        th, td = _int32_pair(text_starts, (B,), q.device) if text_starts is not None else (None, None)
+        nh, nd = nl if nl is not None else (None, None)
+        _check(library().ws_block_causal_attn_fwd_window(
+            _t4(q), _t4(k_new), _t4(v_new), ctypes.byref(desc), host.data_ptr(), dev.data_ptr(), _ptr(nh), _ptr(nd),
+            _ptr(th), _ptr(td), B, Lq, Hq, sinks, window, float(scale), flags, _t4(out), _ptr(lse), ws_ptr, ws_len,
+            _stream()))
+    elif nl is not None:
         th, td = _int32_pair(text_starts, (B,), q.device) if text_starts is not None else (None, None)
         _check(library().ws_block_causal_attn_fwd_varlen(
             _t4(q), _t4(k_new), _t4(v_new), ctypes.byref(desc), host.data_ptr(), dev.data_ptr(),
@@ -411,15 +462,17 @@ def block_causal_attn_fwd_noalloc(q, k_new, v_new, cache, cache_lens, out, lse=N
 
 def block_causal_prefill(q, k, v, block_offsets, scale=None, cache=None, num_kv_heads=None,
                          out=None, out_dtype=torch.bfloat16, want_lse=False, lse=None,
-                         text_starts=None):
+                         text_starts=None, window=None, sinks=0):
     """Whole-sequence block-causal attention.  q [B][L][Hq][d]; k, v
     [B][L][Hkv][d] or None to read them from ``cache``; block_offsets
     [B][nb+1] (host tensor, or a (host, device) pair).  text_starts
     (optional, [B][nb], absolute positions): block n ends in a token-causal
     segment starting there; its token i then sees keys
-    j < max(text_starts[b][n], i + 1)."""
-    got = _native().prefill(q, k, v, block_offsets, scale, cache, num_kv_heads, out, out_dtype, want_lse, lse,
-                            text_starts)
+    j < max(text_starts[b][n], i + 1).  window, sinks: as in
+    ``block_causal_attn_fwd``."""
+    window, sinks = _window(window, sinks)
+    args = (q, k, v, block_offsets, scale, cache, num_kv_heads, out, out_dtype, want_lse, lse, text_starts)
+    got = _native().prefill(*args) if window is None else _native().prefill_window(*args, window, sinks)
     if got is not None:
         rc, out, lse = got
         if rc:
@@ -453,7 +506,12 @@ def block_causal_prefill(q, k, v, block_offsets, scale=None, cache=None, num_kv_
         raise ValueError("block_offsets must be [B][num_blocks + 1]")
     desc = cache.desc() if cache is not None else None
     kvp = ctypes.byref(desc) if desc is not None else None
-    if text_starts is None:
+    if window is not None:
+        th, td = _int32_pair(text_starts, (B, nb), q.device) if text_starts is not None else (None, None)
+        _check(library().ws_block_causal_prefill_window(
+            _t4(q), _t4(k), _t4(v), kvp, off_h.data_ptr(), off_d.data_ptr(), _ptr(th), _ptr(td), B, L, nb, Hq, hkv, D,
+            sinks, window, float(scale), _t4(out), _ptr(lse), _stream()))
+    elif text_starts is None:
         _check(library().ws_block_causal_prefill(
             _t4(q), _t4(k), _t4(v), kvp, off_h.data_ptr(), off_d.data_ptr(), B, L, nb, Hq, hkv, D,
             float(scale), _t4(out), _ptr(lse), _stream()))
@@ -466,12 +524,24 @@ def block_causal_prefill(q, k, v, block_offsets, scale=None, cache=None, num_kv_
 
 
 def block_causal_prefill_bwd(q, k, v, o, dout, lse, block_offsets, scale=None, text_starts=None,
-                             dq=None, dk=None, dv=None, workspace=None):
+                             dq=None, dk=None, dv=None, workspace=None, window=None, sinks=0,
+                             grad_dtype=torch.float32):
     """Gradients of ``block_causal_prefill`` (contiguous K/V) for an upstream
     output gradient dout: returns f32 (dq [B][L][Hq][d], dk, dv
     [B][L][Hkv][d]).  o and lse are the forward's output and lse;
-    text_starts as in ``block_causal_prefill``."""
-    got = _native().prefill_bwd(q, k, v, o, dout, lse, block_offsets, scale, text_starts, dq, dk, dv, workspace)
+    text_starts, window and sinks as in ``block_causal_prefill``.
+    grad_dtype: dtype of the gradients allocated here; bf16 with a window
+    only (the f32 sums rounded once)."""
+    window, sinks = _window(window, sinks)
+    if window is None:
+        if grad_dtype != torch.float32:
+            raise ValueError("gradients without a window are f32")
+        got = _native().prefill_bwd(q, k, v, o, dout, lse, block_offsets, scale, text_starts, dq, dk, dv, workspace)
+    else:
+        if grad_dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"unsupported grad_dtype {grad_dtype}")
+        got = _native().prefill_window_bwd(q, k, v, o, dout, lse, block_offsets, scale, text_starts, dq, dk, dv,
+                                           workspace, window, sinks, grad_dtype)
     if got is not None:
         if got[0]:
             _check(got[0])
@@ -492,20 +562,29 @@ def block_causal_prefill_bwd(q, k, v, o, dout, lse, block_offsets, scale=None, t
     if tuple(off_h.shape) != (B, nb + 1) or tuple(off_d.shape) != (B, nb + 1):
         raise ValueError("block_offsets must be [B][num_blocks + 1]")
     if dq is None:
-        dq = torch.empty((B, L, Hq, D), dtype=torch.float32, device=q.device)
+        dq = torch.empty((B, L, Hq, D), dtype=grad_dtype, device=q.device)
     if dk is None:
-        dk = torch.empty((B, L, hkv, D), dtype=torch.float32, device=q.device)
+        dk = torch.empty((B, L, hkv, D), dtype=grad_dtype, device=q.device)
     if dv is None:
-        dv = torch.empty((B, L, hkv, D), dtype=torch.float32, device=q.device)
+        dv = torch.empty((B, L, hkv, D), dtype=grad_dtype, device=q.device)
     _shape("dq", dq, (B, L, Hq, D))
     _shape("dk", dk, (B, L, hkv, D))
     _shape("dv", dv, (B, L, hkv, D))
-    need = workspace_bytes(WS_OP_PREFILL_BWD, B, Hq, hkv, L, L) if B > 0 and L > 0 else 0
+    need = 0
+    if B > 0 and L > 0:
+        need = workspace_bytes(WS_OP_PREFILL_BWD, B, Hq, hkv, L, L) if window is None else \
+            library().ws_prefill_window_bwd_workspace_bytes(B, Hq, hkv, L, sinks, window)
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     th = td = None
     if text_starts is not None:
         th, td = _int32_pair(text_starts, (B, nb), q.device)
+    if window is not None:
+        _check(library().ws_block_causal_prefill_window_bwd(
+            _t4(q), _t4(k), _t4(v), _t4(o), _t4(dout), _ptr(lse), off_h.data_ptr(), off_d.data_ptr(),
+            _ptr(th), _ptr(td), B, L, nb, Hq, hkv, D, sinks, window, float(scale), _t4(dq), _t4(dk), _t4(dv),
+            _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream()))
+        return dq, dk, dv
     _check(library().ws_block_causal_prefill_bwd(
         _t4(q), _t4(k), _t4(v), _t4(o), _t4(dout), _ptr(lse), off_h.data_ptr(), off_d.data_ptr(),
         _ptr(th), _ptr(td), B, L, nb, Hq, hkv, D, float(scale), _t4(dq), _t4(dk), _t4(dv),

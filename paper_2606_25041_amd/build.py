@@ -2,6 +2,7 @@
 
 Usage: python -m paper_2606_25041_amd.build   (or call build()).
 """
+import concurrent.futures
 import os
 import subprocess
 
@@ -13,7 +14,7 @@ DEVICE_SOURCES = [os.path.join(CSRC, "ws_kernels.hip"), os.path.join(CSRC, "ws_b
                   os.path.join(CSRC, "ws_device.hip")]
 HOST_SOURCES = [os.path.join(CSRC, "ws_api.cpp")]
 SOURCES = DEVICE_SOURCES + HOST_SOURCES + [os.path.join(CSRC, "ws_binding.cpp")]
-HEADERS = [os.path.join(CSRC, "ws_kernels.h"), os.path.join(CSRC, "ws_device_util.h"),
+HEADERS = [os.path.join(CSRC, "ws_kernels.h"), os.path.join(CSRC, "ws_host.h"), os.path.join(CSRC, "ws_device_util.h"),
            os.path.join(os.path.dirname(HERE), "include", "ws_attn.h")]
 # the device code whose hash tags measured counter summaries: the forward
 # kernels (attention, merge, append) and, separately, the gradient kernels
@@ -77,12 +78,15 @@ def build(verbose=False):
     C ABI are compiled separately, then linked into one shared library."""
     common = [hipcc(), f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
               "-Wall", "-Wno-unused-function"]
-    objs, msgs = [], []
+    objs, msgs, cmds = [], [], []
     for src in DEVICE_SOURCES + HOST_SOURCES:
         obj = LIB + "." + os.path.splitext(os.path.basename(src))[0] + ".o"
         flags = KERNEL_FLAGS if src in DEVICE_SOURCES else []
-        msgs += _run(common + flags + ["-c", src, "-o", obj])
+        cmds.append(common + flags + ["-c", src, "-o", obj])
         objs.append(obj)
+    with concurrent.futures.ThreadPoolExecutor(4) as pool:
+        for m in pool.map(_run, cmds):
+            msgs += m
     msgs += _run([hipcc(), f"--offload-arch={ARCH}", "-shared"] + objs + ["-o", LIB + ".tmp"])
     for f in objs:
         os.remove(f)

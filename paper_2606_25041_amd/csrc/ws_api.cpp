@@ -12,10 +12,9 @@
 #include <utility>
 #include <vector>
 
-#include "../../include/ws_attn.h"
-#include "ws_kernels.h"
+#include "ws_host.h"
 
-namespace {
+namespace ws {
 
 thread_local char g_err[512];
 
@@ -34,9 +33,6 @@ int ok() {
 
 constexpr int WS_MAX_SPLITS = ws::MAX_SPLITS;
 static_assert(WS_NOALLOC_SCRATCH_BYTES == ws::NOALLOC_SCRATCH_BYTES, "one scratch size");
-// packed query rows of one (stream, KV head) in a step: G x new_len (the
-// kernels index them in 32-bit arithmetic)
-constexpr int64_t WS_MAX_STEP_ROWS = ((int64_t)1 << 30);
 constexpr int WS_MAX_HEAD_DIM = 128;
 
 int env_int(const char *name, int dflt) {
@@ -103,25 +99,40 @@ int check_paged(const ws_paged_kv *kv) {
     return WS_OK;
 }
 
-// Every page that positions [0, n) of stream b live in must exist.
-int check_pages(const ws_paged_kv *kv, int b, int64_t n) {
-    if (n > (int64_t)kv->max_pages_per_seq * kv->page_size)
+int check_page_range(const int32_t *table, int32_t max_pages, int32_t num_pages, int b, int64_t from, int64_t to) {
+    if (from >= to) return WS_OK;
+    if (to > (int64_t)max_pages * WS_PAGE_SIZE)
         return fail(WS_ERR_CAPACITY, "stream %d needs %lld tokens but holds at most %lld", b,
-                    (long long)n, (long long)kv->max_pages_per_seq * kv->page_size);
-    const int64_t pages = (n + kv->page_size - 1) / kv->page_size;
-    const int32_t *row = kv->page_table_host + (int64_t)b * kv->max_pages_per_seq;
-    for (int64_t p = 0; p < pages; ++p)
-        if (row[p] < 0 || row[p] >= kv->num_pages)
+                    (long long)to, (long long)max_pages * WS_PAGE_SIZE);
+    const int64_t pages = (to + WS_PAGE_SIZE - 1) / WS_PAGE_SIZE;
+    const int32_t *row = table + (int64_t)b * max_pages;
+    for (int64_t p = from / WS_PAGE_SIZE; p < pages; ++p)
+        if (row[p] < 0 || row[p] >= num_pages)
             return fail(WS_ERR_PAGE, "page_table[%d][%lld] = %d outside [0, %d)", b, (long long)p,
-                        (int)row[p], (int)kv->num_pages);
+                        (int)row[p], (int)num_pages);
     return WS_OK;
 }
 
-struct StepPlan {
-    ws::TileShape shape;
-    int nqt;
-    int nsplit;
+// Every page that positions [0, n) of stream b live in must exist.
+int check_pages(const ws_paged_kv *kv, int b, int64_t n) {
+    return check_page_range(kv->page_table_host, kv->max_pages_per_seq, kv->num_pages, b, 0, n);
+}
+
+// A sliding window and the first tokens that stay visible (nullptr: none).
+struct Window {
+    int32_t sinks, window;
 };
+int check_window(const Window *w) {
+    if (w && (w->sinks < 0 || w->window < 0))
+        return fail(WS_ERR_SHAPE, "sinks %d, window %d", (int)w->sinks, (int)w->window);
+    return WS_OK;
+}
+// 64-key tiles of keys [0, end) that rows see whose windows start at key lo:
+// those of the sinks and those from lo on.
+int64_t live_tiles(const Window &w, int64_t lo, int64_t end) {
+    const int64_t first = std::max<int64_t>(lo, 0) / 64;
+    return std::min(((int64_t)w.sinks + 63) / 64, first) + (end + 63) / 64 - first;
+}
 
 // Query tile and KV split count of a streaming step.
 // One launch shape: 8 waves x 32 query rows (256-query tiles).
@@ -140,7 +151,7 @@ constexpr int64_t SPLIT_FIXED_TILES = 4;
 // when the items do not fill the last round (a batch of 3 or 5 long
 // streams, or new blocks of different lengths, nl != NULL, whose tiles of
 // padding only do no work).
-StepPlan plan_step(int num_cus, int batch, int hq, int hkv, int lq, int64_t max_k, const int32_t *nl = nullptr) {
+StepPlan plan_step(int num_cus, int batch, int hq, int hkv, int lq, int64_t max_k, const int32_t *nl) {
     StepPlan p;
     p.shape = default_shape();
     const int64_t qt = p.shape.qtile();
@@ -297,6 +308,36 @@ ws::TileShape plan_prefill(int num_cus, int batch, int hq, int seq, const int32_
     return s;
 }
 
+// The same for a windowed prefill.  Its items hardly differ in length, so the
+// time is the rounds of them times the longest: its live tiles and the fixed
+// costs above (a 128-row item: 0.53 of its tiles, as each step loads two).
+ws::TileShape plan_prefill_window(int num_cus, int batch, int hq, int seq, const int32_t *offsets, const int32_t *text,
+                                  int num_blocks, const Window &w) {
+    ws::TileShape s = default_shape();
+    const int64_t n1 = ((int64_t)seq + 255) / 256, n2 = ((int64_t)seq + 127) / 128, items = (int64_t)batch * hq;
+    if (num_cus <= 0 || items * n1 > FEW_ROUNDS * num_cus) return s;
+    int64_t most[2] = {};   // live tiles of the longest 256-row and 128-row item
+    for (int b = 0; b < batch; ++b) {
+        const int32_t *off = offsets + (int64_t)b * (num_blocks + 1);
+        int64_t lo = 0, lo256 = 0;
+        for (int64_t i = 0, n = 0; i < seq; ++i) {
+            const bool first = i % 128 == 0, last = i % 128 == 127 || i == seq - 1;
+            if (!first && !last) continue;
+            while (off[n + 1] <= i) ++n;
+            const int32_t ts = text ? text[(int64_t)b * num_blocks + n] : off[n + 1];
+            if (first) lo = (i >= ts ? i : off[n]) - w.window;
+            if (i % 256 == 0) lo256 = lo;
+            if (!last) continue;
+            const int64_t end = std::max<int64_t>(ts, i + 1);
+            most[0] = std::max(most[0], live_tiles(w, lo256, end));
+            most[1] = std::max(most[1], live_tiles(w, lo, end));
+        }
+    }
+    auto rounds = [&](int64_t n) -> int64_t { return (n * items + num_cus - 1) / num_cus; };
+    if (rounds(n2) * (53 * most[1] + 300) < rounds(n1) * (100 * most[0] + 250)) s.kg = 2;
+    return s;
+}
+
 // Whether a prefill's items may be dealt to 2^deal classes per group.  Classes
 // of a group that are one item short get work-groups that find no item; each
 // holds a compute unit for about two key tiles.  They cost nothing while the
@@ -310,6 +351,16 @@ bool deal_pays(int cus, const ws::AttnArgs &a, int64_t groups, int deal, ws::Til
     // a causal item's mean tiles, in hundredths (as in plan_prefill)
     const int64_t mean = shape.kg == 2 ? 53 * (a.nqt + 1) + 300 : 200 * (a.nqt + 1) + 250;
     return items <= cus || (items <= (int64_t)1 << 22 && 20 * 200 * none <= mean * a.n_work);
+}
+
+// Keys of the most that one stream's rows see through a window, in whole tiles.
+int64_t window_keys(const Window &w, int batch, int new_len, const int32_t *cache_lens, const int32_t *nl) {
+    int64_t most = 0;
+    for (int b = 0; b < batch; ++b) {
+        const int64_t n = cache_lens[b];
+        most = std::max(most, live_tiles(w, n - w.window, n + (nl ? nl[b] : new_len)));
+    }
+    return 64 * most;
 }
 
 // Splits of a step over streams whose key counts or block lengths differ.
@@ -449,8 +500,9 @@ size_t step_workspace(const StepPlan &p, int batch, int hq, int hkv, int lq) {
 size_t bwd_dl_bytes(int batch, int hq, int seq) {
     return ((size_t)batch * hq * seq * 2 * sizeof(float) + 255) / 256 * 256;
 }
-size_t bwd_rows_bytes(int batch, int hq, int seq) {
-    return bwd_dl_bytes(batch, hq, seq) + (size_t)batch * seq * sizeof(int32_t);
+// (windowed: also the first key of each token's window)
+size_t bwd_rows_bytes(int batch, int hq, int seq, bool windowed = false) {
+    return bwd_dl_bytes(batch, hq, seq) + (windowed ? 2 : 1) * (size_t)batch * seq * sizeof(int32_t);
 }
 
 // dK/dV work-groups: by default one per (stream, KV head, 128 keys), which
@@ -524,7 +576,9 @@ BwdPlan plan_bwd(int num_cus, int batch, int hq, int hkv, int seq, const int32_t
     return p;
 }
 
-size_t bwd_part_offset(int batch, int hq, int seq) { return (bwd_rows_bytes(batch, hq, seq) + 255) / 256 * 256; }
+size_t bwd_part_offset(int batch, int hq, int seq, bool windowed = false) {
+    return (bwd_rows_bytes(batch, hq, seq, windowed) + 255) / 256 * 256;
+}
 
 // bytes of the partial sums of one part: 2 x 128 keys x D floats per group
 // (the largest head dim, which the size query does not know)
@@ -540,6 +594,67 @@ size_t bwd_workspace(int batch, int hq, int hkv, int seq) {
     const BwdPlan p = plan_bwd(CHIP_CUS, batch, hq, hkv, seq, nullptr, INT32_MAX);
     if (!p.split_tiles) return bwd_rows_bytes(batch, hq, seq);
     return bwd_part_offset(batch, hq, seq) + p.tile_start[p.split_tiles] * bwd_part_bytes(batch, hkv);
+}
+
+// dK/dV work-groups of a windowed launch: the key tiles of the sinks are seen by
+// every later row and the others by about `rows` rows each, so the sinks' tiles
+// are split into more parts; both kinds are where the items would leave the
+// chip idle.  The least modelled time (in steps of two chunks, as plan_bwd):
+// the longest part, or the mean load of a unit and 0.3 of the longest, plus the
+// cost of the partial sums.  max_parts: room for partial sums.
+struct BwdWindowPlan {
+    int sink_tiles = 0, sink_parts = 1, tile_parts = 1, tiles = 0;
+    int64_t parts() const {   // slots of partial sums (0: nothing is split)
+        const int64_t rest = tiles - sink_tiles;
+        if (tile_parts > 1) return (int64_t)sink_tiles * sink_parts + rest * tile_parts;
+        return sink_parts > 1 ? (int64_t)sink_tiles * sink_parts : 0;
+    }
+};
+BwdWindowPlan plan_bwd_window(int num_cus, int batch, int hq, int hkv, int seq, const Window &w, int64_t rows,
+                              int64_t max_parts) {
+    BwdWindowPlan p;
+    p.tiles = (seq + 127) / 128;
+    p.sink_tiles = (int)std::min<int64_t>(((int64_t)w.sinks + 127) / 128, p.tiles);
+    if (num_cus <= 0) return p;
+    const int64_t ngrp = (int64_t)batch * hkv, G = hq / hkv, rest = p.tiles - p.sink_tiles;
+    const double sink_steps = G * ((seq + 31) / 32) / 2.0, tile_steps = G * ((std::min<int64_t>(rows, seq) + 31) / 32) / 2.0;
+    constexpr double FIXED = 5, PART = 4, SUM = 3;   // (plan_bwd)
+    const BwdWindowPlan whole = p;
+    double best = 0, unsplit = 0;
+    BwdWindowPlan at = p;
+    for (int tp = 1; tp <= 8; ++tp)
+        for (int sp = 1; sp <= 64; sp = sp < 8 ? sp + 1 : sp + sp / 4) {
+            at.tile_parts = tp;
+            at.sink_parts = sp;
+            if (at.parts() > max_parts) continue;
+            const double s = sink_steps / sp + FIXED + (sp > 1 ? PART : 0), t = tile_steps / tp + FIXED + (tp > 1 ? PART : 0);
+            const int64_t ns = p.sink_tiles * sp, nt = rest * tp;
+            const double longest = std::max(ns ? s : 0, nt ? t : 0), mean = (ns * s + nt * t) * ngrp / num_cus;
+            double cost = std::max(longest, mean + ((ns + nt) * ngrp > num_cus ? 0.3 * longest : 0));
+            if (at.parts()) cost += SUM + PART * ((sp > 1 ? ns : 0) + (tp > 1 ? nt : 0)) * ngrp / num_cus;
+            if (tp == 1 && sp == 1) best = unsplit = cost;
+            if (cost < 0.97 * best) {
+                best = cost;
+                p = at;
+            }
+        }
+    return best < 0.9 * unsplit ? p : whole;   // (a split has to win 10 %)
+}
+
+// Rows that see an average key tile past the sinks: the rows of every 128 keys
+// from the first that sees one of them to the last whose window reaches it.
+int64_t window_rows(const Window &w, int batch, int seq, const int32_t *offsets, const int32_t *text, int num_blocks) {
+    // a row's window and block: rows up to window + 128 keys behind a tile, and
+    // those of the blocks that straddle its ends
+    int64_t longest = 0;
+    for (int b = 0; b < batch; ++b) {
+        const int32_t *off = offsets + (int64_t)b * (num_blocks + 1);
+        for (int n = 0; n < num_blocks; ++n) {
+            const int32_t end = text ? text[(int64_t)b * num_blocks + n] : off[n + 1];
+            longest = std::max<int64_t>(longest, end - off[n]);
+        }
+    }
+    return std::min<int64_t>((int64_t)w.window + 128 + longest, seq);
 }
 
 // Total work items; fails when the grid would not fit the kernel's int math.
@@ -566,18 +681,25 @@ int step_impl(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new, const ws_paged_k
               const int32_t *text_host, const int32_t *text_dev, int32_t batch,
               int32_t new_len, int32_t num_q_heads, float scale, int32_t flags,
               ws_tensor4 out, float *lse, void *workspace, size_t workspace_bytes,
-              void *stream, bool noalloc = false);
+              void *stream, bool noalloc = false, const Window *win = nullptr);
 int append_impl(const ws_paged_kv *kv, int32_t batch, const int32_t *cache_lens_host,
                 const int32_t *cache_lens_dev, const int32_t *nl_host, const int32_t *nl_dev, int32_t new_len,
                 ws_tensor4 k_new, ws_tensor4 v_new, void *stream);
+int bwd_impl(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 o, ws_tensor4 dout, const float *lse,
+             const int32_t *block_offsets_host, const int32_t *block_offsets_dev, const int32_t *text_starts_host,
+             const int32_t *text_starts_dev, int32_t batch, int32_t seq_len, int32_t num_blocks, int32_t num_q_heads,
+             int32_t num_kv_heads, int32_t head_dim, float scale, ws_tensor4 dq, ws_tensor4 dk, ws_tensor4 dv,
+             void *workspace, size_t workspace_bytes, void *stream, const Window *win);
 int prefill_impl(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const ws_paged_kv *kv_or_null,
                  const int32_t *block_offsets_host, const int32_t *block_offsets_dev,
                  const int32_t *text_host, const int32_t *text_dev,
                  int32_t batch, int32_t seq_len, int32_t num_blocks, int32_t num_q_heads,
                  int32_t num_kv_heads, int32_t head_dim, float scale, ws_tensor4 out,
-                 float *lse, void *stream);
+                 float *lse, void *stream, const Window *win = nullptr);
 
-}  // namespace
+}  // namespace ws
+
+using namespace ws;
 
 extern "C" {
 
@@ -616,7 +738,7 @@ size_t ws_workspace_bytes(int32_t op, int32_t batch, int32_t num_q_heads, int32_
     if ((int64_t)(num_q_heads / num_kv_heads) * max_q > WS_MAX_STEP_ROWS) return 0;
     int cus = 0;
     if (ws::current_device_cus(&cus)) return 0;
-    const StepPlan p = plan_step(cus, batch, num_q_heads, num_kv_heads, max_q, max_k);
+    const StepPlan p = plan_step(cus, batch, num_q_heads, num_kv_heads, max_q, max_k, nullptr);
     return step_workspace(p, batch, num_q_heads, num_kv_heads, max_q);
 }
 
@@ -747,6 +869,52 @@ int ws_block_causal_prefill_text(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const
                         scale, out, lse, stream);
 }
 
+int ws_block_causal_attn_fwd_window(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new, const ws_paged_kv *kv,
+                                    const int32_t *cache_lens_host, const int32_t *cache_lens_dev,
+                                    const int32_t *new_lens_host, const int32_t *new_lens_dev,
+                                    const int32_t *text_starts_host, const int32_t *text_starts_dev,
+                                    int32_t batch, int32_t new_len, int32_t num_q_heads, int32_t sinks,
+                                    int32_t window, float scale, int32_t flags, ws_tensor4 out, float *lse,
+                                    void *workspace, size_t workspace_bytes, void *stream) {
+    if (!new_lens_host != !new_lens_dev) return fail(WS_ERR_NULL, "new_lens: give both copies or neither");
+    if (!text_starts_host != !text_starts_dev) return fail(WS_ERR_NULL, "text_starts: give both copies or neither");
+    const Window win{sinks, window};
+    return step_impl(q, k_new, v_new, kv, cache_lens_host, cache_lens_dev, new_lens_host, new_lens_dev,
+                     text_starts_host, text_starts_dev, batch, new_len, num_q_heads, scale, flags, out, lse,
+                     workspace, workspace_bytes, stream, false, &win);
+}
+
+size_t ws_step_workspace_bytes_window(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t new_len,
+                                      const int32_t *cache_lens_host, const int32_t *new_lens_host, int32_t sinks,
+                                      int32_t window) {
+    if (batch <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads || new_len <= 0 ||
+        !cache_lens_host || sinks < 0 || window < 0)
+        return 0;
+    if ((int64_t)(num_q_heads / num_kv_heads) * new_len > WS_MAX_STEP_ROWS) return 0;
+    for (int b = 0; b < batch; ++b) {
+        const int32_t nl = new_lens_host ? new_lens_host[b] : new_len;
+        if (cache_lens_host[b] < 0 || nl < 1 || nl > new_len || (int64_t)cache_lens_host[b] + nl > INT32_MAX) return 0;
+    }
+    int cus = 0;
+    if (ws::current_device_cus(&cus)) return 0;
+    const int64_t keys = window_keys(Window{sinks, window}, batch, new_len, cache_lens_host, new_lens_host);
+    const StepPlan p = plan_step(cus, batch, num_q_heads, num_kv_heads, new_len, keys, new_lens_host);
+    return step_workspace(p, batch, num_q_heads, num_kv_heads, new_len);
+}
+
+int ws_block_causal_prefill_window(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const ws_paged_kv *kv_or_null,
+                                   const int32_t *block_offsets_host, const int32_t *block_offsets_dev,
+                                   const int32_t *text_starts_host, const int32_t *text_starts_dev, int32_t batch,
+                                   int32_t seq_len, int32_t num_blocks, int32_t num_q_heads, int32_t num_kv_heads,
+                                   int32_t head_dim, int32_t sinks, int32_t window, float scale, ws_tensor4 out,
+                                   float *lse, void *stream) {
+    if (!text_starts_host != !text_starts_dev) return fail(WS_ERR_NULL, "text_starts: give both copies or neither");
+    const Window win{sinks, window};
+    return prefill_impl(q, k, v, kv_or_null, block_offsets_host, block_offsets_dev, text_starts_host,
+                        text_starts_dev, batch, seq_len, num_blocks, num_q_heads, num_kv_heads, head_dim,
+                        scale, out, lse, stream, &win);
+}
+
 int ws_block_causal_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 o, ws_tensor4 dout,
                                 const float *lse, const int32_t *block_offsets_host,
                                 const int32_t *block_offsets_dev, const int32_t *text_starts_host,
@@ -754,9 +922,49 @@ int ws_block_causal_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_ten
                                 int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float scale,
                                 ws_tensor4 dq, ws_tensor4 dk, ws_tensor4 dv, void *workspace,
                                 size_t workspace_bytes, void *stream) {
+    return bwd_impl(q, k, v, o, dout, lse, block_offsets_host, block_offsets_dev, text_starts_host, text_starts_dev,
+                    batch, seq_len, num_blocks, num_q_heads, num_kv_heads, head_dim, scale, dq, dk, dv, workspace,
+                    workspace_bytes, stream, nullptr);
+}
+
+int ws_block_causal_prefill_window_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 o, ws_tensor4 dout,
+                                       const float *lse, const int32_t *block_offsets_host,
+                                       const int32_t *block_offsets_dev, const int32_t *text_starts_host,
+                                       const int32_t *text_starts_dev, int32_t batch, int32_t seq_len,
+                                       int32_t num_blocks, int32_t num_q_heads, int32_t num_kv_heads,
+                                       int32_t head_dim, int32_t sinks, int32_t window, float scale, ws_tensor4 dq,
+                                       ws_tensor4 dk, ws_tensor4 dv, void *workspace, size_t workspace_bytes,
+                                       void *stream) {
+    const Window win{sinks, window};
+    return bwd_impl(q, k, v, o, dout, lse, block_offsets_host, block_offsets_dev, text_starts_host, text_starts_dev,
+                    batch, seq_len, num_blocks, num_q_heads, num_kv_heads, head_dim, scale, dq, dk, dv, workspace,
+                    workspace_bytes, stream, &win);
+}
+
+size_t ws_prefill_window_bwd_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                             int32_t seq_len, int32_t sinks, int32_t window) {
+    if (batch <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads || seq_len <= 0 ||
+        sinks < 0 || window < 0)
+        return 0;
+    const BwdWindowPlan p = plan_bwd_window(CHIP_CUS, batch, num_q_heads, num_kv_heads, seq_len, Window{sinks, window},
+                                            std::min<int64_t>((int64_t)window + 128, seq_len), INT64_MAX);
+    return bwd_part_offset(batch, num_q_heads, seq_len, true) + p.parts() * bwd_part_bytes(batch, num_kv_heads);
+}
+
+}  // extern "C"
+
+namespace ws {
+
+// Gradients of a whole sequence (win nullptr: no window).
+int bwd_impl(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 o, ws_tensor4 dout, const float *lse,
+             const int32_t *block_offsets_host, const int32_t *block_offsets_dev, const int32_t *text_starts_host,
+             const int32_t *text_starts_dev, int32_t batch, int32_t seq_len, int32_t num_blocks, int32_t num_q_heads,
+             int32_t num_kv_heads, int32_t head_dim, float scale, ws_tensor4 dq, ws_tensor4 dk, ws_tensor4 dv,
+             void *workspace, size_t workspace_bytes, void *stream, const Window *win) {
     if (batch < 0 || seq_len < 0 || num_blocks < 0 || num_q_heads <= 0 || num_kv_heads <= 0)
         return fail(WS_ERR_SHAPE, "batch %d, seq_len %d, num_blocks %d, heads %d/%d", (int)batch, (int)seq_len,
                     (int)num_blocks, (int)num_q_heads, (int)num_kv_heads);
+    if (int rc = check_window(win)) return rc;
     if (batch == 0 || seq_len == 0) return ok();
     if (int rc = check_tensor("q", q, false)) return rc;
     if (int rc = check_tensor("k", k, false)) return rc;
@@ -766,8 +974,9 @@ int ws_block_causal_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_ten
     if (int rc = check_tensor("dq", dq, true)) return rc;
     if (int rc = check_tensor("dk", dk, true)) return rc;
     if (int rc = check_tensor("dv", dv, true)) return rc;
-    if (dq.dtype != WS_DTYPE_F32 || dk.dtype != WS_DTYPE_F32 || dv.dtype != WS_DTYPE_F32)
-        return fail(WS_ERR_UNSUPPORTED, "dq, dk and dv must be f32");
+    const int32_t grads = win ? dq.dtype : (int32_t)WS_DTYPE_F32;
+    if (dq.dtype != grads || dk.dtype != grads || dv.dtype != grads)
+        return fail(WS_ERR_UNSUPPORTED, win ? "dq, dk and dv must be of one dtype" : "dq, dk and dv must be f32");
     if (!lse) return fail(WS_ERR_NULL, "lse is NULL");
     if ((uintptr_t)lse & 3u) return fail(WS_ERR_ALIGN, "lse must be 4-byte aligned");
     if (!block_offsets_host || !block_offsets_dev) return fail(WS_ERR_NULL, "block offsets pointer is NULL");
@@ -796,7 +1005,10 @@ int ws_block_causal_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_ten
     }
     const int64_t work = (int64_t)batch * num_q_heads * ((seq_len + 127) / 128);
     if (work > INT32_MAX) return fail(WS_ERR_SHAPE, "too many work items");
-    const size_t need = bwd_rows_bytes(batch, num_q_heads, seq_len);
+    // (the kernels count both grids in 32 bits)
+    if (win && (int64_t)batch * num_kv_heads * ((seq_len + 127) / 128 + 16) * 64 > INT32_MAX)
+        return fail(WS_ERR_SHAPE, "too many work items");
+    const size_t need = bwd_rows_bytes(batch, num_q_heads, seq_len, win != nullptr);
     if (!workspace || workspace_bytes < need || !aligned16(workspace))
         return fail(WS_ERR_WORKSPACE, "workspace needs %zu bytes (16-byte aligned), got %zu", need,
                     workspace ? workspace_bytes : (size_t)0);
@@ -822,8 +1034,23 @@ int ws_block_causal_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_ten
     a.scale_log2 = scale * 1.4426950408889634f;
     // the split needs room for its partial sums; a workspace that only holds
     // the row data runs without
-    const size_t part_at = bwd_part_offset(batch, num_q_heads, seq_len), part_bytes = bwd_part_bytes(batch, num_kv_heads);
-    if (workspace_bytes >= part_at + 2 * part_bytes && seq_len <= 128 * ws::BWD_MAX_SPLIT_TILES) {
+    const size_t part_at = bwd_part_offset(batch, num_q_heads, seq_len, win != nullptr);
+    const size_t part_bytes = bwd_part_bytes(batch, num_kv_heads);
+    if (win) {
+        a.has_window = 1;
+        a.sinks = win->sinks;
+        a.window = win->window;
+        a.grads_bf16 = grads == WS_DTYPE_BF16;
+        a.part = (float *)((char *)workspace + part_at);
+        const int64_t room = workspace_bytes > part_at ? (int64_t)((workspace_bytes - part_at) / part_bytes) : 0;
+        int cus = 0;
+        if (ws::current_device_cus(&cus)) cus = 0;
+        const int64_t rows = window_rows(*win, batch, seq_len, block_offsets_host, text_starts_host, num_blocks);
+        const BwdWindowPlan p = plan_bwd_window(cus, batch, num_q_heads, num_kv_heads, seq_len, *win, rows, room);
+        a.sink_tiles = p.sink_tiles;
+        a.sink_parts = p.sink_parts;
+        a.tile_parts = p.tile_parts;
+    } else if (workspace_bytes >= part_at + 2 * part_bytes && seq_len <= 128 * ws::BWD_MAX_SPLIT_TILES) {
         // the first row of any stream that sees each tile's first key
         int32_t first_row[ws::BWD_MAX_SPLIT_TILES];
         for (int kt = 0; kt < (seq_len + 127) / 128; ++kt) first_row[kt] = 128 * kt;
@@ -850,10 +1077,6 @@ int ws_block_causal_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_ten
         return fail(WS_ERR_HIP, "backward launch failed (hip error %d)", e);
     return ok();
 }
-
-}  // extern "C"
-
-namespace {
 
 // Commit new tokens to the cache (nl_* NULL: new_len tokens per stream).
 int append_impl(const ws_paged_kv *kv, int32_t batch, const int32_t *cache_lens_host,
@@ -895,8 +1118,9 @@ int step_impl(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new, const ws_paged_k
               const int32_t *text_host, const int32_t *text_dev, int32_t batch,
               int32_t new_len, int32_t num_q_heads, float scale, int32_t flags,
               ws_tensor4 out, float *lse, void *workspace, size_t workspace_bytes,
-              void *stream, bool noalloc) {
+              void *stream, bool noalloc, const Window *win) {
     if (int rc = check_paged(kv)) return rc;
+    if (int rc = check_window(win)) return rc;
     if (!cache_lens_host || !cache_lens_dev) return fail(WS_ERR_NULL, "cache_lens pointer is NULL");
     if (batch < 0 || new_len < 0 || num_q_heads <= 0)
         return fail(WS_ERR_SHAPE, "batch %d, new_len %d, num_q_heads %d", (int)batch, (int)new_len, (int)num_q_heads);
@@ -918,9 +1142,17 @@ int step_impl(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new, const ws_paged_k
         if (nl_host && (nl_host[b] < 1 || nl_host[b] > new_len))
             return fail(WS_ERR_SHAPE, "new_lens[%d] = %d outside [1, new_len %d]", b, (int)nl_host[b], (int)new_len);
         const int64_t nl = nl_host ? nl_host[b] : new_len;
-        const int64_t need = (int64_t)cache_lens_host[b] + (fuse ? nl : 0);
-        if (int rc = check_pages(kv, b, need)) return rc;
-        if ((int64_t)cache_lens_host[b] + nl > max_k) max_k = (int64_t)cache_lens_host[b] + nl;
+        const int64_t n = cache_lens_host[b], need = n + (fuse ? nl : 0);
+        if (win) {   // only the sinks' and the window's pages are read
+            auto pages = [&](int64_t from, int64_t to) {
+                return check_page_range(kv->page_table_host, kv->max_pages_per_seq, kv->num_pages, b, from, to);
+            };
+            if (int rc = pages(0, std::min<int64_t>(win->sinks, n))) return rc;
+            if (int rc = pages(std::max<int64_t>(n - win->window, 0), need)) return rc;
+        } else if (int rc = check_pages(kv, b, need)) {
+            return rc;
+        }
+        if (n + nl > max_k) max_k = n + nl;
     }
     if (max_k > INT32_MAX) return fail(WS_ERR_SHAPE, "too many keys");
     if (text_host)
@@ -933,8 +1165,9 @@ int step_impl(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new, const ws_paged_k
     int cus = 0;
     if (int e = ws::current_device_cus(&cus))
         return fail(WS_ERR_HIP, "cannot query the device's compute units (hip error %d)", e);
+    if (win) max_k = window_keys(*win, batch, new_len, cache_lens_host, nl_host);
     StepPlan plan = plan_step(cus, batch, num_q_heads, kv->num_kv_heads, new_len, max_k, nl_host);
-    plan.shape.parts_only = parts_only(plan, max_k, out.dtype == WS_DTYPE_F32);
+    plan.shape.parts_only = !win && parts_only(plan, max_k, out.dtype == WS_DTYPE_F32);
     const size_t need_ws = step_workspace(plan, batch, num_q_heads, kv->num_kv_heads, new_len);
     if (noalloc) {
         // the library's per-device scratch array stands in for the workspace
@@ -996,10 +1229,16 @@ int step_impl(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new, const ws_paged_k
         }
     }
     if (!finish_work(a)) return fail(WS_ERR_SHAPE, "too many work items");
-    // streams of different lengths: per-stream splits
+    if (win) {
+        a.has_window = 1;
+        a.sinks = win->sinks;
+        a.window = win->window;
+    }
+    // streams of different lengths: per-stream splits (a window makes all long
+    // streams alike: one count)
     ws::RaggedPlan rag;
     const int64_t slot_bytes = (int64_t)a.Hkv * a.nrb * 32 * kv->head_dim * (a.out_f32 ? 4 : 2);
-    const bool ragged = plan_ragged(rag, cus, plan, batch, num_q_heads, kv->num_kv_heads, new_len, cache_lens_host,
+    const bool ragged = !win && plan_ragged(rag, cus, plan, batch, num_q_heads, kv->num_kv_heads, new_len, cache_lens_host,
                                     nl_host, text_host, slot_bytes);
     if (ragged) {
         a.per_group = rag.deal * rag.per_class;
@@ -1021,10 +1260,11 @@ int prefill_impl(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const ws_paged_kv *kv
                  const int32_t *text_host, const int32_t *text_dev,
                  int32_t batch, int32_t seq_len, int32_t num_blocks, int32_t num_q_heads,
                  int32_t num_kv_heads, int32_t head_dim, float scale, ws_tensor4 out,
-                 float *lse, void *stream) {
+                 float *lse, void *stream, const Window *win) {
     if (batch < 0 || seq_len < 0 || num_blocks < 0 || num_q_heads <= 0 || num_kv_heads <= 0)
         return fail(WS_ERR_SHAPE, "batch %d, seq_len %d, num_blocks %d, heads %d/%d", (int)batch, (int)seq_len,
                     (int)num_blocks, (int)num_q_heads, (int)num_kv_heads);
+    if (int rc = check_window(win)) return rc;
     if (batch == 0 || seq_len == 0) return ok();  // no token: nothing is read or written
     const bool paged = !k.ptr && !v.ptr;
     if (paged) {
@@ -1068,7 +1308,9 @@ int prefill_impl(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const ws_paged_kv *kv
 
     int cus = 0;
     if (ws::current_device_cus(&cus)) cus = 0;   // (the launch reports it)
-    ws::TileShape shape = plan_prefill(cus, batch, num_q_heads, seq_len, block_offsets_host, text_host, num_blocks);
+    ws::TileShape shape = win ? plan_prefill_window(cus, batch, num_q_heads, seq_len, block_offsets_host, text_host,
+                                                    num_blocks, *win)
+                              : plan_prefill(cus, batch, num_q_heads, seq_len, block_offsets_host, text_host, num_blocks);
     ws::AttnArgs a{};
     a.q = (const uint16_t *)q.ptr; a.q_sb = q.stride_b; a.q_st = q.stride_t; a.q_sh = q.stride_h;
     if (paged) {
@@ -1095,6 +1337,11 @@ int prefill_impl(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const ws_paged_kv *kv
     a.nrows = seq_len;
     a.nqt = (seq_len + shape.qtile() - 1) / shape.qtile();
     a.scale_log2 = scale * 1.4426950408889634f;
+    if (win) {
+        a.has_window = 1;
+        a.sinks = win->sinks;
+        a.window = win->window;
+    }
     if (!finish_work(a)) return fail(WS_ERR_SHAPE, "too many work items");
     // Launch order.  An XCD's contiguous range of items cut through a group
     // whenever the (stream, KV head) groups are no multiple of 8, giving one
@@ -1116,4 +1363,4 @@ int prefill_impl(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const ws_paged_kv *kv
     return ok();
 }
 
-}  // namespace
+}  // namespace ws

@@ -39,7 +39,33 @@ struct Abi {
     decltype(&ws_step_workspace_bytes_varlen) workspace_bytes_varlen;
 } abi;
 
+struct WindowAbi {
+    decltype(&ws_block_causal_attn_fwd_window) fwd;
+    decltype(&ws_step_workspace_bytes_window) step_bytes;
+    decltype(&ws_block_causal_prefill_window) prefill;
+    decltype(&ws_block_causal_prefill_window_bwd) bwd;
+    decltype(&ws_prefill_window_bwd_workspace_bytes) bwd_bytes;
+} wabi;
+
 PyObject *cache_class;   // PagedCache
+
+bool take_addresses(void **to, size_t count, PyObject *const *args, Py_ssize_t n) {
+    if (n != (Py_ssize_t)count) {
+        PyErr_SetString(PyExc_TypeError, "one address per ABI function");
+        return false;
+    }
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        void *p = PyLong_AsVoidPtr(args[i]);
+        if (PyErr_Occurred()) return false;
+        to[i] = p;
+    }
+    return true;
+}
+
+PyObject *bind_window(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (!take_addresses((void **)&wabi, sizeof wabi / sizeof(void *), args, n)) return nullptr;
+    Py_RETURN_NONE;
+}
 
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (n != 1 + (Py_ssize_t)(sizeof(Abi) / sizeof(void *))) {
@@ -173,6 +199,18 @@ bool flag(PyObject *o, bool &b) {
     return true;
 }
 
+// window and sinks, checked by the Python code (ints in [0, 2^31)); without them
+// window is -1
+struct Window {
+    int32_t window = -1, sinks = 0;
+};
+bool window_of(PyObject *w, PyObject *s, Window &x) {
+    if (!PyLong_CheckExact(w) || !PyLong_CheckExact(s)) return false;
+    x.window = (int32_t)PyLong_AsLong(w);
+    x.sinks = (int32_t)PyLong_AsLong(s);
+    return true;
+}
+
 at::ScalarType dtype_of(PyObject *o) {
     return THPDtype_Check(o) ? ((THPDtype *)o)->scalar_type : at::kDouble;
 }
@@ -220,9 +258,8 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // step(q, k_new, v_new, cache, lens, scale, fuse_append, out, out_dtype,
 //      want_lse, lse, workspace, text_starts, new_lens, noalloc)
 //   -> (status, out, lse), or None
-PyObject *step(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    HANDLE_TH_ERRORS
-    if (n != 15) Py_RETURN_NONE;
+// (step_window: and window, sinks)
+PyObject *step_of(PyObject *const *a, const Window &win) {
     const at::Tensor *q = tensor(a[0]);
     if (!q || q->dim() != 4) Py_RETURN_NONE;
     const int64_t B = q->size(0), L = q->size(1), H = q->size(2), D = q->size(3);
@@ -263,14 +300,18 @@ PyObject *step(PyObject *, PyObject *const *a, Py_ssize_t n) {
         } else if (!noalloc) {
             int32_t most = 0;
             for (int64_t b = 0; b < B; ++b) most = std::max(most, lens.host[b * lens.h->stride(0)]);
-            wn = nl.host ? abi.workspace_bytes_varlen(B, H, kv.num_kv_heads, L, lens.host, nl.host)
-                         : abi.workspace_bytes(WS_OP_STEP, B, H, kv.num_kv_heads, L, (int32_t)std::min<int64_t>(most + L, INT32_MAX));
+            wn = win.window >= 0 ? wabi.step_bytes(B, H, kv.num_kv_heads, L, lens.host, nl.host, win.sinks, win.window)
+               : nl.host ? abi.workspace_bytes_varlen(B, H, kv.num_kv_heads, L, lens.host, nl.host)
+                       : abi.workspace_bytes(WS_OP_STEP, B, H, kv.num_kv_heads, L, (int32_t)std::min<int64_t>(most + L, INT32_MAX));
             if (wn) {
                 own = at::empty({(int64_t)wn}, q->options().dtype(at::kByte));
                 wp = own.data_ptr();
             }
         }
-        if (noalloc)
+        if (win.window >= 0)
+            rc = wabi.fwd(qd, kd, vd, &kv, lens.host, lens.dev, nl.host, nl.dev, text.host, text.dev, B, L, H, win.sinks,
+                          win.window, scale, flags, od, lp, wp, wn, stream());
+        else if (noalloc)
             rc = abi.fwd_noalloc(qd, kd, vd, &kv, lens.host, lens.dev, B, L, H, scale, flags, od, lp, stream());
         else if (nl.host)
             rc = abi.fwd_varlen(qd, kd, vd, &kv, lens.host, lens.dev, nl.host, nl.dev, text.host, text.dev, B, L, H, scale,
@@ -282,14 +323,27 @@ PyObject *step(PyObject *, PyObject *const *a, Py_ssize_t n) {
             rc = abi.fwd(qd, kd, vd, &kv, lens.host, lens.dev, B, L, H, scale, flags, od, lp, wp, wn, stream());
     }
     return result(rc, {out, lse});
+}
+
+PyObject *step(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 15) Py_RETURN_NONE;
+    return step_of(a, Window{});
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *step_window(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Window win;
+    if (n != 17 || !window_of(a[15], a[16], win)) Py_RETURN_NONE;
+    return step_of(a, win);
     END_HANDLE_TH_ERRORS
 }
 
 // prefill(q, k, v, offsets, scale, cache, num_kv_heads, out, out_dtype,
 //         want_lse, lse, text_starts) -> (status, out, lse), or None
-PyObject *prefill(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    HANDLE_TH_ERRORS
-    if (n != 12) Py_RETURN_NONE;
+// (prefill_window: and window, sinks)
+PyObject *prefill_of(PyObject *const *a, const Window &win) {
     const at::Tensor *q = tensor(a[0]);
     if (!q || q->dim() != 4) Py_RETURN_NONE;
     const int64_t B = q->size(0), L = q->size(1), H = q->size(2), D = q->size(3);
@@ -340,19 +394,34 @@ PyObject *prefill(PyObject *, PyObject *const *a, Py_ssize_t n) {
         token_tensor(&out, {B, L, H, D}, od);
         if (with_lse) allocate(lse, {B, H, L}, at::kFloat, *q);
         float *lp = lse.defined() ? (float *)lse.data_ptr() : nullptr;
-        rc = text.host ? abi.prefill_text(qd, kd, vd, kvp, off.host, off.dev, text.host, text.dev, B, L, nb, H, hkv, D, scale,
+        rc = win.window >= 0 ? wabi.prefill(qd, kd, vd, kvp, off.host, off.dev, text.host, text.dev, B, L, nb, H, hkv, D,
+                                            win.sinks, win.window, scale, od, lp, stream())
+           : text.host ? abi.prefill_text(qd, kd, vd, kvp, off.host, off.dev, text.host, text.dev, B, L, nb, H, hkv, D, scale,
                                           od, lp, stream())
                        : abi.prefill(qd, kd, vd, kvp, off.host, off.dev, B, L, nb, H, hkv, D, scale, od, lp, stream());
     }
     return result(rc, {out, lse});
+}
+
+PyObject *prefill(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 12) Py_RETURN_NONE;
+    return prefill_of(a, Window{});
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *prefill_window(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Window win;
+    if (n != 14 || !window_of(a[12], a[13], win)) Py_RETURN_NONE;
+    return prefill_of(a, win);
     END_HANDLE_TH_ERRORS
 }
 
 // prefill_bwd(q, k, v, o, dout, lse, offsets, scale, text_starts, dq, dk, dv,
 //             workspace) -> (status, dq, dk, dv), or None
-PyObject *prefill_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    HANDLE_TH_ERRORS
-    if (n != 13) Py_RETURN_NONE;
+// (prefill_window_bwd: and window, sinks, grad_dtype)
+PyObject *prefill_bwd_of(PyObject *const *a, const Window &win, at::ScalarType grads) {
     const at::Tensor *q = tensor(a[0]), *k = tensor(a[1]), *lse = tensor(a[5]);
     if (!q || q->dim() != 4 || !k || k->dim() != 4 || !lse) Py_RETURN_NONE;
     const int64_t B = q->size(0), L = q->size(1), H = q->size(2), D = q->size(3), hkv = k->size(2);
@@ -379,11 +448,13 @@ PyObject *prefill_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     int rc = -1;
     {
         NoGil free;
-        const size_t need = wsp ? 0 : abi.workspace_bytes(WS_OP_PREFILL_BWD, B, H, hkv, L, L);
+        const size_t need = wsp ? 0
+                          : win.window >= 0 ? wabi.bwd_bytes(B, H, hkv, L, win.sinks, win.window)
+                                            : abi.workspace_bytes(WS_OP_PREFILL_BWD, B, H, hkv, L, L);
         if (wsp || need) {
-            allocate(dq, {B, L, H, D}, at::kFloat, *q);
-            allocate(dk, {B, L, hkv, D}, at::kFloat, *q);
-            allocate(dv, {B, L, hkv, D}, at::kFloat, *q);
+            allocate(dq, {B, L, H, D}, grads, *q);
+            allocate(dk, {B, L, hkv, D}, grads, *q);
+            allocate(dv, {B, L, hkv, D}, grads, *q);
             token_tensor(&dq, {B, L, H, D}, dqd);
             token_tensor(&dk, {B, L, hkv, D}, dkd);
             token_tensor(&dv, {B, L, hkv, D}, dvd);
@@ -391,17 +462,40 @@ PyObject *prefill_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
                 own = at::empty({(int64_t)need}, q->options().dtype(at::kByte));
                 wsp = &own;
             }
-            rc = abi.bwd(qd, kd, vd, od, dd, (const float *)lse->data_ptr(), off.host, off.dev, text.host, text.dev, B, L, nb,
-                         H, hkv, D, scale, dqd, dkd, dvd, wsp->data_ptr(), wsp->numel(), stream());
+            const float *lp = (const float *)lse->data_ptr();
+            if (win.window >= 0)
+                rc = wabi.bwd(qd, kd, vd, od, dd, lp, off.host, off.dev, text.host, text.dev, B, L, nb, H, hkv, D, win.sinks,
+                              win.window, scale, dqd, dkd, dvd, wsp->data_ptr(), wsp->numel(), stream());
+            else
+                rc = abi.bwd(qd, kd, vd, od, dd, lp, off.host, off.dev, text.host, text.dev, B, L, nb, H, hkv, D, scale, dqd, dkd,
+                             dvd, wsp->data_ptr(), wsp->numel(), stream());
         }
     }
     if (rc < 0) Py_RETURN_NONE;   // (the Python code names the mistake)
     return result(rc, {dq, dk, dv});
+}
+
+PyObject *prefill_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 13) Py_RETURN_NONE;
+    return prefill_bwd_of(a, Window{}, at::kFloat);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *prefill_window_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Window win;
+    if (n != 16 || !window_of(a[13], a[14], win)) Py_RETURN_NONE;
+    return prefill_bwd_of(a, win, dtype_of(a[15]));
     END_HANDLE_TH_ERRORS
 }
 
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)())bind, METH_FASTCALL, "the cache class, then the C ABI's addresses in Abi's order"},
+    {"bind_window", (PyCFunction)(void (*)())bind_window, METH_FASTCALL, "the windowed ABI's addresses in WindowAbi's order"},
+    {"step_window", (PyCFunction)(void (*)())step_window, METH_FASTCALL, nullptr},
+    {"prefill_window", (PyCFunction)(void (*)())prefill_window, METH_FASTCALL, nullptr},
+    {"prefill_window_bwd", (PyCFunction)(void (*)())prefill_window_bwd, METH_FASTCALL, nullptr},
     {"append", (PyCFunction)(void (*)())append, METH_FASTCALL, nullptr},
     {"step", (PyCFunction)(void (*)())step, METH_FASTCALL, nullptr},
     {"prefill", (PyCFunction)(void (*)())prefill, METH_FASTCALL, nullptr},

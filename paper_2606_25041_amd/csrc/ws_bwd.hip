@@ -60,6 +60,14 @@ __device__ __forceinline__ void tr_bases(int lane, uint32_t (&tb)[2]) {
     }
 }
 
+// Four neighbouring gradient values to element ofs of a f32 or bf16 tensor
+// (bf16: one rounding of the finished f32 sums).
+template <bool BF16>
+__device__ __forceinline__ void store_grad(float *base, int64_t ofs, f32x4 val) {
+    if constexpr (BF16) *(u32x2 *)((uint16_t *)base + ofs) = u32x2{pack_bf16x2(val[0], val[1]), pack_bf16x2(val[2], val[3])};
+    else *(f32x4 *)(base + ofs) = val;
+}
+
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
@@ -93,7 +101,10 @@ __device__ __forceinline__ void dma_rows(const char *g, int64_t st_bytes, int r0
 // masks run only on the tiles that straddle some row's key end: 2 x 16384
 // tokens, GQA 32/8 x 128: 6.1 -> 5.4 ms, bitwise the same dQ.  Two MFMAs of
 // read-ahead and three measured the same.
-template <int D>
+// WIN (sliding window with sinks): the tiles between the sinks and the first
+// row's window are never loaded, as in the forward; the first key of each
+// token's window goes to the dK/dV launch beside its key end.
+template <int D, bool WIN, bool BF16>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void bwd_dq_kernel(const BwdArgs a) {
     constexpr int ROWB = 2 * D, KK = D / 16, MD = D / 32;
     constexpr int TILEB = 64 * ROWB;
@@ -123,6 +134,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int k_hi = token_key_end(win, min(q0 + 127, a.L - 1), lane);
     const int kfull = token_key_end(win, q0, lane);
     const int my_kend = lane_key_end(win, min(q0 + 32 * wave, a.L - 1), rc, lane);
+    int my_klo = 0, lo_max = 0, nst = 0, gap = 0;
+    if constexpr (WIN) {
+        const int first = max(token_anchor(win, q0, lane) - a.window, 0) / 64;
+        lo_max = token_anchor(win, min(q0 + 127, a.L - 1), lane) - a.window;
+        my_klo = lane_anchor(win, min(q0 + 32 * wave, a.L - 1), rc, lane) - a.window;
+        nst = min((int)(((uint32_t)a.sinks + 63) / 64), first);
+        gap = first - nst;
+    }
+    auto tile_of = [&](int u) -> int { return WIN && u >= nst ? u + gap : u; };
     const float lse2 = a.lse[((int64_t)b * a.Hq + h) * a.L + rc] * 1.4426950408889634f;
     const float c2 = a.scale_log2;
 
@@ -162,7 +182,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         float *dl = a.dl + 2 * ((int64_t)b * a.Hq + h) * a.L + row;
         dl[0] = lse2;
         dl[a.L] = nD;
-        if (h == 0) a.kend[(int64_t)b * a.L + row] = my_kend;
+        if (h == 0) {
+            a.kend[(WIN ? 2 : 1) * (int64_t)b * a.L + row] = my_kend;
+            if constexpr (WIN) a.kend[(2 * (int64_t)b + 1) * a.L + row] = my_klo;
+        }
     }
     const char *kg = (const char *)(a.k + b * a.k_sb + g * a.k_sh);
     const char *vg = (const char *)(a.v + b * a.v_sb + g * a.v_sh);
@@ -178,8 +201,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const uint32_t lch = (uint32_t)(16 * ((lane % LPR) ^ swz<D>(lrow)));
     const uint32_t kofs = (uint32_t)lrow * (uint32_t)kst + lch, vofs = (uint32_t)lrow * (uint32_t)vst + lch;
     const bool wide = a.wide_strides != 0;
-    auto issue_part = [&](int t, int i) {
-        const uint32_t kl = lds_addr(smem) + (t & 1) * 2 * TILEB;
+    auto issue_part = [&](int u, int i) {
+        const uint32_t kl = lds_addr(smem) + (u & 1) * 2 * TILEB;
+        const int t = tile_of(u);
         if ((t + 1) * 64 > k_hi || wide) {
             if (i || t * 64 >= k_hi) return;
             // (the lane is hidden from the optimiser, so that what this rare
@@ -203,13 +227,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     for (int md = 0; md < MD; ++md)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[md][v] = 0.f;
-    const int ntile = (k_hi + 63) / 64;
+    const int ntile = (k_hi + 63) / 64 - gap;
 #pragma unroll
     for (int i = 0; i < 2 * NI; ++i) issue_part(0, i);
     wait_vm_lgkm<0>();
     wg_barrier();
-    for (int t = 0; t < ntile; ++t) {
-        const char *kt = smem + (t & 1) * 2 * TILEB, *vt = kt + TILEB;
+    for (int u = 0; u < ntile; ++u) {
+        const int t = tile_of(u);
+        const char *kt = smem + (u & 1) * 2 * TILEB, *vt = kt + TILEB;
         // One MFMA stream over the tile's two halves of 32 keys, every vector
         // instruction beside a matrix instruction that does not need it:
         // S0; dP0 beside P0 = exp2(S0 c2 - lse2); S1 beside dS0 = P0 (dP0 -
@@ -231,11 +256,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         // some row's end only (a real branch: the compiler would otherwise
         // turn this rare path into selects executed on every tile)
         auto mask = [&](int h) {
-            if ((t + 1) * 64 > kfull) {
+            if ((t + 1) * 64 > kfull || (WIN && t * 64 < lo_max && (t + 1) * 64 > a.sinks)) {
                 asm volatile("" ::: "memory");
 #pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    if (t * 64 + h * 32 + 8 * (v >> 2) + 4 * hf + (v & 3) >= my_kend) S[h][v] = 0.f;
+                for (int v = 0; v < 16; ++v) {
+                    const int key = t * 64 + h * 32 + 8 * (v >> 2) + 4 * hf + (v & 3);
+                    if (key >= my_kend || (WIN && key < my_klo && key >= a.sinks)) S[h][v] = 0.f;
+                }
             }
         };
 #pragma unroll
@@ -254,11 +281,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             else
                 dPt[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % (AH + 1)], dof[j % KK], dPt[h], 0, 0, 0);
 #pragma unroll
-            for (int u = 0; u < PS; ++u) {
-                if (j >= KK) weights(h, PS * (j - KK) + u);
-                else if (h == 1) grads(0, PS * j + u);
+            for (int e = 0; e < PS; ++e) {
+                if (j >= KK) weights(h, PS * (j - KK) + e);
+                else if (h == 1) grads(0, PS * j + e);
             }
-            if (i >= 1 && i <= 2 * NI) issue_part(t + 1, i - 1);
+            if (i >= 1 && i <= 2 * NI) issue_part(u + 1, i - 1);
             __builtin_amdgcn_sched_barrier(0);
             if (j == 2 * KK - 1) mask(h);
         }
@@ -271,7 +298,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                                                                  acc[i % MD], 0, 0, 0);
             if (i < 2 * MD) {
 #pragma unroll
-                for (int u = 0; u < PG; ++u) grads(1, PG * i + u);
+                for (int e = 0; e < PG; ++e) grads(1, PG * i + e);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -279,7 +306,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         wg_barrier();
     }
     if (row < a.L) {
-        float *op = a.dq + b * a.dq_sb + (int64_t)row * a.dq_st + h * a.dq_sh;
+        const int64_t ofs = b * a.dq_sb + (int64_t)row * a.dq_st + h * a.dq_sh;
 #pragma unroll
         for (int md = 0; md < MD; ++md)
 #pragma unroll
@@ -287,7 +314,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 f32x4 val;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) val[e] = acc[md][4 * gq + e] * a.scale;
-                *(f32x4 *)(op + 32 * md + 8 * gq + 4 * hf) = val;
+                store_grad<BF16>(a.dq, ofs + 32 * md + 8 * gq + 4 * hf, val);
             }
     }
 }
@@ -311,7 +338,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // measured the same.  A barrier per group of four waves instead of the
 // work-group's, with or without a half-step offset between the groups,
 // measured the same too.
-template <int D>
+// WIN (sliding window with sinks): a key is seen by the rows up to the last
+// whose window reaches it, so the chunks are counted from that row instead of
+// the sequence end; a key tile with sinks is seen to the end, and its parts
+// are separate work-groups (BwdArgs), the heaviest, dispatched first.
+template <int D, bool WIN, bool BF16>
 __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     constexpr int ROWB = 2 * D, KK = D / 16, MD = D / 32;
     constexpr int TILEK = 128 * ROWB, TILEC = 32 * ROWB;
@@ -319,7 +350,8 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     constexpr int SMEM = 2 * TILEK + 2 * 2 * 2 * TILEC;   // K, V; [group][stage][Q, dO]
     static_assert(2 * 4 * MD * 16 * 64 * 4 <= SMEM, "the partial sums fit the tiles' space");
     __shared__ __attribute__((aligned(1024))) char smem[SMEM];
-    __shared__ __attribute__((aligned(256))) float srow[2][2][128];   // [group][stage][lse2, -D, key end (twice) of 32 rows]
+    // [group][stage][lse2, -D, key end, key end again (WIN: first key) of 32 rows]
+    __shared__ __attribute__((aligned(256))) float srow[2][2][128];
     const int nkt = (a.L + 127) / 128;
     const int wid = blockIdx.x;
     // Key tiles from the first keys (seen by the most rows: the heaviest)
@@ -332,8 +364,35 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     // (one L2 read serves them); the launch is rounded up to whole blocks
     // and work-groups past the last key tile exit at once.
     const int ngrp = a.B * a.Hkv;
-    int kt, grpi, split = 0, nsplit = 1;
-    if (a.split_tiles) {
+    int kt, grpi, split = 0, nsplit = 1, slot = 0;
+    if constexpr (WIN) {
+        const int nsink = a.sink_tiles * a.sink_parts * ngrp, w = wid - (nsink + NUM_XCD - 1) / NUM_XCD * NUM_XCD;
+        if (w < 0) {
+            slot = wid / ngrp;
+            grpi = wid - slot * ngrp;
+            kt = slot / a.sink_parts;
+            split = slot - kt * a.sink_parts;
+            nsplit = a.sink_parts;
+            if (kt >= a.sink_tiles) return;
+        } else {
+            int it;   // the other tiles' parts, in the order of the unsplit launch below
+            if (ngrp % NUM_XCD == 0) {
+                const int gpx = ngrp / NUM_XCD, x = w % NUM_XCD, l = w / NUM_XCD;
+                const int kb = l / (gpx * KB_DKDV), r = l - kb * gpx * KB_DKDV;
+                it = kb * KB_DKDV + r % KB_DKDV;
+                grpi = x + NUM_XCD * (r / KB_DKDV);
+            } else {
+                it = w / ngrp;
+                grpi = w - it * ngrp;
+            }
+            nsplit = a.tile_parts;
+            kt = it / nsplit;
+            split = it - kt * nsplit;
+            kt += a.sink_tiles;
+            slot = a.sink_tiles * a.sink_parts + it;
+            if (kt >= nkt) return;
+        }
+    } else if (a.split_tiles) {
         // items in tile order, the groups as the fast digit (with a multiple
         // of 8 groups each stays on one XCD)
         const int it = wid / ngrp;
@@ -346,6 +405,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
         kt = lo;
         split = it - a.tile_start[kt];
         nsplit = a.tile_start[kt + 1] - a.tile_start[kt];
+        slot = it;
     } else if (ngrp % NUM_XCD == 0) {
         const int gpx = ngrp / NUM_XCD, x = wid % NUM_XCD, l = wid / NUM_XCD;
         const int kb = l / (gpx * KB_DKDV), r = l - kb * gpx * KB_DKDV;
@@ -379,7 +439,16 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
         }
     }
     // first row that sees any of these keys (key ends do not decrease)
-    const int32_t *kend_b = a.kend + (int64_t)b * a.L;
+    const int32_t *kend_b = a.kend + (WIN ? 2 : 1) * (int64_t)b * a.L;
+    // window: first row past r0 whose window starts behind key k (L: none)
+    auto window_end = [&](int r0, int k) -> int {
+        int lo = r0, hi = a.L;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (ld_uniform(kend_b, (int64_t)a.L + mid) > k) hi = mid; else lo = mid + 1;
+        }
+        return lo;
+    };
     int lo = 0, hi = a.L - 1;
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
@@ -394,7 +463,8 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     // none of these keys, so the masking zeroes their terms.
     // A split takes a contiguous share [first, total) of the chunks; group grp
     // takes chunks first + grp, first + grp + 2, ...
-    const int nch = (a.L - i0 + 31) / 32;
+    const int last = WIN && kw0 >= a.sinks ? window_end(i0, min(kw0 + 127, a.L - 1)) : a.L;   // end of those rows
+    const int nch = (last - i0 + 31) / 32;
     const int first = (int)((int64_t)a.G * nch * split / nsplit);
     const int total = (int)((int64_t)a.G * nch * (split + 1) / nsplit);
     const int nstep = (total - first + 1) / 2;
@@ -411,6 +481,12 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
         }
         im = mlo;
     }
+    // ... and, with a window, before row il
+    int il = a.L;
+    if constexpr (WIN) {
+        const int k0 = max(kw0 + 32 * sub, a.sinks);
+        if (k0 < kw0 + 32 * sub + 32) il = window_end(i0, k0);
+    }
     // Q and dO rows of one chunk go straight to LDS: wave-wide load i of wave
     // `sub` fills rows 4 RPW i + RPW sub .. + RPW - 1 of the tile, from a
     // wave-uniform base and a per-lane 32-bit offset (the swizzle repeats
@@ -422,7 +498,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     const uint32_t lch = (uint32_t)(16 * ((lane % LPR) ^ swz<D>(lrow)));
     const uint32_t qofs = (uint32_t)(lrow * (uint32_t)qst) + lch, dofs = (uint32_t)(lrow * (uint32_t)dst) + lch;
     // lanes 0..31 fetch lse2 and lanes 32..63 -D of the chunk's rows
-    const uint32_t rofs = 4u * (uint32_t)(l32 + hf * a.L), eofs = 4u * (uint32_t)l32;
+    const uint32_t rofs = 4u * (uint32_t)(l32 + hf * a.L), eofs = WIN ? rofs : 4u * (uint32_t)l32;
     const bool wide = a.wide_strides != 0;   // 32-bit row offsets do not reach
     // Next chunk to load (chunk ni of the tile): its
     // first row (may be negative: rows before 0 are no rows), its query head
@@ -430,7 +506,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     // (lse2 of a head, then -D).  Advanced by additions only.
     const int64_t qsh = 2 * a.q_sh, dsh = 2 * a.do_sh, rsh = 8 * (int64_t)a.L;
     const int64_t qwrap = a.G * qsh + 32 * qst, dwrap = a.G * dsh + 32 * dst, rwrap = a.G * rsh + 128;
-    int ni = first + grp, nh = ni % a.G, nr0 = a.L - 32 * (ni / a.G + 1);
+    int ni = first + grp, nh = ni % a.G, nr0 = last - 32 * (ni / a.G + 1);
     const char *nq = (const char *)(a.q + b * a.q_sb) + (kvh * a.G + nh) * qsh + nr0 * qst;
     const char *nd = (const char *)(a.dout + b * a.do_sb) + (kvh * a.G + nh) * dsh + nr0 * dst;
     const char *nr = (const char *)a.dl + ((int64_t)b * a.Hq + kvh * a.G + nh) * rsh + 4 * (int64_t)nr0;
@@ -467,7 +543,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
             dma_rows<D, 4, 32>(nd - nr0 * dst, dst, nr0, a.L - 1, base + TILEC, sub, ln);
             const int64_t r = max(nr0 + (ln & 31), 0);
             if (sub == 0) dma4(nr + 4 * (r - nr0 + (ln >> 5) * (int64_t)a.L), rl);
-            if (sub == 1) dma4(kend_b + r, rl + 256);
+            if (sub == 1) dma4(kend_b + r + (WIN ? (ln >> 5) * (int64_t)a.L : 0), rl + 256);
         } else if (i < NI) {
             dma16s(nq + i * (4 * RPW) * qst, qofs, base + i * 4096 + sub * 1024);
         } else if (i < 2 * NI) {
@@ -538,7 +614,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
             if (i >= 1 && i <= NPART) issue_part(i - 1, st ^ 1);
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (r0 < im) {
+        if (r0 < im || (WIN && r0 + 32 > il)) {
             // (a real branch: the compiler would otherwise turn this rare
             // path into selects executed on every chunk)
             int ln = lane;
@@ -548,9 +624,13 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
             for (int gq = 0; gq < 4; ++gq) {
                 const int r = 8 * gq + 4 * (ln >> 5);
                 const i32x4 ke = *(const i32x4 *)&srow[grp][st][64 + r];
+                i32x4 kl = ke;
+                if constexpr (WIN) kl = *(const i32x4 *)&srow[grp][st][96 + r];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    S[4 * gq + e] = ((r0 + r + e >= 0) & (ky < ke[e])) ? S[4 * gq + e] : 0.f;
+                for (int e = 0; e < 4; ++e) {
+                    const bool in = !WIN || (ky >= kl[e]) | (ky < a.sinks);
+                    S[4 * gq + e] = ((r0 + r + e >= 0) & (ky < ke[e]) & in) ? S[4 * gq + e] : 0.f;
+                }
             }
         }
         // P (rows 8 (v / 4) + 4 hf + v % 4 of the lane's key) as B fragments
@@ -612,7 +692,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     wg_barrier();
     if (grp == 0 && nsplit > 1) {
         // this split's sums, unscaled, in register order (1 KB per store)
-        float *pp = a.part + (((int64_t)(a.tile_start[kt] + split) * ngrp + grpi) * 2 * 128 + 32 * sub) * D + 4 * lane;
+        float *pp = a.part + (((int64_t)slot * ngrp + grpi) * 2 * 128 + 32 * sub) * D + 4 * lane;
 #pragma unroll
         for (int md = 0; md < MD; ++md)
 #pragma unroll
@@ -630,8 +710,8 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
         return;
     }
     if (grp == 0 && key < a.L) {
-        float *kp = a.dk + b * a.dk_sb + (int64_t)key * a.dk_st + kvh * a.dk_sh;
-        float *vp = a.dv + b * a.dv_sb + (int64_t)key * a.dv_st + kvh * a.dv_sh;
+        const int64_t kofs = b * a.dk_sb + (int64_t)key * a.dk_st + kvh * a.dk_sh;
+        const int64_t vofs = b * a.dv_sb + (int64_t)key * a.dv_st + kvh * a.dv_sh;
 #pragma unroll
         for (int md = 0; md < MD; ++md)
 #pragma unroll
@@ -643,8 +723,8 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
                     kv[e] = (dk[md][v] + part[pbase + (md * 16 + v) * 64]) * a.scale;
                     vv[e] = dv[md][v] + part[4 * MD * 16 * 64 + pbase + (md * 16 + v) * 64];
                 }
-                *(f32x4 *)(kp + 32 * md + 8 * gq + 4 * hf) = kv;
-                *(f32x4 *)(vp + 32 * md + 8 * gq + 4 * hf) = vv;
+                store_grad<BF16>(a.dk, kofs + 32 * md + 8 * gq + 4 * hf, kv);
+                store_grad<BF16>(a.dv, vofs + 32 * md + 8 * gq + 4 * hf, vv);
             }
     }
 }
@@ -685,21 +765,79 @@ __global__ __launch_bounds__(256) void bwd_sum_kernel(const BwdArgs a) {
     *(f32x4 *)(op + d0) = sum;
 }
 
+// The same for the parts of a windowed launch.  The part counts differ between
+// the two kinds of tile, so the parts are added in fours.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void bwd_sum_window_kernel(const BwdArgs a) {
+    constexpr int PER = 128 * D / 4 / 256;   // blocks per (tile, group, dK or dV)
+    const int ngrp = a.B * a.Hkv;
+    const int blk = blockIdx.x % PER, wh = blockIdx.x / PER % 2, tg = blockIdx.x / (2 * PER);
+    int kt = tg / ngrp;
+    const int grpi = tg - kt * ngrp;
+    if (a.sink_parts == 1) kt += a.sink_tiles;   // (their tiles are whole)
+    const bool sink = kt < a.sink_tiles;
+    const int ns = sink ? a.sink_parts : a.tile_parts;
+    const int s0 = sink ? kt * ns : a.sink_tiles * a.sink_parts + (kt - a.sink_tiles) * ns;
+    const int u = blk * 256 + threadIdx.x;   // ((sub * MD + md) * 4 + gq) * 64 + lane
+    const int64_t stride = (int64_t)ngrp * 2 * 128 * D;
+    const float *pp = a.part + (((int64_t)s0 * ngrp + grpi) * 2 + wh) * 128 * D + 4 * u;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < ns; s += 4) {
+        f32x4 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = *(const f32x4 *)(pp + min(s + i, ns - 1) * stride);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (s + i < ns)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] += x[i][e];
+    }
+    const int lane = u & 63, gq = (u >> 6) & 3, md = (u >> 8) % (D / 32), sub = (u >> 8) / (D / 32);
+    const int key = kt * 128 + 32 * sub + (lane & 31);
+    if (key >= a.L) return;
+    const int b = grpi / a.Hkv, kvh = grpi - b * a.Hkv;
+    const int d0 = 32 * md + 8 * gq + 4 * (lane >> 5);
+    if (!wh)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] *= a.scale;
+    if (wh) store_grad<BF16>(a.dv, b * a.dv_sb + (int64_t)key * a.dv_st + kvh * a.dv_sh + d0, sum);
+    else store_grad<BF16>(a.dk, b * a.dk_sb + (int64_t)key * a.dk_st + kvh * a.dk_sh + d0, sum);
+}
+
+template <int D, bool BF16>
+int launch_bwd_window_t(const BwdArgs &a, hipStream_t st) {
+    const int64_t nqt = (a.L + 127) / 128, ngrp = (int64_t)a.B * a.Hkv;
+    hipLaunchKernelGGL((bwd_dq_kernel<D, true, BF16>), dim3((unsigned)(a.B * a.Hq * nqt)), dim3(256), 0, st, a);
+    if (int e = (int)hipGetLastError()) return e;
+    const int64_t sinks = (a.sink_tiles * a.sink_parts * ngrp + NUM_XCD - 1) / NUM_XCD * NUM_XCD;
+    const int64_t rest = (nqt - a.sink_tiles) * a.tile_parts;
+    const int64_t grid = sinks + (ngrp % NUM_XCD == 0 ? ngrp * ((rest + KB_DKDV - 1) / KB_DKDV) * KB_DKDV : ngrp * rest);
+    hipLaunchKernelGGL((bwd_dkdv_kernel<D, true, BF16>), dim3((unsigned)grid), dim3(512), 0, st, a);
+    if (int e = (int)hipGetLastError()) return e;
+    const int64_t summed = (a.sink_parts > 1 ? a.sink_tiles : 0) + (a.tile_parts > 1 ? nqt - a.sink_tiles : 0);
+    if (summed) {
+        constexpr int64_t PER = 128 * D / 4 / 256;
+        hipLaunchKernelGGL((bwd_sum_window_kernel<D, BF16>), dim3((unsigned)(summed * ngrp * 2 * PER)), dim3(256), 0, st, a);
+    }
+    return (int)hipGetLastError();
+}
+
 template <int D>
 int launch_bwd_t(const BwdArgs &a, hipStream_t st) {
+    if (a.has_window) return a.grads_bf16 ? launch_bwd_window_t<D, true>(a, st) : launch_bwd_window_t<D, false>(a, st);
     const int64_t nqt = (a.L + 127) / 128;
-    hipLaunchKernelGGL(bwd_dq_kernel<D>, dim3((unsigned)(a.B * a.Hq * nqt)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((bwd_dq_kernel<D, false, false>), dim3((unsigned)(a.B * a.Hq * nqt)), dim3(256), 0, st, a);
     if (int e = (int)hipGetLastError()) return e;
     const int64_t ngrp = (int64_t)a.B * a.Hkv;
     if (a.split_tiles) {
-        hipLaunchKernelGGL(bwd_dkdv_kernel<D>, dim3((unsigned)(ngrp * a.tile_start[nqt])), dim3(512), 0, st, a);
+        hipLaunchKernelGGL((bwd_dkdv_kernel<D, false, false>), dim3((unsigned)(ngrp * a.tile_start[nqt])), dim3(512), 0, st, a);
         if (int e = (int)hipGetLastError()) return e;
         constexpr int64_t PER = 128 * D / 4 / 256;
         hipLaunchKernelGGL(bwd_sum_kernel<D>, dim3((unsigned)(a.split_tiles * ngrp * 2 * PER)), dim3(256), 0, st, a);
         return (int)hipGetLastError();
     }
     const int64_t grid = ngrp % NUM_XCD == 0 ? ngrp * ((nqt + KB_DKDV - 1) / KB_DKDV) * KB_DKDV : ngrp * nqt;
-    hipLaunchKernelGGL(bwd_dkdv_kernel<D>, dim3((unsigned)grid), dim3(512), 0, st, a);
+    hipLaunchKernelGGL((bwd_dkdv_kernel<D, false, false>), dim3((unsigned)grid), dim3(512), 0, st, a);
     return (int)hipGetLastError();
 }
 

@@ -123,6 +123,41 @@ __device__ __forceinline__ int lane_key_end(const BlockWindow &win, int first, i
     }
 }
 
+// The position a sliding window of token i is counted from: i in a
+// token-causal segment, else the start of i's block.  i wave-uniform and not
+// before the window of blocks.  Non-decreasing in i.
+__device__ __forceinline__ int token_anchor(const BlockWindow &win, int i, int lane) {
+    BlockWindow w = win;
+    int n = window_block(w, i);
+    if (n - w.base >= 64) {   // (more than 64 blocks in a tile)
+        w = block_window(w.off, w.text, w.nb, i, lane);
+        n = window_block(w, i);
+    }
+    return w.text && i >= block_ts(w, n) ? i : ld_uniform(w.off, n);
+}
+// The same for each lane's token: first .. first + 31, clamped by the caller
+// (first wave-uniform, the lanes' tokens not decreasing from it).
+__device__ __forceinline__ int lane_anchor(const BlockWindow &win, int first, int token, int lane) {
+    BlockWindow w = win;
+    int n = window_block(w, first);
+    if (n - w.base >= 64) {
+        w = block_window(w.off, w.text, w.nb, first, lane);
+        n = window_block(w, first);
+    }
+    if (n - w.base > 32) w = window_at(w, n, lane);   // (up to 32 blocks follow)
+    int anchor = 0, start = ld_uniform(w.off, n);
+    bool done = false;
+    for (;; ++n) {
+        const int e = block_end(w, n);
+        if (!done && token < e) {
+            anchor = w.text && token >= block_ts(w, n) ? token : start;
+            done = true;
+        }
+        if (!__builtin_amdgcn_ballot_w64(!done) || n + 1 >= w.nb) return anchor;
+        start = e;
+    }
+}
+
 // Two floats rounded to bf16 (RNE), lo in the low half: one v_cvt_pk_bf16_f32.
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));

@@ -115,6 +115,11 @@ struct AttnArgs {
     int32_t text_arg[32];   // step: segment starts by value (new_len: none)
     int32_t nl_arg[32];     // step: new-block lengths by value
     FastDiv fd_nrb;         // divider by nrb (the merge)
+    // sliding window (has_window): row i sees the keys j < its key end with
+    // j < sinks or j >= anchor - window; the anchor is i for a row of a
+    // token-causal segment and the start of its block for any other (a step:
+    // positions n_pool + t)
+    int32_t has_window, sinks, window;
 };
 
 constexpr int LENS_IN_ARGS = 32;
@@ -199,6 +204,15 @@ struct BwdArgs {
     float *part;
     int32_t split_tiles;
     uint16_t tile_start[BWD_MAX_SPLIT_TILES + 1];
+    // sliding window (has_window; AttnArgs): kend then holds, per stream, the
+    // key ends of the tokens and the first keys of their windows, [B][2][L].
+    // The first sink_tiles key tiles are seen by every later row and taken in
+    // sink_parts parts each, the others in tile_parts; parts of a tile that has
+    // more than one write partial sums at slot (kt * sink_parts or
+    // sink_tiles * sink_parts + (kt - sink_tiles) * tile_parts) + part.
+    int32_t has_window, sinks, window;
+    int32_t sink_tiles, sink_parts, tile_parts;
+    int32_t grads_bf16;   // dq, dk, dv are bf16 (windowed only)
 };
 
 // Launch shapes compiled into the library.

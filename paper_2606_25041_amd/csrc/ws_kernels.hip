@@ -97,10 +97,21 @@ using Plan = std::conditional_t<RAGGED, RaggedPlan, NoPlan>;
 // LDS at the end.  Twice the work items, each half as long, for the same
 // matrix work, at twice the tile loads per query row: for sequences whose
 // 256-row items leave compute units idle.
-template <int D, int NW, int NB, int KIND, bool F32, int KG>
+//
+// WIN: a sliding window with sinks.  Row i sees the keys j < kend(i) with
+// j < sinks or j >= klo(i), klo(i) = anchor - window never decreasing along the
+// rows, so a query tile's keys are the sink tiles [0, nst) and the tiles
+// [first, ntile), first that of its first row's klo; everything between is
+// never loaded.  The loop counts these live tiles u = 0, 1, ...; the tile of u
+// is u, or u + gap past the sinks.  f32 outputs take P as the sum of two bf16
+// values (hi + lo, two MFMAs per V fragment), so that they hold f32 accuracy
+// (2^-17 of a weight) rather than bf16's.
+template <int D, int NW, int NB, int KIND, bool F32, int KG, bool WIN = false>
 __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const Plan<KIND == STEP_RAGGED> rp) {
     constexpr bool step = KIND == STEP || KIND == STEP_SPLIT || KIND == STEP_RAGGED;
     constexpr bool RAGGED = KIND == STEP_RAGGED;
+    static_assert(!WIN || (!RAGGED && KIND != STEP_SPLIT), "windows: one split count, one step instance");
+    constexpr bool P2 = WIN && F32;        // P as hi + lo
     constexpr int NT = NW * 64;
     constexpr int QT = NW * 32 * NB / KG;  // query rows per work-group
     static_assert(KG == 1 || (KG == 2 && !step), "key groups: prefill only");
@@ -281,7 +292,31 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         k_hi = token_key_end(win, q_last, lane);
         kfull = token_key_end(win, q0, lane);
     }
-    const int ntile = (k_hi + KT - 1) / KT;
+    // window: the first and last row's klo, at least 0 (first <= own key < k_hi),
+    // the live tiles and their mapping
+    int lo_min = 0, lo_max = 0, nst = 0, gap = 0;
+    if constexpr (WIN) {
+        if (step) {
+            const int t0 = (int)fastdiv((uint32_t)q0, fd_gq);
+            const int t1 = (int)fastdiv((uint32_t)(min(q0 + QT, (int)nrows) - 1), fd_gq);
+            lo_min = n_pool + (t0 >= ts ? t0 : 0);
+            lo_max = n_pool + (t1 >= ts ? t1 : 0);
+        } else {
+            lo_min = token_anchor(win, q0, lane);
+            lo_max = token_anchor(win, min(q0 + QT, a.Lq) - 1, lane);
+        }
+        lo_min = max(lo_min - a.window, 0);
+        lo_max = max(lo_max - a.window, 0);
+        const int first = lo_min / KT;
+        nst = min((int)(((uint32_t)a.sinks + KT - 1) / KT), first);
+        gap = first - nst;
+    }
+    auto tile_of = [&](int u) -> int { return WIN && u >= nst ? u + gap : u; };
+    // whether a step's tile holds keys between the sinks and the window: no row
+    // sees them, so their slots may hold anything (a prefill's keys are all
+    // seen by their own row)
+    auto holed = [&](int kt) -> bool { return WIN && step && kt < lo_min && kt + KT > a.sinks; };
+    const int ntile = (k_hi + KT - 1) / KT - gap;
     // (split * ntile < 2^31: ntile < 2^25 and split < MAX_SPLITS = 32)
     const int t_begin = (int)fastdiv(split * (uint32_t)ntile, fd_split);
     const int t_end = (int)fastdiv((split + 1) * (uint32_t)ntile, fd_split);
@@ -292,12 +327,18 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     // with the tile loads), so no page-table read sits in front of them.
     const int32_t *ptab = a.page_table + (int64_t)b * a.max_pages;
     const int tp_end = min(t_end, (n_pool + KT - 1) / KT);   // tiles with cache rows
-    auto page_glb = [&](int t) -> int { return KIND != PREFILL_CONTIGUOUS && t < tp_end ? ld_uniform(ptab, t) : 0; };
+    auto page_glb = [&](int t) -> int {
+        if constexpr (WIN) {
+            const int u = tile_of(t);
+            return KIND != PREFILL_CONTIGUOUS && t < t_end && u < (n_pool + KT - 1) / KT ? ld_uniform(ptab, u) : 0;
+        }
+        return KIND != PREFILL_CONTIGUOUS && t < tp_end ? ld_uniform(ptab, t) : 0;
+    };
 
     // ---- this lane's query rows -------------------------------------------
     // row n of the lane: q0 + rblk * 32 * NB + 32 * n + l32 (the fragments
     // are staged through LDS in the pipeline prologue, below)
-    int row[NB], kend[NB], tok[NB], hqr[NB];
+    int row[NB], kend[NB], klo[NB], tok[NB], hqr[NB];
     bf16x8 qf[NB][KK];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
@@ -307,6 +348,10 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         hqr[n] = row_head(pc, tok[n]);
         if constexpr (step) kend[n] = n_pool + min(nl, max(ts, tok[n] + 1));
         else kend[n] = lane_key_end(win, min(q0 + rblk * 32 * NB + 32 * n, (int)nrows - 1), tok[n], lane);
+        klo[n] = 0;
+        if constexpr (WIN && step) klo[n] = n_pool + (tok[n] >= ts ? tok[n] : 0) - a.window;
+        else if constexpr (WIN)
+            klo[n] = lane_anchor(win, min(q0 + rblk * 32 * NB + 32 * n, (int)nrows - 1), tok[n], lane) - a.window;
     }
 
     // ---- direct-to-LDS tile loads -----------------------------------------
@@ -345,12 +390,14 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         bool straddle;
     };
     auto plan_tile = [&](int u, int s, int page) -> TileLoad {
-        const int kt = u * KT;
+        const int kt = tile_of(u) * KT;
         TileLoad t;
         t.kd = lds_addr(smem) + s * TILEB + lwave * 1024;
         t.vd = t.kd + VRING;
         t.straddle = false;
-        if (KIND != PREFILL_CONTIGUOUS && kt + KT <= n_pool) {
+        if (holed(kt)) {
+            t.straddle = true;
+        } else if (KIND != PREFILL_CONTIGUOUS && kt + KT <= n_pool) {
             // whole tile in one cache page
             const int64_t tb = ((int64_t)page * a.Hkv + kvh) * TILEB;
             t.bk = kpool_b + tb;
@@ -377,7 +424,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     };
     // rows past the end repeat the last key (their scores are masked)
     auto issue_straddle = [&](int u, int s, int page) {
-        const int kt = u * KT;
+        const int kt = tile_of(u) * KT;
         const uint32_t kd = lds_addr(smem) + s * TILEB + lwave * 1024;
         const uint32_t vd = kd + VRING;
         const int64_t tb = ((int64_t)page * a.Hkv + kvh) * TILEB;
@@ -387,7 +434,10 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         const uint32_t lofs_c = lofs_p - lrow0 * ROWB;   // the chunk's byte offset in a row
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const int r = min(lrow0 + i * NWD * RPW, k_hi - 1 - kt);   // row within the tile
+            int r = min(lrow0 + i * NWD * RPW, k_hi - 1 - kt);   // row within the tile
+            // (window: nor is a key between the sinks and lo_min; in a tile
+            // before the window's first the last sink stands in for it)
+            if (WIN && step && kt + r >= a.sinks && kt + r < lo_min) r = (kt + KT <= lo_min ? a.sinks - 1 : lo_min) - kt;
             const char *gk, *gv;
             if (KIND == PREFILL_PAGED || (step && kt + r < n_pool)) {
                 gk = kg + (uint32_t)(r * ROWB) + lofs_c;
@@ -489,7 +539,8 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     // fp32 lane sums ls (so lse is exact to fp32 rounding).  One straight block:
     // all exponents, then all exps, then the packs and a pairwise sum, so
     // the dependent steps of different scores overlap.
-    auto softmax_weights = [&](const Tile &sc, bf16x8 (&pf)[NB][4], const float (&m_use)[NB], float (&ls)[NB]) {
+    constexpr int PF = P2 ? 8 : 4;    // fragments of P per 64 keys (4..7: the low parts)
+    auto softmax_weights = [&](const Tile &sc, bf16x8 (&pf)[NB][PF], const float (&m_use)[NB], float (&ls)[NB]) {
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             float x[32];
@@ -498,7 +549,10 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
 #pragma unroll
             for (int f = 0; f < 32; ++f) x[f] = fast_exp2(x[f]);
 #pragma unroll
-            for (int f = 0; f < 32; ++f) pf[n][f >> 3][f & 7] = (__bf16)x[f];
+            for (int f = 0; f < 32; ++f) {
+                pf[n][f >> 3][f & 7] = (__bf16)x[f];
+                if constexpr (P2) pf[n][4 + (f >> 3)][f & 7] = (__bf16)(x[f] - (float)(__bf16)x[f]);
+            }
             // pairwise sum in a fixed order (the same for every tile)
 #pragma unroll
             for (int w = 1; w < 32; w *= 2)
@@ -519,7 +573,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     };
     // element masks only where the tile is not visible to every row
     auto mask = [&](int t, Tile &sc) {
-        const int kt = t * KT;
+        const int kt = tile_of(t) * KT;
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -527,7 +581,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int key = kt + mb * 32 + (v >> 2) * 8 + 4 * hf + (v & 3);
-                    if (key >= kend[n]) sc[n][mb][v] = -INFINITY;
+                    if (key >= kend[n] || (WIN && key < klo[n] && key >= a.sinks)) sc[n][mb][v] = -INFINITY;
                 }
     };
     // Running max (log2 domain) from a tile's in-lane max, with lazy rescale:
@@ -582,8 +636,9 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         }
     };
     // softmax of a tile: mask, running max, P weights and their sum
-    auto softmax = [&](int t, Tile &sc, bf16x8 (&pf)[NB][4]) {
-        if ((t + 1) * KT > kfull) {
+    auto softmax = [&](int t, Tile &sc, bf16x8 (&pf)[NB][PF]) {
+        const int kt = tile_of(t) * KT;
+        if (kt + KT > kfull || (WIN && kt < lo_max && kt + KT > a.sinks)) {
             // (a real branch: the compiler would otherwise turn this rare
             // path into selects executed on every tile)
             asm volatile("" ::: "memory");
@@ -613,7 +668,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     };
     // O^T[d][query] += V^T P^T from the V tile of a stage; V reads RAHEAD
     // steps ahead of their MFMAs
-    auto pv = [&](uint32_t soff, const bf16x8 (&pf)[NB][4]) {
+    auto pv = [&](uint32_t soff, const bf16x8 (&pf)[NB][PF]) {
         const uint32_t v0 = vbase[0] + soff, v1 = vbase[1] + soff;
         bf16x8 vf[RAHEAD + 1];
 #pragma unroll
@@ -622,8 +677,11 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         for (int i = 0; i < NPV; ++i) {
             if (i + RAHEAD < NPV) vf[(i + RAHEAD) % (RAHEAD + 1)] = vread(v0, v1, i + RAHEAD);
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
+            for (int n = 0; n < NB; ++n) {
                 o[n][i % MD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % (RAHEAD + 1)], pf[n][i / MD], o[n][i % MD], 0, 0, 0);
+                if constexpr (P2)
+                    o[n][i % MD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % (RAHEAD + 1)], pf[n][4 + i / MD], o[n][i % MD], 0, 0, 0);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -645,7 +703,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     // only takes part in the loads and barriers
     const bool busy = q0 + rblk * 32 < (int)nrows;
     Tile S;
-    bf16x8 pf[NB][4];
+    bf16x8 pf[NB][PF];
     const int n_tiles = t_end - t_begin;
     auto stage_off = [&](int t) -> uint32_t { return (uint32_t)((t - t_begin) % NSTAGE) * TILEB; };
     if constexpr (KG == 2) {
@@ -1133,23 +1191,28 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {
     }
 }
 
-template <int D, int KIND, int KG>
+template <int D, int KIND, int KG, bool WIN = false>
 int launch_attn_t(const AttnArgs &a, const Plan<KIND == STEP_RAGGED> &rp, hipStream_t st) {
     const dim3 grid(a.per_xcd * NUM_XCD), block(8 * 64);
     if (a.out_f32)
-        hipLaunchKernelGGL((attn_kernel<D, 8, 1, KIND, true, KG>), grid, block, 0, st, a, rp);
+        hipLaunchKernelGGL((attn_kernel<D, 8, 1, KIND, true, KG, WIN>), grid, block, 0, st, a, rp);
     else
-        hipLaunchKernelGGL((attn_kernel<D, 8, 1, KIND, false, KG>), grid, block, 0, st, a, rp);
+        hipLaunchKernelGGL((attn_kernel<D, 8, 1, KIND, false, KG, WIN>), grid, block, 0, st, a, rp);
     return (int)hipGetLastError();
 }
 
-template <int D, int KIND>
+template <int D, int KIND, bool WIN = false>
 int launch_prefill_t(const AttnArgs &a, int key_groups, hipStream_t st) {
-    return key_groups == 2 ? launch_attn_t<D, KIND, 2>(a, NoPlan{}, st) : launch_attn_t<D, KIND, 1>(a, NoPlan{}, st);
+    return key_groups == 2 ? launch_attn_t<D, KIND, 2, WIN>(a, NoPlan{}, st)
+                           : launch_attn_t<D, KIND, 1, WIN>(a, NoPlan{}, st);
 }
 
 template <int D>
 int launch_attn_d(const AttnArgs &a, const RaggedPlan *rag, TileShape shape, hipStream_t st) {
+    if (a.has_window)
+        return a.mode == MODE_STEP ? launch_attn_t<D, STEP, 1, true>(a, NoPlan{}, st)
+             : a.paged ? launch_prefill_t<D, PREFILL_PAGED, true>(a, shape.kg, st)
+                       : launch_prefill_t<D, PREFILL_CONTIGUOUS, true>(a, shape.kg, st);
     return rag ? launch_attn_t<D, STEP_RAGGED, 1>(a, *rag, st)
          : a.mode == MODE_STEP ? shape.parts_only ? launch_attn_t<D, STEP_SPLIT, 1>(a, NoPlan{}, st)
                                                   : launch_attn_t<D, STEP, 1>(a, NoPlan{}, st)
