@@ -493,6 +493,84 @@ size_t ws_prefill_window_bwd_workspace_bytes(int32_t batch, int32_t num_q_heads,
                                              int32_t seq_len, int32_t sinks, int32_t window);
 
 /*
+ * A paged KV cache held in 4 bits: the history of a long session at 1 / 3.76 of
+ * the bf16 cache's memory and read traffic.  32 neighbouring head dims of a
+ * token and KV head share a scale 2^e (the OCP microscaling format MXFP4: e2m1
+ * elements, one e8m0 scale byte e + 127 per 32): with amax = max |x|, e is the
+ * least integer with amax <= 6 * 2^e, held in [-100, 125]; an element is
+ * x * 2^-e rounded to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (ties to the
+ * even code, at most 6) with its sign.  So a value comes back off by at most
+ * max(2^(e-2), |x| / 5), which is at most 1 / 5 of its block's amax (|x| up to
+ * 6 * 2^125), and is a bf16.  A block of 32 that holds a NaN or an infinity (scale byte 255)
+ * comes back as 32 NaN.
+ * pool is [num_pages][num_kv_heads][68 * head_dim] bytes, 16-byte aligned: one
+ * (page, KV head) holds the keys, then the values, each as codes [64][head_dim
+ * / 2] (two a byte, the even head dim in the low half) and scale bytes
+ * [64][head_dim / 32].  The other fields are as in ws_paged_kv.
+ */
+typedef struct {
+    void *pool;
+    const int32_t *page_table_dev;
+    const int32_t *page_table_host;
+    int32_t num_pages;
+    int32_t page_size;          /* must be WS_PAGE_SIZE */
+    int32_t max_pages_per_seq;
+    int32_t num_kv_heads;
+    int32_t head_dim;
+} ws_paged_kv4;
+
+/*
+ * ws_kv_append_4bit -- ws_kv_append(_varlen) into a 4-bit cache: the new
+ * tokens' keys and values are rounded as above.  new_lens may be NULL on host
+ * and device (every stream commits new_len tokens).  Errors as
+ * ws_kv_append_varlen.
+ */
+int ws_kv_append_4bit(const ws_paged_kv4 *kv, int32_t batch,
+                      const int32_t *cache_lens_host, const int32_t *cache_lens_dev,
+                      const int32_t *new_lens_host, const int32_t *new_lens_dev,
+                      int32_t new_len, ws_tensor4 k_new, ws_tensor4 v_new, void *stream);
+
+/*
+ * ws_kv_read_4bit -- the values that positions [starts[b], starts[b] + length)
+ * of each stream stand for (a session that moves to another cache, a check of
+ * what was committed).  starts_host / _dev: int32 [batch], same values; k, v:
+ * bf16 [batch][length][num_kv_heads][head_dim], written.  The positions must have
+ * been committed.  Errors as ws_kv_append.
+ */
+int ws_kv_read_4bit(const ws_paged_kv4 *kv, int32_t batch, const int32_t *starts_host,
+                    const int32_t *starts_dev, int32_t length, ws_tensor4 k, ws_tensor4 v, void *stream);
+
+/*
+ * ws_block_causal_attn_fwd_4bit -- a streaming step over a 4-bit cache.  Same
+ * arguments and errors as ws_block_causal_attn_fwd_varlen, but new_lens and
+ * text_starts may each be NULL on host and device (every block holds new_len
+ * tokens; no segment).  The new block's own keys and values enter as they are,
+ * in bf16; WS_FUSE_APPEND commits them rounded (as ws_kv_append_4bit would) and
+ * leaves the result as it is.  f32 outputs hold f32 accuracy over the rounded
+ * history.  workspace: at least ws_step_workspace_bytes_4bit(...) bytes for the
+ * same arguments.
+ */
+int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new,
+                                  const ws_paged_kv4 *kv,
+                                  const int32_t *cache_lens_host, const int32_t *cache_lens_dev,
+                                  const int32_t *new_lens_host, const int32_t *new_lens_dev,
+                                  const int32_t *text_starts_host, const int32_t *text_starts_dev,
+                                  int32_t batch, int32_t new_len, int32_t num_q_heads,
+                                  float scale, int32_t flags,
+                                  ws_tensor4 out, float *lse,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * ws_step_workspace_bytes_4bit -- device workspace bytes of
+ * ws_block_causal_attn_fwd_4bit for these host arrays (int32 [batch] each;
+ * new_lens_host may be NULL), planned for the current device.  0 when none is
+ * needed, an argument is invalid or no device is available.
+ */
+size_t ws_step_workspace_bytes_4bit(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                    int32_t new_len, const int32_t *cache_lens_host,
+                                    const int32_t *new_lens_host);
+
+/*
  * Workspace bytes ws_block_causal_attn_fwd (and its _text variant) needs
  * for this shape (op =
  * WS_OP_STEP; num_kv_heads = the cache's; max_k = largest cache_lens[b] +

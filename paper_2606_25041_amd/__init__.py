@@ -19,6 +19,8 @@ lengths padded to a common one)
   block_causal_prefill_bwd(q, k, v, o, dout, lse, block_offsets, ...)
 (with window and sinks: the *_window entry points, attention to the first tokens
 and a sliding window of the latest)
+  PagedCache4: a cache held in 4 bits; kv_append and block_causal_attn_fwd take it,
+  kv_read(cache, starts, length) returns what it holds
   workspace_bytes(op, batch, num_q_heads, num_kv_heads, max_q, max_k)
   step_workspace_bytes_varlen(batch, num_q_heads, num_kv_heads, new_len, cache_lens, new_lens)
   step_plan(batch, num_q_heads, num_kv_heads, new_len, cache_lens, new_lens=None, num_cus=0)
@@ -32,7 +34,7 @@ import torch  # loads the HIP runtime that libwsattn.so then shares
 
 from . import build as _build
 
-__all__ = ["WsError", "PagedCache", "kv_append", "block_causal_attn_fwd", "block_causal_attn_fwd_noalloc",
+__all__ = ["WsError", "PagedCache", "PagedCache4", "kv_append", "kv_read", "block_causal_attn_fwd", "block_causal_attn_fwd_noalloc",
            "block_causal_prefill", "block_causal_prefill_bwd", "workspace_bytes",
            "step_workspace_bytes_varlen", "step_plan", "library",
            "abi_version", "WS_OP_STEP", "WS_OP_PREFILL", "WS_OP_PREFILL_BWD", "PAGE_SIZE"]
@@ -58,6 +60,13 @@ class Tensor4(ctypes.Structure):
     _fields_ = [("ptr", ctypes.c_void_p), ("dtype", ctypes.c_int32),
                 ("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64),
                 ("stride_h", ctypes.c_int64)]
+
+
+class PagedKV4Desc(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("page_table_dev", ctypes.c_void_p),
+                ("page_table_host", ctypes.c_void_p), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
 class PagedKVDesc(ctypes.Structure):
@@ -139,6 +148,16 @@ def library():
             Tensor4, Tensor4, Tensor4, P, ctypes.c_size_t, P]
         lib.ws_prefill_window_bwd_workspace_bytes.restype = ctypes.c_size_t
         lib.ws_prefill_window_bwd_workspace_bytes.argtypes = [I32, I32, I32, I32, I32, I32]
+        KV4 = ctypes.POINTER(PagedKV4Desc)
+        lib.ws_kv_append_4bit.restype = ctypes.c_int
+        lib.ws_kv_append_4bit.argtypes = [KV4, I32, P, P, P, P, I32, Tensor4, Tensor4, P]
+        lib.ws_kv_read_4bit.restype = ctypes.c_int
+        lib.ws_kv_read_4bit.argtypes = [KV4, I32, P, P, I32, Tensor4, Tensor4, P]
+        lib.ws_block_causal_attn_fwd_4bit.restype = ctypes.c_int
+        lib.ws_block_causal_attn_fwd_4bit.argtypes = [
+            Tensor4, Tensor4, Tensor4, KV4, P, P, P, P, P, P, I32, I32, I32, F, I32, Tensor4, P, P, ctypes.c_size_t, P]
+        lib.ws_step_workspace_bytes_4bit.restype = ctypes.c_size_t
+        lib.ws_step_workspace_bytes_4bit.argtypes = [I32, I32, I32, I32, P, P]
         if lib.ws_abi_version() != 5:
             raise RuntimeError("libwsattn.so ABI version mismatch")
         _bind_native(lib)
@@ -162,6 +181,8 @@ def _bind_native(lib):
     _NATIVE.bind_window(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
         "ws_block_causal_attn_fwd_window", "ws_step_workspace_bytes_window", "ws_block_causal_prefill_window",
         "ws_block_causal_prefill_window_bwd", "ws_prefill_window_bwd_workspace_bytes")))
+    _NATIVE.bind_cache4(PagedCache4, *(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
+        "ws_kv_append_4bit", "ws_kv_read_4bit", "ws_block_causal_attn_fwd_4bit", "ws_step_workspace_bytes_4bit")))
 
 
 def _native():
@@ -245,6 +266,35 @@ class PagedCache:
                            self.num_kv_heads, self.head_dim)
 
 
+class PagedCache4:
+    """Caller-owned paged full-history KV cache held in 4 bits (MXFP4: 32
+    neighbouring head dims of a token and head share a power-of-two scale;
+    the format is stated in include/ws_attn.h).
+
+    pool: uint8 device [num_pages][num_kv_heads][68 * head_dim], contiguous;
+    page_table: int32 [batch][max_pages_per_seq] (kept on host and device).
+    kv_append, kv_read and block_causal_attn_fwd take it.
+    """
+
+    def __init__(self, pool, page_table):
+        if pool.dim() != 3 or pool.dtype != torch.uint8 or not pool.is_contiguous() or pool.shape[2] % 68:
+            raise ValueError("pool must be contiguous uint8 [num_pages][num_kv_heads][68 * head_dim]")
+        self.pool = pool
+        self.page_table_host = page_table.to(torch.int32).cpu().contiguous()
+        self.page_table = self.page_table_host.to(pool.device)
+        self.num_pages, self.num_kv_heads = pool.shape[:2]
+        self.head_dim = pool.shape[2] // 68
+
+    @classmethod
+    def allocate(cls, num_pages, num_kv_heads, head_dim, page_table, device="cuda"):
+        """A new pool (its contents are undefined until committed)."""
+        return cls(torch.empty((num_pages, num_kv_heads, 68 * head_dim), dtype=torch.uint8, device=device), page_table)
+
+    def desc(self):
+        return PagedKV4Desc(self.pool.data_ptr(), self.page_table.data_ptr(), self.page_table_host.data_ptr(),
+                            self.num_pages, PAGE_SIZE, self.page_table_host.shape[1], self.num_kv_heads, self.head_dim)
+
+
 def _lens(cache_lens, device):
     """(host int32 tensor, device int32 tensor) from a list / tensor / pair."""
     if isinstance(cache_lens, tuple):
@@ -290,8 +340,10 @@ def step_plan(batch, num_q_heads, num_kv_heads, new_len, cache_lens, new_lens=No
 
 def kv_append(cache, cache_lens, k_new, v_new, new_lens=None):
     """Commit k_new/v_new [B][Ln][Hkv][d] at positions cache_lens[b] + t
-    (only t < new_lens[b] when new_lens, [B], is given)."""
-    rc = _native().append(cache, cache_lens, k_new, v_new, new_lens)
+    (only t < new_lens[b] when new_lens, [B], is given).  A PagedCache4 stores
+    them in 4 bits."""
+    four = isinstance(cache, PagedCache4)
+    rc = (_native().append4 if four else _native().append)(cache, cache_lens, k_new, v_new, new_lens)
     if rc is not None:
         if rc:
             _check(rc)
@@ -303,7 +355,11 @@ def kv_append(cache, cache_lens, k_new, v_new, new_lens=None):
     _check_lens(host, dev, B)
     _check_table(cache, B)
     desc = cache.desc()
-    if new_lens is None:
+    if four:
+        nh, nd = (None, None) if new_lens is None else _int32_pair(new_lens, (B,), k_new.device)
+        _check(library().ws_kv_append_4bit(ctypes.byref(desc), B, host.data_ptr(), dev.data_ptr(), _ptr(nh), _ptr(nd),
+                                           Ln, _t4(k_new), _t4(v_new), _stream()))
+    elif new_lens is None:
         _check(library().ws_kv_append(ctypes.byref(desc), B, host.data_ptr(), dev.data_ptr(),
                                       Ln, _t4(k_new), _t4(v_new), _stream()))
     else:
@@ -311,6 +367,37 @@ def kv_append(cache, cache_lens, k_new, v_new, new_lens=None):
         _check(library().ws_kv_append_varlen(ctypes.byref(desc), B, host.data_ptr(), dev.data_ptr(),
                                              nh.data_ptr(), nd.data_ptr(), Ln, _t4(k_new), _t4(v_new),
                                              _stream()))
+
+
+def kv_read(cache, starts, length, k=None, v=None):
+    """The keys and values that positions [starts[b], starts[b] + length) of a
+    4-bit cache stand for: bf16 (k, v) [B][length][Hkv][d], written into the
+    caller's tensors where given.  starts: [B] (host array-like, or a (host,
+    device) pair).  The positions must have been committed."""
+    if not isinstance(cache, PagedCache4):
+        raise ValueError("kv_read reads a PagedCache4")
+    got = _native().read4(cache, starts, length, k, v)
+    if got is not None:
+        if got[0]:
+            _check(got[0])
+        return got[1:]
+    host, dev = _lens(starts, cache.pool.device)
+    B, length = host.shape[0], operator.index(length)
+    if length < 0:
+        raise ValueError("length must not be negative")
+    shape = (B, length, cache.num_kv_heads, cache.head_dim)
+    if k is None:
+        k = torch.empty(shape, dtype=torch.bfloat16, device=cache.pool.device)
+    if v is None:
+        v = torch.empty(shape, dtype=torch.bfloat16, device=cache.pool.device)
+    _shape("k", k, shape)
+    _shape("v", v, shape)
+    _check_lens(host, dev, B)
+    _check_table(cache, B)
+    desc = cache.desc()
+    _check(library().ws_kv_read_4bit(ctypes.byref(desc), B, host.data_ptr(), dev.data_ptr(), length, _t4(k), _t4(v),
+                                     _stream()))
+    return k, v
 
 
 def _window(window, sinks):
@@ -356,11 +443,17 @@ def block_causal_attn_fwd(q, k_new, v_new, cache, cache_lens, scale=None, fuse_a
     token-causal segment: before itself).  Only the pages of cache positions
     [0, sinks) and [cache_lens[b] - window, cache_lens[b]) are then read; the
     table's other entries may hold anything.
+    A PagedCache4 is read as the bf16 values it stands for (no window), and a
+    committed block is stored in 4 bits; the step itself sees it unrounded.
     Returns out (and lse [B][Hq][Lq] f32 when want_lse)."""
     window, sinks = _window(window, sinks)
+    four = isinstance(cache, PagedCache4)
+    if four and window is not None:
+        raise ValueError("a window over a 4-bit cache is not supported")
     args = (q, k_new, v_new, cache, cache_lens, scale, fuse_append, out, out_dtype, want_lse, lse, workspace,
             text_starts, new_lens, False)
-    got = _native().step(*args) if window is None else _native().step_window(*args, window, sinks)
+    got = _native().step4(*args) if four else \
+        _native().step(*args) if window is None else _native().step_window(*args, window, sinks)
     if got is not None:
         rc, out, lse = got
         if rc:
@@ -385,6 +478,9 @@ def block_causal_attn_fwd(q, k_new, v_new, cache, cache_lens, scale=None, fuse_a
     nl = None if new_lens is None else _int32_pair(new_lens, (B,), q.device)
     if B == 0 or Lq == 0:
         need = 0
+    elif four:
+        need = library().ws_step_workspace_bytes_4bit(B, Hq, cache.num_kv_heads, Lq, host.data_ptr(),
+                                                      None if nl is None else nl[0].data_ptr())
     elif window is not None:
         need = library().ws_step_workspace_bytes_window(B, Hq, cache.num_kv_heads, Lq, host.data_ptr(),
                                                         None if nl is None else nl[0].data_ptr(), sinks, window)
@@ -398,9 +494,14 @@ def block_causal_attn_fwd(q, k_new, v_new, cache, cache_lens, scale=None, fuse_a
     ws_len = workspace.numel() if workspace is not None else 0
     desc = cache.desc()
     flags = WS_FUSE_APPEND if fuse_append else 0
-    if window is not None:
+    if four or window is not None:
         th, td = _int32_pair(text_starts, (B,), q.device) if text_starts is not None else (None, None)
         nh, nd = nl if nl is not None else (None, None)
+    if four:
+        _check(library().ws_block_causal_attn_fwd_4bit(
+            _t4(q), _t4(k_new), _t4(v_new), ctypes.byref(desc), host.data_ptr(), dev.data_ptr(), _ptr(nh), _ptr(nd),
+            _ptr(th), _ptr(td), B, Lq, Hq, float(scale), flags, _t4(out), _ptr(lse), ws_ptr, ws_len, _stream()))
+    elif window is not None:
         _check(library().ws_block_causal_attn_fwd_window(
             _t4(q), _t4(k_new), _t4(v_new), ctypes.byref(desc), host.data_ptr(), dev.data_ptr(), _ptr(nh), _ptr(nd),
             _ptr(th), _ptr(td), B, Lq, Hq, sinks, window, float(scale), flags, _t4(out), _ptr(lse), ws_ptr, ws_len,
@@ -432,6 +533,8 @@ def block_causal_attn_fwd_noalloc(q, k_new, v_new, cache, cache_lens, out, lse=N
     cache_lens is a (host, device) pair of int32 [B] tensors, out the
     [B][Lq][Hq][d] output (bf16 or f32), lse None or f32 [B][Hq][Lq].
     Calls on one device must be ordered (they share the scratch array)."""
+    if isinstance(cache, PagedCache4):
+        raise ValueError("the allocation-free step reads a PagedCache")
     if out is not None:
         got = _native().step(q, k_new, v_new, cache, cache_lens, scale, fuse_append, out, None, False, lse, None, None,
                              None, True)
@@ -470,6 +573,8 @@ def block_causal_prefill(q, k, v, block_offsets, scale=None, cache=None, num_kv_
     segment starting there; its token i then sees keys
     j < max(text_starts[b][n], i + 1).  window, sinks: as in
     ``block_causal_attn_fwd``."""
+    if isinstance(cache, PagedCache4):
+        raise ValueError("a prefill reads a PagedCache")
     window, sinks = _window(window, sinks)
     args = (q, k, v, block_offsets, scale, cache, num_kv_heads, out, out_dtype, want_lse, lse, text_starts)
     got = _native().prefill(*args) if window is None else _native().prefill_window(*args, window, sinks)

@@ -11,15 +11,15 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwsattn.so")
 # device sources (built with KERNEL_FLAGS) and the host-only C ABI
 DEVICE_SOURCES = [os.path.join(CSRC, "ws_kernels.hip"), os.path.join(CSRC, "ws_bwd.hip"),
-                  os.path.join(CSRC, "ws_device.hip")]
-HOST_SOURCES = [os.path.join(CSRC, "ws_api.cpp")]
+                  os.path.join(CSRC, "ws_cache4.hip"), os.path.join(CSRC, "ws_device.hip")]
+HOST_SOURCES = [os.path.join(CSRC, "ws_api.cpp"), os.path.join(CSRC, "ws_api4.cpp")]
 SOURCES = DEVICE_SOURCES + HOST_SOURCES + [os.path.join(CSRC, "ws_binding.cpp")]
 HEADERS = [os.path.join(CSRC, "ws_kernels.h"), os.path.join(CSRC, "ws_host.h"), os.path.join(CSRC, "ws_device_util.h"),
-           os.path.join(os.path.dirname(HERE), "include", "ws_attn.h")]
+           os.path.join(CSRC, "ws_cache4.h"), os.path.join(os.path.dirname(HERE), "include", "ws_attn.h")]
 # the device code whose hash tags measured counter summaries: the forward
 # kernels (attention, merge, append) and, separately, the gradient kernels
 KERNEL_SOURCES = [os.path.join(CSRC, "ws_kernels.hip"), os.path.join(CSRC, "ws_kernels.h"),
-                  os.path.join(CSRC, "ws_device_util.h")]
+                  os.path.join(CSRC, "ws_device_util.h"), os.path.join(CSRC, "ws_cache4.h")]
 BWD_KERNEL_SOURCES = [os.path.join(CSRC, "ws_bwd.hip"), os.path.join(CSRC, "ws_kernels.h"),
                       os.path.join(CSRC, "ws_device_util.h")]
 ARCH = "gfx950"

@@ -47,7 +47,15 @@ struct WindowAbi {
     decltype(&ws_prefill_window_bwd_workspace_bytes) bwd_bytes;
 } wabi;
 
-PyObject *cache_class;   // PagedCache
+struct Cache4Abi {
+    decltype(&ws_kv_append_4bit) append;
+    decltype(&ws_kv_read_4bit) read;
+    decltype(&ws_block_causal_attn_fwd_4bit) fwd;
+    decltype(&ws_step_workspace_bytes_4bit) step_bytes;
+} abi4;
+
+PyObject *cache_class;    // PagedCache
+PyObject *cache4_class;   // PagedCache4
 
 bool take_addresses(void **to, size_t count, PyObject *const *args, Py_ssize_t n) {
     if (n != (Py_ssize_t)count) {
@@ -64,6 +72,16 @@ bool take_addresses(void **to, size_t count, PyObject *const *args, Py_ssize_t n
 
 PyObject *bind_window(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (!take_addresses((void **)&wabi, sizeof wabi / sizeof(void *), args, n)) return nullptr;
+    Py_RETURN_NONE;
+}
+
+PyObject *bind_cache4(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n < 1 || !take_addresses((void **)&abi4, sizeof abi4 / sizeof(void *), args + 1, n - 1)) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "the cache class first");
+        return nullptr;
+    }
+    Py_INCREF(args[0]);
+    Py_XSETREF(cache4_class, args[0]);
     Py_RETURN_NONE;
 }
 
@@ -134,6 +152,7 @@ struct NoGil {
 };
 
 PyObject *names[7];   // attribute names of PagedCache, in the order below
+PyObject *pool_name;  // PagedCache4: "pool" in place of the first two
 
 // The paged cache's descriptor, with its table checked for `batch` rows.  The
 // cache's tensors are held: without the GIL another thread may replace them.
@@ -161,6 +180,32 @@ bool paged(PyObject *cache, int64_t batch, Paged &d) {
                         (int32_t)PyLong_AsLong(v[4]), WS_PAGE_SIZE, (int32_t)th->size(1), (int32_t)PyLong_AsLong(v[5]),
                         (int32_t)PyLong_AsLong(v[6])};
         d.hold[0] = *k, d.hold[1] = *vp, d.hold[2] = *th, d.hold[3] = *td;
+    }
+    for (PyObject *o : v) Py_XDECREF(o);
+    return ok;
+}
+
+// The same of a PagedCache4
+struct Paged4 : ws_paged_kv4 {
+    at::Tensor hold[3];
+};
+bool paged4(PyObject *cache, int64_t batch, Paged4 &d) {
+    if ((PyObject *)Py_TYPE(cache) != cache4_class) return false;
+    PyObject *v[6] = {};
+    bool ok = true;
+    for (int i = 0; i < 6 && ok; ++i) ok = (v[i] = PyObject_GetAttr(cache, i ? names[i + 1] : pool_name)) != nullptr;
+    if (!ok) PyErr_Clear();
+    if (ok) {
+        const at::Tensor *p = tensor(v[0]), *th = tensor(v[1]), *td = tensor(v[2]);
+        ok = p && th && td && p->is_cuda() && th->dim() == 2 && th->size(0) >= batch && td->sizes() == th->sizes() &&
+             PyLong_CheckExact(v[3]) && PyLong_CheckExact(v[4]) && PyLong_CheckExact(v[5]);
+        if (ok) {
+            static_cast<ws_paged_kv4 &>(d) =
+                ws_paged_kv4{p->data_ptr(), (const int32_t *)td->data_ptr(), (const int32_t *)th->data_ptr(),
+                             (int32_t)PyLong_AsLong(v[3]), WS_PAGE_SIZE, (int32_t)th->size(1),
+                             (int32_t)PyLong_AsLong(v[4]), (int32_t)PyLong_AsLong(v[5])};
+            d.hold[0] = *p, d.hold[1] = *th, d.hold[2] = *td;
+        }
     }
     for (PyObject *o : v) Py_XDECREF(o);
     return ok;
@@ -255,23 +300,81 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// append4(cache, lens, k_new, v_new, new_lens) -> status, or None
+PyObject *append4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 5) Py_RETURN_NONE;
+    const at::Tensor *k = tensor(a[2]);
+    if (!k || k->dim() != 4) Py_RETURN_NONE;
+    const int64_t B = k->size(0), L = k->size(1);
+    Paged4 kv{};
+    ws_tensor4 kd, vd;
+    Ints lens, nl;
+    if (!paged4(a[0], B, kv) || !token_tensor(k, {B, L, kv.num_kv_heads, kv.head_dim}, kd) ||
+        !token_tensor(tensor(a[3]), {B, L, kv.num_kv_heads, kv.head_dim}, vd) || a[1] == Py_None ||
+        !int_pair(a[1], {B}, false, lens) || !int_pair(a[4], {B}, true, nl))
+        Py_RETURN_NONE;
+    int rc;
+    {
+        NoGil free;
+        rc = abi4.append(&kv, B, lens.host, lens.dev, nl.host, nl.dev, L, kd, vd, stream());
+    }
+    return PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
+// read4(cache, starts, length, k, v) -> (status, k, v), or None
+PyObject *read4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 5 || !PyTuple_CheckExact(a[1]) || PyTuple_GET_SIZE(a[1]) != 2 || !PyLong_CheckExact(a[2])) Py_RETURN_NONE;
+    const at::Tensor *h = tensor(PyTuple_GET_ITEM(a[1], 0));
+    if (!h || h->dim() != 1) Py_RETURN_NONE;
+    int over = 0;
+    const int64_t B = h->size(0), L = PyLong_AsLongAndOverflow(a[2], &over);
+    Paged4 kv{};
+    ws_tensor4 kd, vd;
+    Ints starts;
+    if (over || L < 0 || L > INT32_MAX || !paged4(a[0], B, kv) || !int_pair(a[1], {B}, false, starts)) Py_RETURN_NONE;
+    const int64_t H = kv.num_kv_heads, D = kv.head_dim;
+    at::Tensor k, v;
+    if (!given(a[3], {B, L, H, D}, k) || (k.defined() && !token_tensor(&k, {B, L, H, D}, kd)) ||
+        !given(a[4], {B, L, H, D}, v) || (v.defined() && !token_tensor(&v, {B, L, H, D}, vd)))
+        Py_RETURN_NONE;
+    int rc;
+    {
+        NoGil free;
+        allocate(k, {B, L, H, D}, at::kBFloat16, kv.hold[0]);
+        allocate(v, {B, L, H, D}, at::kBFloat16, kv.hold[0]);
+        token_tensor(&k, {B, L, H, D}, kd);
+        token_tensor(&v, {B, L, H, D}, vd);
+        rc = abi4.read(&kv, B, starts.host, starts.dev, L, kd, vd, stream());
+    }
+    return result(rc, {k, v});
+    END_HANDLE_TH_ERRORS
+}
+
 // step(q, k_new, v_new, cache, lens, scale, fuse_append, out, out_dtype,
 //      want_lse, lse, workspace, text_starts, new_lens, noalloc)
 //   -> (status, out, lse), or None
-// (step_window: and window, sinks)
-PyObject *step_of(PyObject *const *a, const Window &win) {
+// (step_window: and window, sinks; step4: a PagedCache4)
+PyObject *step_of(PyObject *const *a, const Window &win, bool four = false) {
     const at::Tensor *q = tensor(a[0]);
     if (!q || q->dim() != 4) Py_RETURN_NONE;
     const int64_t B = q->size(0), L = q->size(1), H = q->size(2), D = q->size(3);
     if (B == 0 || L == 0) Py_RETURN_NONE;
     Paged kv{};
+    Paged4 kv4{};
     ws_tensor4 qd, kd, vd, od;
     Ints lens, text, nl;
     bool fuse, want_lse, noalloc;
     float scale;
-    if (!flag(a[6], fuse) || !flag(a[9], want_lse) || !flag(a[14], noalloc) || !paged(a[3], B, kv) || kv.head_dim != D ||
-        !token_tensor(q, {B, L, H, D}, qd) || !token_tensor(tensor(a[1]), {B, L, kv.num_kv_heads, D}, kd) ||
-        !token_tensor(tensor(a[2]), {B, L, kv.num_kv_heads, D}, vd) || a[4] == Py_None ||
+    if (!flag(a[6], fuse) || !flag(a[9], want_lse) || !flag(a[14], noalloc) ||
+        !(four ? paged4(a[3], B, kv4) : paged(a[3], B, kv)))
+        Py_RETURN_NONE;
+    const int64_t hkv = four ? kv4.num_kv_heads : kv.num_kv_heads;
+    if ((four ? kv4.head_dim : kv.head_dim) != D ||
+        !token_tensor(q, {B, L, H, D}, qd) || !token_tensor(tensor(a[1]), {B, L, hkv, D}, kd) ||
+        !token_tensor(tensor(a[2]), {B, L, hkv, D}, vd) || a[4] == Py_None ||
         !int_pair(a[4], {B}, false, lens) || !scale_of(a[5], D, scale) || !int_pair(a[12], {B}, true, text) ||
         !int_pair(a[13], {B}, true, nl))
         Py_RETURN_NONE;
@@ -300,15 +403,19 @@ PyObject *step_of(PyObject *const *a, const Window &win) {
         } else if (!noalloc) {
             int32_t most = 0;
             for (int64_t b = 0; b < B; ++b) most = std::max(most, lens.host[b * lens.h->stride(0)]);
-            wn = win.window >= 0 ? wabi.step_bytes(B, H, kv.num_kv_heads, L, lens.host, nl.host, win.sinks, win.window)
-               : nl.host ? abi.workspace_bytes_varlen(B, H, kv.num_kv_heads, L, lens.host, nl.host)
-                       : abi.workspace_bytes(WS_OP_STEP, B, H, kv.num_kv_heads, L, (int32_t)std::min<int64_t>(most + L, INT32_MAX));
+            wn = four ? abi4.step_bytes(B, H, hkv, L, lens.host, nl.host)
+               : win.window >= 0 ? wabi.step_bytes(B, H, hkv, L, lens.host, nl.host, win.sinks, win.window)
+               : nl.host ? abi.workspace_bytes_varlen(B, H, hkv, L, lens.host, nl.host)
+                         : abi.workspace_bytes(WS_OP_STEP, B, H, hkv, L, (int32_t)std::min<int64_t>(most + L, INT32_MAX));
             if (wn) {
                 own = at::empty({(int64_t)wn}, q->options().dtype(at::kByte));
                 wp = own.data_ptr();
             }
         }
-        if (win.window >= 0)
+        if (four)
+            rc = abi4.fwd(qd, kd, vd, &kv4, lens.host, lens.dev, nl.host, nl.dev, text.host, text.dev, B, L, H, scale, flags,
+                          od, lp, wp, wn, stream());
+        else if (win.window >= 0)
             rc = wabi.fwd(qd, kd, vd, &kv, lens.host, lens.dev, nl.host, nl.dev, text.host, text.dev, B, L, H, win.sinks,
                           win.window, scale, flags, od, lp, wp, wn, stream());
         else if (noalloc)
@@ -337,6 +444,13 @@ PyObject *step_window(PyObject *, PyObject *const *a, Py_ssize_t n) {
     Window win;
     if (n != 17 || !window_of(a[15], a[16], win)) Py_RETURN_NONE;
     return step_of(a, win);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *step4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 15) Py_RETURN_NONE;
+    return step_of(a, Window{}, true);
     END_HANDLE_TH_ERRORS
 }
 
@@ -493,6 +607,10 @@ PyObject *prefill_window_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)())bind, METH_FASTCALL, "the cache class, then the C ABI's addresses in Abi's order"},
     {"bind_window", (PyCFunction)(void (*)())bind_window, METH_FASTCALL, "the windowed ABI's addresses in WindowAbi's order"},
+    {"bind_cache4", (PyCFunction)(void (*)())bind_cache4, METH_FASTCALL, "PagedCache4, then the 4-bit ABI's addresses"},
+    {"append4", (PyCFunction)(void (*)())append4, METH_FASTCALL, nullptr},
+    {"read4", (PyCFunction)(void (*)())read4, METH_FASTCALL, nullptr},
+    {"step4", (PyCFunction)(void (*)())step4, METH_FASTCALL, nullptr},
     {"step_window", (PyCFunction)(void (*)())step_window, METH_FASTCALL, nullptr},
     {"prefill_window", (PyCFunction)(void (*)())prefill_window, METH_FASTCALL, nullptr},
     {"prefill_window_bwd", (PyCFunction)(void (*)())prefill_window_bwd, METH_FASTCALL, nullptr},
@@ -509,5 +627,6 @@ PyMODINIT_FUNC PyInit__wsbinding() {
     const char *n[7] = {"k_pool", "v_pool", "page_table_host", "page_table", "num_pages", "num_kv_heads", "head_dim"};
     for (int i = 0; i < 7; ++i)
         if (!(names[i] = PyUnicode_InternFromString(n[i]))) return nullptr;
+    if (!(pool_name = PyUnicode_InternFromString("pool"))) return nullptr;
     return PyModule_Create(&module);
 }

@@ -120,6 +120,9 @@ struct AttnArgs {
     // token-causal segment and the start of its block for any other (a step:
     // positions n_pool + t)
     int32_t has_window, sinks, window;
+    // step over a cache held in 4 bits: its pool (else nullptr; kpool and vpool
+    // are unused then)
+    uint8_t *pool4;
 };
 
 constexpr int LENS_IN_ARGS = 32;
@@ -161,6 +164,23 @@ struct AppendArgs {
     int32_t max_pages;
     const int32_t *cache_lens;
     const int32_t *new_lens;   // NULL: every stream commits Ln tokens
+    int32_t B, Ln, Hkv, D;
+};
+
+// 4-bit cache (ws_cache4.h): one (page, KV head) of the pool, keys then values
+constexpr int cache4_bytes(int D) { return 2 * 64 * (D / 2 + D / 32); }
+
+// Tokens written to, or read from, a 4-bit cache.  kn / vn: bf16 sources of an
+// append, or destinations of a read (start: the first position of each stream).
+struct Cache4Args {
+    uint16_t *kn, *vn;
+    int64_t kn_sb, kn_st, kn_sh;
+    int64_t vn_sb, vn_st, vn_sh;
+    uint8_t *pool;
+    const int32_t *page_table;
+    int32_t max_pages;
+    const int32_t *start;
+    const int32_t *new_lens;   // append: tokens of each stream, or NULL: Ln
     int32_t B, Ln, Hkv, D;
 };
 
@@ -231,6 +251,8 @@ struct TileShape {
 int launch_attention(const AttnArgs &a, const RaggedPlan *rag, int head_dim, TileShape shape, void *stream);
 int launch_combine(const AttnArgs &a, const RaggedPlan *rag, int head_dim, void *stream);
 int launch_append(const AppendArgs &a, void *stream);
+int launch_append4(const Cache4Args &a, void *stream);
+int launch_read4(const Cache4Args &a, void *stream);
 // dQ (with the row data), then dK/dV and the sum of its parts; 0 or a HIP error code
 int launch_prefill_bwd(const BwdArgs &a, int head_dim, void *stream);
 // Compute units of the current HIP device (queried once per device, then

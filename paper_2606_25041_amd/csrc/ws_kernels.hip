@@ -49,6 +49,7 @@
 
 #include "ws_kernels.h"
 #include "ws_device_util.h"
+#include "ws_cache4.h"
 
 namespace ws {
 namespace {
@@ -77,16 +78,34 @@ __device__ __forceinline__ void append_share(const AttnArgs &a, int b, int kvh, 
     }
 }
 
+// The same into the 4-bit cache: four threads share a block of 32 values.
+template <int D, int NT>
+__device__ __forceinline__ void append_share4(const AttnArgs &a, int b, int kvh, int ai, int napp, int n_pool, int nl,
+                                              const int32_t *ptab, int tid) {
+    constexpr int CH = D / 8;
+    const int s0 = (int)((int64_t)ai * a.Lq / napp);
+    const int n = max(min((int)((int64_t)(ai + 1) * a.Lq / napp), nl) - s0, 0) * CH;
+    for (int u = tid; u < n; u += NT) {   // (n is a multiple of 4: a block's threads stay together)
+        const int t = s0 + u / CH, c = u % CH;
+        const int pos = n_pool + t;
+        uint8_t *g = a.pool4 + ((int64_t)ptab[pos >> 6] * a.Hkv + kvh) * cache4_bytes(D);
+        store_block4<D>(g, pos & 63, c, *(const u32x4 *)(a.kc + b * a.kc_sb + (int64_t)t * a.kc_st + kvh * a.kc_sh + 8 * c));
+        store_block4<D>(g + cache4_bytes(D) / 2, pos & 63, c,
+                        *(const u32x4 *)(a.vc + b * a.vc_sb + (int64_t)t * a.vc_st + kvh * a.vc_sh + 8 * c));
+    }
+}
+
 // What a launch does, fixed at compile time: a kernel that serves one kind of
 // call carries fewer scalars through its loop (spilled: contiguous prefill 14,
 // split step 22, per-stream 45 to 49; one kernel for all had 22) and none of
 // the others' code through the instruction cache, where short launches spend
 // their time.  Prefill of 2 x 16384 tokens 3.93 -> 3.76 ms; its loop still reads
 // five spilled scalars back per tile.
-enum Kind { PREFILL_CONTIGUOUS, PREFILL_PAGED, STEP, STEP_SPLIT, STEP_RAGGED };
+enum Kind { PREFILL_CONTIGUOUS, PREFILL_PAGED, STEP, STEP_SPLIT, STEP_RAGGED, STEP_CACHE4 };
 
 // STEP_SPLIT: every item writes partials, none rows of the output.
 // STEP_RAGGED: the streams have their own split counts (rp).
+// STEP_CACHE4: the cache is held in 4 bits (ws_cache4.h).
 struct NoPlan {};
 template <bool RAGGED>
 using Plan = std::conditional_t<RAGGED, RaggedPlan, NoPlan>;
@@ -108,10 +127,11 @@ using Plan = std::conditional_t<RAGGED, RaggedPlan, NoPlan>;
 // (2^-17 of a weight) rather than bf16's.
 template <int D, int NW, int NB, int KIND, bool F32, int KG, bool WIN = false>
 __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const Plan<KIND == STEP_RAGGED> rp) {
-    constexpr bool step = KIND == STEP || KIND == STEP_SPLIT || KIND == STEP_RAGGED;
+    constexpr bool step = KIND == STEP || KIND == STEP_SPLIT || KIND == STEP_RAGGED || KIND == STEP_CACHE4;
+    constexpr bool C4 = KIND == STEP_CACHE4;
     constexpr bool RAGGED = KIND == STEP_RAGGED;
-    static_assert(!WIN || (!RAGGED && KIND != STEP_SPLIT), "windows: one split count, one step instance");
-    constexpr bool P2 = WIN && F32;        // P as hi + lo
+    static_assert(!WIN || (!RAGGED && KIND != STEP_SPLIT && !C4), "windows: one split count, one step instance");
+    constexpr bool P2 = (WIN || C4) && F32;        // P as hi + lo
     constexpr int NT = NW * 64;
     constexpr int QT = NW * 32 * NB / KG;  // query rows per work-group
     static_assert(KG == 1 || (KG == 2 && !step), "key groups: prefill only");
@@ -231,8 +251,9 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         if ((int)fastdiv((uint32_t)q0, fd_gq) >= nl0) {
             if (a.fuse_append) {
                 const int np0 = a.lens_in_args ? a.lens_arg[b] : ld_uniform(a.cache_lens, b);
-                append_share<D, NT>(a, b, kvh, (int)(qi * a.nsplit + split), a.nqt * a.nsplit, np0, nl0,
-                                    a.page_table + (int64_t)b * a.max_pages, tid);
+                const auto share = C4 ? append_share4<D, NT> : append_share<D, NT>;
+                share(a, b, kvh, (int)(qi * a.nsplit + split), a.nqt * a.nsplit, np0, nl0,
+                      a.page_table + (int64_t)b * a.max_pages, tid);
             }
             return;
         }
@@ -281,10 +302,14 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         ts = a.lens_in_args ? a.text_arg[b] : a.has_text ? ld_uniform(a.text_starts, b) : a.Lq;
         nl = a.lens_in_args ? a.nl_arg[b] : a.has_new_lens ? ld_uniform(a.new_lens, b) : a.Lq;
     }
+    // key position of the first new token: behind the cache (4-bit cache: from
+    // the next whole tile on, so that no tile mixes the two)
+    int n_new = 0;
     if (step) {
+        n_new = C4 ? (n_pool + KT - 1) / KT * KT : n_pool;
         const int t_last = (int)fastdiv((uint32_t)(min(q0 + QT, (int)nrows) - 1), fd_gq);
-        k_hi = n_pool + min(nl, max(ts, t_last + 1));
-        kfull = n_pool + min(nl, max(ts, (int)fastdiv((uint32_t)q0, fd_gq) + 1));
+        k_hi = n_new + min(nl, max(ts, t_last + 1));
+        kfull = n_new + min(nl, max(ts, (int)fastdiv((uint32_t)q0, fd_gq) + 1));
     } else {
         n_pool = KIND == PREFILL_PAGED ? a.Lq : 0;
         const int q_last = min(q0 + QT, a.Lq) - 1;
@@ -346,7 +371,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         const int pc = min(row[n], (int)nrows - 1);
         tok[n] = row_token(pc);
         hqr[n] = row_head(pc, tok[n]);
-        if constexpr (step) kend[n] = n_pool + min(nl, max(ts, tok[n] + 1));
+        if constexpr (step) kend[n] = n_new + min(nl, max(ts, tok[n] + 1));
         else kend[n] = lane_key_end(win, min(q0 + rblk * 32 * NB + 32 * n, (int)nrows - 1), tok[n], lane);
         klo[n] = 0;
         if constexpr (WIN && step) klo[n] = n_pool + (tok[n] >= ts ? tok[n] : 0) - a.window;
@@ -470,6 +495,54 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         else wait_vm_lgkm<0>();
     };
 
+    // ---- 4-bit cache: tiles through registers -------------------------------
+    // Thread tid holds 1/8 of key row tid / 8 of a tile: a cached tile's codes
+    // and scale byte of K and V, or a new tile's bf16 values, loaded one loop
+    // step ahead of their way into the ring (values exact in bf16).  Rows past
+    // the last key repeat it.
+    constexpr int NC = D / 64;             // 16-byte chunks per thread
+    u32x4 rk[NC], rv[NC];
+    auto load4 = [&](int u, int page) {
+        const int kt = u * KT;
+        const int part = tid & 7;
+        if (kt < n_new) {
+            const int r = min(tid >> 3, n_pool - 1 - kt);
+            const uint8_t *g = a.pool4 + ((int64_t)page * a.Hkv + kvh) * cache4_bytes(D);
+            const uint8_t *kc4 = g + r * (D / 2) + part * (D / 16), *vc4 = kc4 + cache4_bytes(D) / 2;
+            const uint8_t *sc4 = g + KT * D / 2 + r * (D / 32) + part * (D / 32) / 8;
+            if constexpr (D == 128) {
+                const u32x2 x = *(const u32x2 *)kc4, y = *(const u32x2 *)vc4;
+                rk[0][0] = x[0], rk[0][1] = x[1], rv[0][0] = y[0], rv[0][1] = y[1];
+            } else {
+                rk[0][0] = *(const uint32_t *)kc4;
+                rv[0][0] = *(const uint32_t *)vc4;
+            }
+            rk[0][2] = sc4[0];
+            rv[0][2] = sc4[cache4_bytes(D) / 2];
+        } else {
+            const int64_t r = min(tid >> 3, k_hi - 1 - kt) + (kt - n_new);
+            const u32x4 *kn = (const u32x4 *)(kc_b + r * kst2 + part * (16 * NC));
+            const u32x4 *vn = (const u32x4 *)(vc_b + r * vst2 + part * (16 * NC));
+#pragma unroll
+            for (int c = 0; c < NC; ++c) rk[c] = kn[c], rv[c] = vn[c];
+        }
+    };
+    auto store4 = [&](int u, int s) {
+        const int r = tid >> 3, part = tid & 7;
+        if (u * KT < n_new) {
+            const uint32_t ck[2] = {rk[0][0], rk[0][1]}, cv[2] = {rv[0][0], rv[0][1]};
+            const uint32_t sk = rk[0][2], sv = rv[0][2];
+#pragma unroll
+            for (int c = 0; c < NC; ++c) rk[c] = unpack4(ck[c], sk), rv[c] = unpack4(cv[c], sv);
+        }
+        char *to = smem + s * TILEB + r * ROWB;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            *(u32x4 *)(to + 16 * ((NC * part + c) ^ swz<D>(r))) = rk[c];
+            *(u32x4 *)(to + VRING + 16 * ((NC * part + c) ^ swz<D>(r))) = rv[c];
+        }
+    };
+
     // ---- LDS read addresses -----------------------------------------------
     // K (A operand of S^T = K Q^T): lane (l32, hf) reads key row 32 * mb + l32,
     // chunk 2 * kk + hf, at kbase ^ (32 * kk): the row offset has no bits
@@ -581,7 +654,8 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int key = kt + mb * 32 + (v >> 2) * 8 + 4 * hf + (v & 3);
-                    if (key >= kend[n] || (WIN && key < klo[n] && key >= a.sinks)) sc[n][mb][v] = -INFINITY;
+                    const int end = C4 && kt < n_new ? n_pool : kend[n];
+                    if (key >= end || (WIN && key < klo[n] && key >= a.sinks)) sc[n][mb][v] = -INFINITY;
                 }
     };
     // Running max (log2 domain) from a tile's in-lane max, with lazy rescale:
@@ -638,7 +712,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     // softmax of a tile: mask, running max, P weights and their sum
     auto softmax = [&](int t, Tile &sc, bf16x8 (&pf)[NB][PF]) {
         const int kt = tile_of(t) * KT;
-        if (kt + KT > kfull || (WIN && kt < lo_max && kt + KT > a.sinks)) {
+        if (kt + KT > kfull || (WIN && kt < lo_max && kt + KT > a.sinks) || (C4 && kt < n_new && kt + KT > n_pool)) {
             // (a real branch: the compiler would otherwise turn this rare
             // path into selects executed on every tile)
             asm volatile("" ::: "memory");
@@ -708,6 +782,42 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     auto stage_off = [&](int t) -> uint32_t { return (uint32_t)((t - t_begin) % NSTAGE) * TILEB; };
     if constexpr (KG == 2) {
         // (below)
+    } else if constexpr (C4) {
+        // The same loop with tiles that every wave's threads bring in: in the
+        // softmax phase of step j tile j + 2 goes from the registers to the ring
+        // (its stage was last read in step j - 2) and the loads of tile j + 3 are
+        // issued.  A tile is read two steps after its store, so the trailing
+        // waves' share, one phase late, is complete too.
+        if (n_tiles > 0) {
+            const int n3 = min(n_tiles, 3);
+            for (int i = 0; i < n3; ++i) {
+                load4(t_begin + i, page_glb(t_begin + i));
+                if (i < 2) store4(t_begin + i, i);
+            }
+            int pg_next = page_glb(t_begin + 3);
+            wait_vm_lgkm<0>();   // (the query loads)
+            read_q();
+            wait_vm_lgkm<63>();
+            wg_barrier();
+            if (!lead) wg_barrier();
+            for (int j = t_begin; j <= t_end; ++j) {
+                asm volatile("" : "+v"(kbase), "+v"(vbase[0]), "+v"(vbase[1]));
+                if (busy) {
+                    if (j < t_end) qk(stage_off(j), S);
+                    if (j > t_begin) pv(stage_off(j - 1), pf);
+                }
+                wg_barrier();
+                if (j + 2 < t_end) store4(j + 2, (j + 2 - t_begin) % NSTAGE);
+                if (j + 3 < t_end) load4(j + 3, pg_next);
+                if (busy && j < t_end) softmax(j, S, pf);
+                pg_next = page_glb(j + 4);
+                wait_vm_lgkm<63>();   // (this wave's share of tile j + 2 is in the ring)
+                wg_barrier();
+            }
+            if (lead) wg_barrier();
+        } else {
+            wait_vm_lgkm<0>();
+        }
     } else if (n_tiles > 0) {
         // Prologue: the leading waves issue the first three tiles and wait
         // for the first and their query rows (the other two stay in flight
@@ -992,8 +1102,10 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     // This kernel reads the new block from kc/vc, never from the slots being
     // written, so the append can trail the attention; it comes after the
     // epilogue's stores so that its loads overlap their drain.
-    if (step && a.fuse_append && hh == 0)
-        append_share<D, NT>(a, b, kvh, (int)(qi * nsplit + split), napp, n_pool, nl, ptab, tid);
+    if (step && a.fuse_append && hh == 0) {
+        const auto share = C4 ? append_share4<D, NT> : append_share<D, NT>;
+        share(a, b, kvh, (int)(qi * nsplit + split), napp, n_pool, nl, ptab, tid);
+    }
 }
 
 // The merge is bound by latency: one round trip of loads behind the work
@@ -1213,6 +1325,7 @@ int launch_attn_d(const AttnArgs &a, const RaggedPlan *rag, TileShape shape, hip
         return a.mode == MODE_STEP ? launch_attn_t<D, STEP, 1, true>(a, NoPlan{}, st)
              : a.paged ? launch_prefill_t<D, PREFILL_PAGED, true>(a, shape.kg, st)
                        : launch_prefill_t<D, PREFILL_CONTIGUOUS, true>(a, shape.kg, st);
+    if (a.pool4) return launch_attn_t<D, STEP_CACHE4, 1>(a, NoPlan{}, st);
     return rag ? launch_attn_t<D, STEP_RAGGED, 1>(a, *rag, st)
          : a.mode == MODE_STEP ? shape.parts_only ? launch_attn_t<D, STEP_SPLIT, 1>(a, NoPlan{}, st)
                                                   : launch_attn_t<D, STEP, 1>(a, NoPlan{}, st)
