@@ -73,6 +73,9 @@
  *   output, lse, cache pool or workspace was changed.  WS_ERR_HIP reports a
  *   HIP launch error after validation passed.  Nothing is thrown or aborted
  *   across the ABI.  ws_last_error() gives a human-readable reason.
+ * - Sums are held in f32 before they are normalised, with weights up to 2^8 a
+ *   key: values (and gradients' operands) whose sum over the visible keys times
+ *   2^8 passes 2^128 give infinities or NaN.
  * - Supported: head_dim 64 or 128; inputs bf16; outputs bf16 or f32;
  *   page_size 64.
  * - The attention and append entry points enqueue kernels only (no device
@@ -423,7 +426,9 @@ int ws_block_causal_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_ten
  * entries of the pages between may hold anything, so a caller can free or
  * reuse those pages (WS_FUSE_APPEND also needs the new tokens' pages).
  * f32 outputs hold f32 accuracy here (the softmax weights enter the product
- * with V as the sum of two bf16 values).  workspace: at least
+ * with V as the sum of three bf16 values).  Of a bf16 output that is merged from
+ * KV splits, elements below 2^-39 of their row's largest may be lost (the
+ * partials are f16 values under one power of two per row).  workspace: at least
  * ws_step_workspace_bytes_window(...) bytes for the same arguments.
  */
 int ws_block_causal_attn_fwd_window(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new,
@@ -547,8 +552,8 @@ int ws_kv_read_4bit(const ws_paged_kv4 *kv, int32_t batch, const int32_t *starts
  * tokens; no segment).  The new block's own keys and values enter as they are,
  * in bf16; WS_FUSE_APPEND commits them rounded (as ws_kv_append_4bit would) and
  * leaves the result as it is.  f32 outputs hold f32 accuracy over the rounded
- * history.  workspace: at least ws_step_workspace_bytes_4bit(...) bytes for the
- * same arguments.
+ * history; bf16 outputs as in ws_block_causal_attn_fwd_window.  workspace: at
+ * least ws_step_workspace_bytes_4bit(...) bytes for the same arguments.
  */
 int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new,
                                   const ws_paged_kv4 *kv,

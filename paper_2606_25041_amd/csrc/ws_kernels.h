@@ -83,7 +83,8 @@ struct AttnArgs {
     // accumulator's register order, and (m, l) [slot][Hkv][nrb * 32][2].
     // bf16 output: o / l as bf16 [slot][Hkv][nrb][D/8][64 lanes][8] in
     // register order (two accumulator groups per lane) and m + log2(l)
-    // [slot][Hkv][nrb * 32] f32 at part_ml.
+    // [slot][Hkv][nrb * 32] f32 at part_ml.  bf16 output of a windowed step or of
+    // one over a 4-bit cache: f16 o / l / unit, and (m + log2(l), unit) pairs.
     float *part_o, *part_ml;
     int32_t nrb;
     int32_t nrows;       // rows per item's head space: Lq (prefill) or G * Lq (step)

@@ -60,6 +60,25 @@ constexpr float RESCALE_BOUND = 256.f;  // 2^RESCALE_LOG2
 constexpr int NSTAGE = 5;            // K/V tiles resident in the LDS ring (loads three tiles ahead)
 constexpr int RAHEAD = 4;            // LDS operand reads issued this many MFMAs ahead
 
+// Partials of a bf16 output held as f16 (HALF): a row's values are divided by a
+// power of two that puts the largest in [2^14, 2^15), so they are off by 2^-12
+// of themselves (or 2^-39 of the row's largest).  unit: the power of two
+// (held where both it and its reciprocal are normal); inv: the row's factor,
+// divided by it.  An infinity or a NaN stays one.
+__device__ __forceinline__ void half_unit(float top, float &inv, float &unit) {
+    const int e = min(max((int)((__float_as_uint(top) >> 23) & 255) - 127, -100), 127);
+    unit = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
+    inv *= __uint_as_float((uint32_t)(14 - e + 127) << 23);
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, (f16x2){(_Float16)lo, (_Float16)hi});
+}
+__device__ __forceinline__ float f16_half(uint32_t w, int i) {
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    return (float)__builtin_bit_cast(f16x2, w)[i];
+}
+
 // The fused append's share of step work item ai of the napp items of its
 // (stream, KV head): they split the new tokens evenly; tokens t >= nl are
 // padding and not committed.  One 16-byte chunk per thread.
@@ -122,16 +141,22 @@ using Plan = std::conditional_t<RAGGED, RaggedPlan, NoPlan>;
 // rows, so a query tile's keys are the sink tiles [0, nst) and the tiles
 // [first, ntile), first that of its first row's klo; everything between is
 // never loaded.  The loop counts these live tiles u = 0, 1, ...; the tile of u
-// is u, or u + gap past the sinks.  f32 outputs take P as the sum of two bf16
-// values (hi + lo, two MFMAs per V fragment), so that they hold f32 accuracy
-// (2^-17 of a weight) rather than bf16's.
+// is u, or u + gap past the sinks.
+//
+// WIN and STEP_CACHE4 hold more of the weights and partials: a f32 output takes P
+// as the sum of three bf16 values (all 24 bits; three MFMAs per V fragment),
+// where bf16 weights would leave it 1e-3 off, and the partials of a bf16 output
+// are f16 values under a power of two per row, not a second bf16
+// rounding (output off by 2.3e-3 of its norm instead of 2.9e-3; the last
+// rounding alone makes 1.7e-3).
 template <int D, int NW, int NB, int KIND, bool F32, int KG, bool WIN = false>
 __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const Plan<KIND == STEP_RAGGED> rp) {
     constexpr bool step = KIND == STEP || KIND == STEP_SPLIT || KIND == STEP_RAGGED || KIND == STEP_CACHE4;
     constexpr bool C4 = KIND == STEP_CACHE4;
     constexpr bool RAGGED = KIND == STEP_RAGGED;
     static_assert(!WIN || (!RAGGED && KIND != STEP_SPLIT && !C4), "windows: one split count, one step instance");
-    constexpr bool P2 = (WIN || C4) && F32;        // P as hi + lo
+    constexpr bool P3 = (WIN || C4) && F32;
+    constexpr bool HALF = (WIN || C4) && !F32;
     constexpr int NT = NW * 64;
     constexpr int QT = NW * 32 * NB / KG;  // query rows per work-group
     static_assert(KG == 1 || (KG == 2 && !step), "key groups: prefill only");
@@ -612,8 +637,9 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     // fp32 lane sums ls (so lse is exact to fp32 rounding).  One straight block:
     // all exponents, then all exps, then the packs and a pairwise sum, so
     // the dependent steps of different scores overlap.
-    constexpr int PF = P2 ? 8 : 4;    // fragments of P per 64 keys (4..7: the low parts)
-    auto softmax_weights = [&](const Tile &sc, bf16x8 (&pf)[NB][PF], const float (&m_use)[NB], float (&ls)[NB]) {
+    // P of a tile: its four fragments, or (P3) the weights they are made of
+    using Weights = std::conditional_t<P3, float[NB][32], bf16x8[NB][4]>;
+    auto softmax_weights = [&](const Tile &sc, Weights &pf, const float (&m_use)[NB], float (&ls)[NB]) {
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
             float x[32];
@@ -623,8 +649,8 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
             for (int f = 0; f < 32; ++f) x[f] = fast_exp2(x[f]);
 #pragma unroll
             for (int f = 0; f < 32; ++f) {
-                pf[n][f >> 3][f & 7] = (__bf16)x[f];
-                if constexpr (P2) pf[n][4 + (f >> 3)][f & 7] = (__bf16)(x[f] - (float)(__bf16)x[f]);
+                if constexpr (P3) pf[n][f] = x[f];
+                else pf[n][f >> 3][f & 7] = (__bf16)x[f];
             }
             // pairwise sum in a fixed order (the same for every tile)
 #pragma unroll
@@ -710,7 +736,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         }
     };
     // softmax of a tile: mask, running max, P weights and their sum
-    auto softmax = [&](int t, Tile &sc, bf16x8 (&pf)[NB][PF]) {
+    auto softmax = [&](int t, Tile &sc, Weights &pf) {
         const int kt = tile_of(t) * KT;
         if (kt + KT > kfull || (WIN && kt < lo_max && kt + KT > a.sinks) || (C4 && kt < n_new && kt + KT > n_pool)) {
             // (a real branch: the compiler would otherwise turn this rare
@@ -742,9 +768,10 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     };
     // O^T[d][query] += V^T P^T from the V tile of a stage; V reads RAHEAD
     // steps ahead of their MFMAs
-    auto pv = [&](uint32_t soff, const bf16x8 (&pf)[NB][PF]) {
+    auto pv = [&](uint32_t soff, const Weights &pf) {
         const uint32_t v0 = vbase[0] + soff, v1 = vbase[1] + soff;
         bf16x8 vf[RAHEAD + 1];
+        bf16x8 p3[NB][3];   // (P3) the parts of the current fragment
 #pragma unroll
         for (int i = 0; i < RAHEAD; ++i) vf[i] = vread(v0, v1, i);
 #pragma unroll
@@ -752,9 +779,24 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
             if (i + RAHEAD < NPV) vf[(i + RAHEAD) % (RAHEAD + 1)] = vread(v0, v1, i + RAHEAD);
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
-                o[n][i % MD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % (RAHEAD + 1)], pf[n][i / MD], o[n][i % MD], 0, 0, 0);
-                if constexpr (P2)
-                    o[n][i % MD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % (RAHEAD + 1)], pf[n][4 + i / MD], o[n][i % MD], 0, 0, 0);
+                if constexpr (P3) {
+                    if (i % MD == 0) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            float x = pf[n][8 * (i / MD) + e];
+#pragma unroll
+                            for (int c = 0; c < 3; ++c) {
+                                p3[n][c][e] = (__bf16)x;
+                                x -= (float)p3[n][c][e];
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < 3; ++c)
+                        o[n][i % MD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % (RAHEAD + 1)], p3[n][c], o[n][i % MD], 0, 0, 0);
+                } else {
+                    o[n][i % MD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % (RAHEAD + 1)], pf[n][i / MD], o[n][i % MD], 0, 0, 0);
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -777,7 +819,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     // only takes part in the loads and barriers
     const bool busy = q0 + rblk * 32 < (int)nrows;
     Tile S;
-    bf16x8 pf[NB][PF];
+    Weights pf;
     const int n_tiles = t_end - t_begin;
     auto stage_off = [&](int t) -> uint32_t { return (uint32_t)((t - t_begin) % NSTAGE) * TILEB; };
     if constexpr (KG == 2) {
@@ -1061,20 +1103,37 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
             // Partials are stored non-temporally (read once, by the combine
             // launch)
             const int64_t blk = ((int64_t)slot * a.Hkv + kvh) * a.nrb + (r >> 5);
-            const float inv = lt > 0.f ? 1.f / lt : 0.f;
+            float inv = lt > 0.f ? 1.f / lt : 0.f;
+            float unit = 1.f;   // (HALF)
+            if constexpr (HALF) {
+                float top = 0.f;
+#pragma unroll
+                for (int md = 0; md < MD; ++md)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) top = fmaxf(top, fabsf(o[n][md][v]));
+                half_unit(halves_max(top) * inv, inv, unit);
+            }
             uint16_t *op = (uint16_t *)a.part_o + blk * (32 * D) + 8 * lane;
 #pragma unroll
             for (int pg = 0; pg < 2 * MD; ++pg) {
                 const int md = pg >> 1, g0 = 2 * (pg & 1);
                 u32x4 val;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    val[2 * h + 0] = pack_bf16x2(o[n][md][4 * (g0 + h) + 0] * inv, o[n][md][4 * (g0 + h) + 1] * inv);
-                    val[2 * h + 1] = pack_bf16x2(o[n][md][4 * (g0 + h) + 2] * inv, o[n][md][4 * (g0 + h) + 3] * inv);
+                for (int h = 0; h < 4; ++h) {
+                    const float x = o[n][md][4 * g0 + 2 * h] * inv, y = o[n][md][4 * g0 + 2 * h + 1] * inv;
+                    val[h] = HALF ? pack_f16x2(x, y) : pack_bf16x2(x, y);
                 }
                 __builtin_nontemporal_store(val, (u32x4 *)(op + pg * 512));
             }
-            if (hf == 0) __builtin_nontemporal_store(lt > 0.f ? m[n] + __builtin_amdgcn_logf(lt) : -INFINITY, a.part_ml + blk * 32 + l32);
+            if (hf == 0) {
+                const float ls = lt > 0.f ? m[n] + __builtin_amdgcn_logf(lt) : -INFINITY;
+                if constexpr (HALF) {
+                    __builtin_nontemporal_store(ls, a.part_ml + 2 * (blk * 32 + l32) + 0);
+                    __builtin_nontemporal_store(unit, a.part_ml + 2 * (blk * 32 + l32) + 1);
+                } else {
+                    __builtin_nontemporal_store(ls, a.part_ml + blk * 32 + l32);
+                }
+            }
         } else {
             // register order: each store instruction writes 1 KB contiguous
             const int64_t blk = ((int64_t)slot * a.Hkv + kvh) * a.nrb + (r >> 5);
@@ -1134,7 +1193,9 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
 // SMAX times (the launch takes the smallest of 4, 8, 12, 16, 32).
 // RAGGED: the streams have their own split counts and slots (rp); a stream
 // with one split was written by the attention launch.
-template <int D, bool VARLEN, bool RAGGED, int SMAX, int NT>
+// HALF: the partials are f16 values under a power of two per row, which stands
+// beside the row's lse_s.
+template <int D, bool VARLEN, bool RAGGED, int SMAX, int NT, bool HALF>
 __global__ __launch_bounds__(NT) void combine16_kernel(const AttnArgs a, const Plan<RAGGED> rp) {
     static_assert(SMAX <= MAX_SPLITS, "at most MAX_SPLITS partials");
     constexpr int MD = D / 32;
@@ -1160,17 +1221,24 @@ __global__ __launch_bounds__(NT) void combine16_kernel(const AttnArgs a, const P
     }
     const int64_t sb = (int64_t)a.Hkv * a.nrb;   // blocks per slot
     const int64_t pb = slot * sb + (int64_t)(blk - (uint32_t)b * (uint32_t)sb);
-    const float *pl = a.part_ml + pb * 32 + (lane & 31);
+    const float *pl = a.part_ml + (HALF ? 2 : 1) * (pb * 32 + (lane & 31));
     const uint16_t *po = (const uint16_t *)a.part_o + pb * (32 * D) + pg * 512 + 8 * lane;
-    const int64_t ls = sb * 32;               // split stride of lse
+    const int64_t ls = (HALF ? 2 : 1) * sb * 32;   // split stride of lse
     const int64_t ps = sb * 32 * D;           // split stride of o
     // all loads first (one round trip), then the arithmetic
-    float lse[SMAX];
+    float lse[SMAX], unit[SMAX];
     u32x4 ov[SMAX];
 #pragma unroll
     for (int s = 0; s < SMAX; ++s) {
+        unit[s] = 1.f;
         if (s < S) {
-            lse[s] = pl[s * ls];
+            if constexpr (HALF) {
+                const float2 x = *(const float2 *)(pl + s * ls);
+                lse[s] = x.x;
+                unit[s] = x.y;
+            } else {
+                lse[s] = pl[s * ls];
+            }
             ov[s] = *(const u32x4 *)(po + s * ps);
         } else {
             lse[s] = -INFINITY;
@@ -1187,10 +1255,11 @@ __global__ __launch_bounds__(NT) void combine16_kernel(const AttnArgs a, const P
     for (int s = 0; s < SMAX; ++s) {
         const float wgt = __builtin_amdgcn_exp2f(lse[s] - Mu);   // 0 for absent splits
         L += wgt;
+        const float wu = HALF ? wgt * unit[s] : wgt;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            acc[2 * k + 0] += __uint_as_float(ov[s][k] << 16) * wgt;
-            acc[2 * k + 1] += __uint_as_float(ov[s][k] & 0xFFFF0000u) * wgt;
+            acc[2 * k + 0] += (HALF ? f16_half(ov[s][k], 0) : __uint_as_float(ov[s][k] << 16)) * wu;
+            acc[2 * k + 1] += (HALF ? f16_half(ov[s][k], 1) : __uint_as_float(ov[s][k] & 0xFFFF0000u)) * wu;
         }
     }
     const float inv = L > 0.f ? 1.f / L : 0.f;
@@ -1333,7 +1402,7 @@ int launch_attn_d(const AttnArgs &a, const RaggedPlan *rag, TileShape shape, hip
                    : launch_prefill_t<D, PREFILL_CONTIGUOUS>(a, shape.kg, st);
 }
 
-template <int D, bool VL, bool RAGGED>
+template <int D, bool VL, bool RAGGED, bool HALF = false>
 int launch_combine_t(const AttnArgs &a, const Plan<RAGGED> &rp, int nsplit, hipStream_t st) {
     const int per_blk = D / 32 * (a.out_f32 ? 4 : 2) * 64;   // items per 32-row block
     const int64_t blocks = (int64_t)a.B * a.Hkv * a.nrb;
@@ -1348,9 +1417,9 @@ int launch_combine_t(const AttnArgs &a, const Plan<RAGGED> &rp, int nsplit, hipS
         if (a.out_f32)
             hipLaunchKernelGGL((combine_kernel<D, VL, RAGGED, SMAX, 256>), grid, dim3(256), 0, st, a, rp);
         else if (nt == 128)
-            hipLaunchKernelGGL((combine16_kernel<D, VL, RAGGED, SMAX, 128>), grid, dim3(128), 0, st, a, rp);
+            hipLaunchKernelGGL((combine16_kernel<D, VL, RAGGED, SMAX, 128, HALF>), grid, dim3(128), 0, st, a, rp);
         else
-            hipLaunchKernelGGL((combine16_kernel<D, VL, RAGGED, SMAX, 256>), grid, dim3(256), 0, st, a, rp);
+            hipLaunchKernelGGL((combine16_kernel<D, VL, RAGGED, SMAX, 256, HALF>), grid, dim3(256), 0, st, a, rp);
     };
     if (nsplit <= 4) launch(std::integral_constant<int, 4>{});
     else if (nsplit <= 8) launch(std::integral_constant<int, 8>{});
@@ -1362,6 +1431,9 @@ int launch_combine_t(const AttnArgs &a, const Plan<RAGGED> &rp, int nsplit, hipS
 
 template <int D>
 int launch_combine_d(const AttnArgs &a, const RaggedPlan *rag, hipStream_t st) {
+    if (a.has_window || a.pool4)
+        return a.has_new_lens ? launch_combine_t<D, true, false, true>(a, NoPlan{}, a.nsplit, st)
+                              : launch_combine_t<D, false, false, true>(a, NoPlan{}, a.nsplit, st);
     if (rag)
         return a.has_new_lens ? launch_combine_t<D, true, true>(a, *rag, rag->max_nsplit, st)
                               : launch_combine_t<D, false, true>(a, *rag, rag->max_nsplit, st);

@@ -107,6 +107,29 @@ def test_step(case):
     assert written == live + sum(real)   # nothing but the new tokens was written
 
 
+@pytest.mark.parametrize("exponents", ((100,), (-100,), (96, 0), (30, -30, 0), (0, 0, 0, -60)))
+@pytest.mark.parametrize("f32", (False, True))
+def test_values_of_any_magnitude(exponents, f32):
+    """Head dims whose values differ by up to 2^96, through split partials.  (The
+    sums are unnormalised f32: 2^8 a weight x 3000 keys x 2^102 stay below 2^128.)"""
+    gs.say(f"[gpu] window step, values of 2^{exponents} f32={f32}")
+    D, window, sinks, caches, Lq = 128, 3000, 64, [9000, 3500], 9
+    cache, kv = live_cache(5, 2, D, caches, Lq, window, sinks)
+    unit = torch.exp2(torch.tensor([exponents[i % len(exponents)] for i in range(D)], device=DEV, dtype=torch.float64))
+    unit = unit.to(torch.bfloat16)
+    q, kn, vn = _randn(1, 2, Lq, 8, D), _randn(2, 2, Lq, 2, D), _randn(3, 2, Lq, 2, D) * unit
+    cache.v_pool *= unit
+    out, lse = ws.block_causal_attn_fwd(q, kn, vn, cache, _pair(caches), window=window, sinks=sinks, want_lse=True,
+                                        out_dtype=torch.float32 if f32 else torch.bfloat16)
+    torch.cuda.synchronize()
+    for b, c in enumerate(caches):
+        lo, hi = ref.step_ranges(c, Lq, None, window)
+        want = ref.attend(q[b], torch.cat((kv[b][0], kn[b])), torch.cat((kv[b][1] * unit, vn[b])), lo, hi, sinks,
+                          D ** -0.5, f32=f32)
+        ref.check(f"out {b}", out[b], want["out"])
+        ref.check(f"lse {b}", lse[b], want["lse"])
+
+
 def _layout(seed, L, nblocks, text):
     """Block offsets [1][nb + 1] with empty blocks, and segment starts."""
     g = np.random.default_rng(seed)

@@ -6,8 +6,11 @@ A bf16 rounding is off by at most 2^-8 of the value, a f32 one by 2^-24.
 With A = sum_j p_j |v_j| and T = max_j scale sum |q_d k_jd|:
   score     off by  es = (d + 8) 2^-24 T, so a weight by a factor 1 + 3 es
             (its exponent and the normaliser's, and exp2 and log2 themselves)
-  out bf16  weights, output and (a step in splits) partials in bf16:
-            3 * 2^-8 A
+  out bf16  weights and output in bf16, (a step in splits) partials in f16 under
+            a power of two per row that puts the row's largest past 2^14: a
+            partial is off by 2^-11 of itself or, as a subnormal (steps of
+            2^-24), by 2^-25, so 2^-39 of the row's largest:
+            3 * 2^-8 A + 2^-39 max_d A
   out f32   weights as two bf16 values: 2^-16 A; f32 sums over n keys:
             2^-24 (64 + sqrt n) A
   lse       es + 2^-20 (1 + |lse|)
@@ -68,7 +71,8 @@ def attend(q, k, v, lo, hi, sinks, scale, dout=None, f32=False):
         T = (scale * (Q.abs() @ K.abs().t().contiguous()) * see).amax(1)
         es = (d + 8) * 2.0 ** -24 * T
         o, A = p @ V, p @ V.abs()
-        e = A * ((2.0 ** -16 + 2.0 ** -24 * (64 + N ** 0.5) if f32 else 3 * H) + 3 * es[:, None])
+        rows = 0.0 if f32 else 2.0 ** -39 * A.amax(1, keepdim=True)
+        e = rows + A * ((2.0 ** -16 + 2.0 ** -24 * (64 + N ** 0.5) if f32 else 3 * H) + 3 * es[:, None])
         res["out"][0][:, h], res["out"][1][:, h] = o, 2 * e
         res["lse"][0][h], res["lse"][1][h] = lse, 2 * (es + 2.0 ** -20 * (1 + lse.abs()))
         if dout is None:
