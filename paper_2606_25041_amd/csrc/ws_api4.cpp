@@ -51,6 +51,31 @@ int64_t tile_keys(int batch, int new_len, const int32_t *cache_lens, const int32
     return 64 * most;
 }
 
+// A step of few packed rows: tiles in one line per KV head, an even share for
+// each work-group, one work-group per compute unit (its LDS tiles allow one);
+// a share is at least a tile per wave.
+bool few_rows(int batch, int G, int new_len) { return batch <= LENS_IN_ARGS && (int64_t)G * new_len <= FEW_ROWS; }
+
+Few4Plan plan_few(int num_cus, int batch, int hkv, int new_len, const int32_t *cache_lens, const int32_t *nl) {
+    Few4Plan p{};
+    int64_t at = 0;
+    for (int b = 0; b < batch; ++b) {
+        p.start[b] = (int32_t)at;
+        at += ((int64_t)cache_lens[b] + 63) / 64 + ((nl ? nl[b] : new_len) + 63) / 64;
+    }
+    p.start[batch] = (int32_t)at;   // (at most 32 streams of 2^25 tiles)
+    const int64_t most = std::max(1, num_cus / hkv);
+    p.per = (int32_t)std::max<int64_t>((at + most - 1) / most, 8);
+    p.nwg = (int32_t)((at + p.per - 1) / p.per);
+    p.fd_per = fastdiv_make((uint32_t)p.per);
+    return p;
+}
+
+// Partials: a part of 32 rows x D and the rows' (m, l), f32, per KV head.
+size_t few_workspace(const Few4Plan &p, int batch, int hkv, int d) {
+    return p.nwg <= 1 ? 0 : (size_t)(p.nwg + batch) * hkv * 32 * (d + 2) * sizeof(float);
+}
+
 }  // namespace
 }  // namespace ws
 
@@ -112,6 +137,9 @@ size_t ws_step_workspace_bytes_4bit(int32_t batch, int32_t num_q_heads, int32_t 
     }
     int cus = 0;
     if (current_device_cus(&cus)) return 0;
+    if (few_rows(batch, num_q_heads / num_kv_heads, new_len))
+        return few_workspace(plan_few(cus, batch, num_kv_heads, new_len, cache_lens_host, new_lens_host), batch,
+                             num_kv_heads, 128);
     const StepPlan p = plan_step(cus, batch, num_q_heads, num_kv_heads, new_len,
                                  tile_keys(batch, new_len, cache_lens_host, new_lens_host), new_lens_host);
     return step_workspace(p, batch, num_q_heads, num_kv_heads, new_len);
@@ -157,9 +185,18 @@ int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_n
     int cus = 0;
     if (int e = current_device_cus(&cus))
         return fail(WS_ERR_HIP, "cannot query the device's compute units (hip error %d)", e);
-    const StepPlan plan = plan_step(cus, batch, num_q_heads, kv->num_kv_heads, new_len,
-                                    tile_keys(batch, new_len, cache_lens_host, nl_host), nl_host);
-    const size_t need = step_workspace(plan, batch, num_q_heads, kv->num_kv_heads, new_len);
+    const bool few = few_rows(batch, G, new_len);
+    Few4Plan line{};
+    StepPlan plan{};
+    size_t need;
+    if (few) {
+        line = plan_few(cus, batch, kv->num_kv_heads, new_len, cache_lens_host, nl_host);
+        need = few_workspace(line, batch, kv->num_kv_heads, 128);
+    } else {
+        plan = plan_step(cus, batch, num_q_heads, kv->num_kv_heads, new_len,
+                         tile_keys(batch, new_len, cache_lens_host, nl_host), nl_host);
+        need = step_workspace(plan, batch, num_q_heads, kv->num_kv_heads, new_len);
+    }
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
         return fail(WS_ERR_WORKSPACE, "workspace needs %zu bytes (16-byte aligned), got %zu", need,
                     workspace ? workspace_bytes : (size_t)0);
@@ -176,14 +213,18 @@ int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_n
     a.B = batch; a.Lq = new_len; a.Hq = num_q_heads; a.Hkv = kv->num_kv_heads; a.G = G;
     a.mode = MODE_STEP;
     a.fuse_append = fuse;
-    a.nsplit = plan.nsplit;
-    a.nqt = plan.nqt;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.gi = 1;
     a.nrows = G * new_len;
     a.nrb = (a.nrows + 31) / 32;
     a.fd_nrb = fastdiv_make((uint32_t)a.nrb);
-    if (plan.nsplit > 1) {
+    a.fd_gq = fastdiv_make((uint32_t)G);
+    a.nsplit = plan.nsplit;
+    a.nqt = plan.nqt;
+    if (few) {
+        a.part_o = (float *)workspace;
+        a.part_ml = a.part_o + (size_t)(line.nwg + batch) * a.Hkv * 32 * kv->head_dim;
+    } else if (plan.nsplit > 1) {
         a.part_o = (float *)workspace;
         a.part_ml = a.part_o + (size_t)plan.nsplit * batch * a.Hkv * a.nrb * 32 * kv->head_dim;
     }
@@ -202,6 +243,11 @@ int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_n
             a.text_arg[b] = text_host ? text_host[b] : new_len;
             a.nl_arg[b] = nl_host ? nl_host[b] : new_len;
         }
+    }
+    if (few) {
+        if (int e = launch_few4(a, line, kv->head_dim, stream))
+            return fail(WS_ERR_HIP, "attention launch failed (hip error %d)", e);
+        return ok();
     }
     if (!finish_work(a)) return fail(WS_ERR_SHAPE, "too many work items");
     if (int e = launch_attention(a, nullptr, kv->head_dim, plan.shape, stream))

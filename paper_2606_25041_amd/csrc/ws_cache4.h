@@ -20,7 +20,8 @@
 namespace ws {
 namespace {
 
-// Eight values of a chunk (codes: four bytes, scale byte s) as bf16.
+// Eight values of a chunk (codes: four bytes, scale byte s) as bf16.  A scale
+// whose exponent field is 255 makes the conversion return NaN.
 __device__ __forceinline__ u32x4 unpack4(uint32_t codes, uint32_t s) {
     const float scale = __uint_as_float(s << 23);
     u32x4 x;
@@ -28,7 +29,6 @@ __device__ __forceinline__ u32x4 unpack4(uint32_t codes, uint32_t s) {
     x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
     x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
     x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
-    if (s == 255) x = u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
     return x;
 }
 

@@ -185,6 +185,20 @@ struct Cache4Args {
     int32_t B, Ln, Hkv, D;
 };
 
+// A step of at most FEW_ROWS packed rows per (stream, KV head) over a 4-bit
+// cache (beside the AttnArgs).  The tiles of all streams, each a cache page or
+// the new block behind them, stand in one line; work-group w of a KV head takes
+// tiles [w * per, (w + 1) * per) of it, so that all read the same amount whatever
+// the streams' lengths.  The part of a work-group in a stream has the partial
+// slot w + stream (both grow along the line, one of them at every part).
+constexpr int FEW_ROWS = 32;
+struct Few4Plan {
+    int32_t per;                       // tiles of a work-group
+    int32_t nwg;                       // work-groups of a KV head
+    FastDiv fd_per;                    // divider by per
+    int32_t start[LENS_IN_ARGS + 1];   // first tile of each stream, and the end
+};
+
 // Key tiles (128 keys) of a dK/dV launch that may be split over work-groups,
 // and splits of one of them, at most.
 constexpr int BWD_MAX_SPLIT_TILES = 128;
@@ -254,6 +268,8 @@ int launch_combine(const AttnArgs &a, const RaggedPlan *rag, int head_dim, void 
 int launch_append(const AppendArgs &a, void *stream);
 int launch_append4(const Cache4Args &a, void *stream);
 int launch_read4(const Cache4Args &a, void *stream);
+// a step of few rows: the attention, then the merge of its partials
+int launch_few4(const AttnArgs &a, const Few4Plan &p, int head_dim, void *stream);
 // dQ (with the row data), then dK/dV and the sum of its parts; 0 or a HIP error code
 int launch_prefill_bwd(const BwdArgs &a, int head_dim, void *stream);
 // Compute units of the current HIP device (queried once per device, then
