@@ -447,7 +447,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         t.straddle = false;
         if (holed(kt)) {
             t.straddle = true;
-        } else if (KIND != PREFILL_CONTIGUOUS && kt + KT <= n_pool) {
+        } else if (KIND != PREFILL_CONTIGUOUS && !C4 && kt + KT <= n_pool) {
             // whole tile in one cache page
             const int64_t tb = ((int64_t)page * a.Hkv + kvh) * TILEB;
             t.bk = kpool_b + tb;
@@ -456,7 +456,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
             t.ok = t.ov = lofs_p;
         } else if (KIND != PREFILL_PAGED && kt >= n_pool && kt + KT <= k_hi) {
             // whole tile in the contiguous keys
-            const int64_t j0 = kt - n_pool + lwave * RPW;
+            const int64_t j0 = kt - (C4 ? n_new : n_pool) + lwave * RPW;
             t.bk = kc_b + j0 * kst2;
             t.bv = vc_b + j0 * vst2;
             t.sk = NWD * RPW * kst2;
@@ -479,7 +479,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         const uint32_t vd = kd + VRING;
         const int64_t tb = ((int64_t)page * a.Hkv + kvh) * TILEB;
         const char *kg = kpool_b + tb, *vg = vpool_b + tb;
-        const int64_t c0 = (int64_t)(kt - n_pool);   // contiguous row of the tile's first key
+        const int64_t c0 = (int64_t)(kt - (C4 ? n_new : n_pool));   // contiguous row of the tile's first key
         const char *kcg = kc_b + c0 * kst2, *vcg = vc_b + c0 * vst2;
         const uint32_t lofs_c = lofs_p - lrow0 * ROWB;   // the chunk's byte offset in a row
 #pragma unroll
@@ -521,58 +521,58 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     };
 
     // ---- 4-bit cache: tiles through registers -------------------------------
-    // Thread tid holds 1/8 of key row tid / 8 of a tile: a cached tile's codes
-    // and scale byte of K and V, or a new tile's bf16 values, loaded one loop
-    // step ahead of their way into the ring (values exact in bf16).  Rows past
-    // the last key repeat it.
-    constexpr int NC = D / 64;             // 16-byte chunks per thread
-    u32x4 rk[NC], rv[NC];
+    // Thread tid holds 1/8 of key row tid / 8 of a cached tile: its codes and V's
+    // scale byte, and K's scales of row tid % 64, loaded one loop step ahead of
+    // their way into the ring (unconditionally, so that nothing waits for them
+    // before).  Rows past the last cached token repeat it.  V is unpacked on the
+    // way (its values are exact in bf16); K's codes stay as they are, so that a
+    // wave reads a quarter of the bytes for S^T, and unpacking the fragments
+    // stands beside the MFMAs (2 x (512 + 131072) keys, GQA 64/8 x 128: 5.38 ms
+    // with K unpacked on the way too and loads that a branch's merge waited for,
+    // 5.22 with K's codes in the ring, 4.13 with unconditional loads).  16-byte
+    // chunk c of a row of codes lies in slot c ^ cswz(row).
+    constexpr int NC = D / 64;             // 16-byte chunks of unpacked values per thread
+    auto cswz = [](int r) -> int { return D == 128 ? (r >> 2) & 3 : (r >> 3) & 1; };
+    const int tc_end = C4 ? min(t_end, n_new / KT) : 0;   // end of the cached tiles
+    // tile u's page (the last one's past the end, any page where there is none)
+    auto page4 = [&](int u) -> int { return n_pool > 0 ? ld_uniform(ptab, max(min(u, tc_end - 1), 0)) : 0; };
+    u32x2 rk4, rv4;
+    uint32_t sk4, sv4;
     auto load4 = [&](int u, int page) {
-        const int kt = u * KT;
-        const int part = tid & 7;
-        if (kt < n_new) {
-            const int r = min(tid >> 3, n_pool - 1 - kt);
-            const uint8_t *g = a.pool4 + ((int64_t)page * a.Hkv + kvh) * cache4_bytes(D);
-            const uint8_t *kc4 = g + r * (D / 2) + part * (D / 16), *vc4 = kc4 + cache4_bytes(D) / 2;
-            const uint8_t *sc4 = g + KT * D / 2 + r * (D / 32) + part * (D / 32) / 8;
-            if constexpr (D == 128) {
-                const u32x2 x = *(const u32x2 *)kc4, y = *(const u32x2 *)vc4;
-                rk[0][0] = x[0], rk[0][1] = x[1], rv[0][0] = y[0], rv[0][1] = y[1];
-            } else {
-                rk[0][0] = *(const uint32_t *)kc4;
-                rv[0][0] = *(const uint32_t *)vc4;
-            }
-            rk[0][2] = sc4[0];
-            rv[0][2] = sc4[cache4_bytes(D) / 2];
+        const int kt = max(min(u, tc_end - 1), 0) * KT, part = tid & 7;
+        const int r = max(min(tid >> 3, n_pool - 1 - kt), 0), rs = max(min(tid & 63, n_pool - 1 - kt), 0);
+        const uint8_t *g = a.pool4 + ((int64_t)page * a.Hkv + kvh) * cache4_bytes(D);
+        const uint32_t oc = r * (D / 2) + part * (D / 16), os = KT * D / 2;
+        if constexpr (D == 128) {
+            rk4 = *(const u32x2 *)(g + oc);
+            rv4 = *(const u32x2 *)(g + oc + cache4_bytes(D) / 2);
+            sk4 = *(const uint32_t *)(g + os + rs * (D / 32));
         } else {
-            const int64_t r = min(tid >> 3, k_hi - 1 - kt) + (kt - n_new);
-            const u32x4 *kn = (const u32x4 *)(kc_b + r * kst2 + part * (16 * NC));
-            const u32x4 *vn = (const u32x4 *)(vc_b + r * vst2 + part * (16 * NC));
-#pragma unroll
-            for (int c = 0; c < NC; ++c) rk[c] = kn[c], rv[c] = vn[c];
+            rk4[0] = *(const uint32_t *)(g + oc);
+            rv4[0] = *(const uint32_t *)(g + oc + cache4_bytes(D) / 2);
+            sk4 = *(const uint16_t *)(g + os + rs * (D / 32));
         }
+        sv4 = g[os + r * (D / 32) + part * (D / 32) / 8 + cache4_bytes(D) / 2];
     };
-    auto store4 = [&](int u, int s) {
+    auto store4 = [&](int s) {
         const int r = tid >> 3, part = tid & 7;
-        if (u * KT < n_new) {
-            const uint32_t ck[2] = {rk[0][0], rk[0][1]}, cv[2] = {rv[0][0], rv[0][1]};
-            const uint32_t sk = rk[0][2], sv = rv[0][2];
+        char *to = smem + s * TILEB;
+        if constexpr (D == 128) *(u32x2 *)(to + r * (D / 2) + 16 * ((part >> 1) ^ cswz(r)) + 8 * (part & 1)) = rk4;
+        else *(uint32_t *)(to + r * (D / 2) + 16 * ((part >> 2) ^ cswz(r)) + 4 * (part & 3)) = rk4[0];
+        if (tid < KT) *(uint32_t *)(to + KT * D / 2 + 4 * tid) = sk4;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) rk[c] = unpack4(ck[c], sk), rv[c] = unpack4(cv[c], sv);
-        }
-        char *to = smem + s * TILEB + r * ROWB;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            *(u32x4 *)(to + 16 * ((NC * part + c) ^ swz<D>(r))) = rk[c];
-            *(u32x4 *)(to + VRING + 16 * ((NC * part + c) ^ swz<D>(r))) = rv[c];
-        }
+        for (int c = 0; c < NC; ++c)
+            *(u32x4 *)(to + VRING + r * ROWB + 16 * ((NC * part + c) ^ swz<D>(r))) = unpack4(rv4[c], sv4);
     };
 
     // ---- LDS read addresses -----------------------------------------------
     // K (A operand of S^T = K Q^T): lane (l32, hf) reads key row 32 * mb + l32,
     // chunk 2 * kk + hf, at kbase ^ (32 * kk): the row offset has no bits
     // below 128 and chunk 2 * kk ^ swz only changes bits 5.. of the slot.
-    uint32_t kbase = l32 * ROWB + 16 * (hf ^ swz<D>(l32));
+    // (4-bit cache: step kk = 4 s + f takes dims 64 s + 32 hf + 8 f + [0, 8), the
+    // order in which a lane holds a cached key's codes: chunk 8 s + 4 hf + f, at
+    // kbase ^ (128 s + 16 f))
+    uint32_t kbase = l32 * ROWB + 16 * ((C4 ? 4 * hf : hf) ^ swz<D>(l32));
     // V^T fragments (A operand of O^T += V^T P^T) by transpose reads: lane
     // reads key rows 16 * ks4 + vr and +8, 4 head-dim columns of chunk
     // 4 * md + vc, at vbase[e] ^ (64 * md).
@@ -588,7 +588,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     auto read_q = [&]() {
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk)
-            qf[0][kk] = *(const bf16x8 *)(smem + q_stage + (kbase ^ (32 * kk)));
+            qf[0][kk] = *(const bf16x8 *)(smem + q_stage + (kbase ^ (C4 ? 128 * (kk >> 2) + 16 * (kk & 3) : 32 * kk)));
     };
 
     const float c2 = a.scale_log2;
@@ -615,7 +615,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     // commutes with the XORs on the low address bits)
     // K fragment of S^T step i (kk = i / 2, key block mb = i % 2)
     auto kread = [&](uint32_t kb, int i) -> bf16x8 {
-        return *(const bf16x8 *)(smem + (i & 1) * 32 * ROWB + (kb ^ (32 * (i >> 1))));
+        return *(const bf16x8 *)(smem + (i & 1) * 32 * ROWB + (kb ^ (C4 ? 128 * (i >> 3) + 16 * ((i >> 1) & 3) : 32 * (i >> 1))));
     };
     // V^T fragment of O^T step i (ks4 = i / MD, md = i % MD) by two
     // transpose reads
@@ -735,6 +735,35 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    // The same from a cached tile's codes: two words in front of the MFMAs that
+    // take them, unpacked one step ahead.
+    auto qk4 = [&](uint32_t soff, Tile &sn) {
+        u32x4 raw[2][NC];
+        uint32_t sc[2];
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb) {
+            const int r = 32 * mb + l32;
+#pragma unroll
+            for (int s = 0; s < NC; ++s)
+                raw[mb][s] = *(const u32x4 *)(smem + soff + r * (D / 2) + 16 * ((2 * s + hf) ^ cswz(r)));
+            sc[mb] = *(const uint32_t *)(smem + soff + KT * D / 2 + 4 * r) >> (8 * hf);
+        }
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sn[0][mb][v] = 0.f;
+        auto frag = [&](int i) -> bf16x8 {   // step i: kk = i / 2, key block i % 2
+            const int s = i >> 3, f = (i >> 1) & 3;
+            return __builtin_bit_cast(bf16x8, unpack4(raw[i & 1][s][f], (sc[i & 1] >> (16 * s)) & 255));
+        };
+        bf16x8 kf[3] = {frag(0), frag(1), frag(1)};
+#pragma unroll
+        for (int i = 0; i < NQK; ++i) {
+            if (i + 2 < NQK) kf[(i + 2) % 3] = frag(i + 2);
+            sn[0][i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % 3], qf[0][i >> 1], sn[0][i & 1], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
     // softmax of a tile: mask, running max, P weights and their sum
     auto softmax = [&](int t, Tile &sc, Weights &pf) {
         const int kt = tile_of(t) * KT;
@@ -825,34 +854,43 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     if constexpr (KG == 2) {
         // (below)
     } else if constexpr (C4) {
-        // The same loop with tiles that every wave's threads bring in: in the
-        // softmax phase of step j tile j + 2 goes from the registers to the ring
-        // (its stage was last read in step j - 2) and the loads of tile j + 3 are
-        // issued.  A tile is read two steps after its store, so the trailing
-        // waves' share, one phase late, is complete too.
+        // The same loop with cached tiles that every wave's threads bring in: in
+        // the softmax phase of step j tile j + 2 goes from the registers to the
+        // ring (its stage was last read in step j - 2) and the loads of tile j + 3
+        // are issued.  A tile is read two steps after its store, so the trailing
+        // waves' share, one phase late, is complete too.  The new block's tiles
+        // come as in a bf16 step.
         if (n_tiles > 0) {
-            const int n3 = min(n_tiles, 3);
-            for (int i = 0; i < n3; ++i) {
-                load4(t_begin + i, page_glb(t_begin + i));
-                if (i < 2) store4(t_begin + i, i);
+            for (int i = 0; i < min(n_tiles, 3); ++i) {
+                const int u = t_begin + i;
+                if (u < tc_end) {
+                    load4(u, page4(u));
+                    if (i < 2) store4(i);
+                } else if (lead) {
+                    issue_tile(u, i, 0);
+                }
             }
-            int pg_next = page_glb(t_begin + 3);
-            wait_vm_lgkm<0>();   // (the query loads)
+            int pg_next = page4(t_begin + 3);
+            wait_vm_lgkm<0>();   // (the query loads, and new tiles)
             read_q();
             wait_vm_lgkm<63>();
             wg_barrier();
             if (!lead) wg_barrier();
             for (int j = t_begin; j <= t_end; ++j) {
-                asm volatile("" : "+v"(kbase), "+v"(vbase[0]), "+v"(vbase[1]));
+                asm volatile("" : "+v"(kbase), "+v"(vbase[0]), "+v"(vbase[1]), "+v"(lofs_k), "+v"(lofs_v));
                 if (busy) {
-                    if (j < t_end) qk(stage_off(j), S);
+                    if (j < tc_end) qk4(stage_off(j), S);
+                    else if (j < t_end) qk(stage_off(j), S);
                     if (j > t_begin) pv(stage_off(j - 1), pf);
                 }
                 wg_barrier();
-                if (j + 2 < t_end) store4(j + 2, (j + 2 - t_begin) % NSTAGE);
-                if (j + 3 < t_end) load4(j + 3, pg_next);
+                if (j + 2 < tc_end) store4((j + 2 - t_begin) % NSTAGE);
+                load4(j + 3, pg_next);
+                if (lead && j + 3 >= tc_end && j + 3 < t_end) issue_tile(j + 3, (j + 3 - t_begin) % NSTAGE, 0);
                 if (busy && j < t_end) softmax(j, S, pf);
-                pg_next = page_glb(j + 4);
+                pg_next = page4(j + 4);
+                // a new tile j + 1 landed; tiles j + 2 and j + 3 may stay in flight
+                if (lead && j + 1 >= tc_end && j + 1 < t_end) wait_tiles(min(2, t_end - 2 - j));
                 wait_vm_lgkm<63>();   // (this wave's share of tile j + 2 is in the ring)
                 wg_barrier();
             }
