@@ -87,7 +87,13 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     char *vt = smem + wave * TILEB;
     const float c2 = a.scale_log2;
-    // LDS addresses of the transpose reads (attn_kernel)
+    // LDS addresses of the transpose reads (attn_kernel), and of the unpacked
+    // values: load i of V's codes gives a lane row i * VR + lane / LB (the swizzle
+    // repeats every 16 rows), dims 32 (lane % LB) + [0, 32): chunk f of them at
+    // wbase ^ (16 f), + i * VR rows
+    constexpr int LB = D / 32, VR = 64 / LB;
+    static_assert(VR % 16 == 0, "the swizzle must repeat across the loads");
+    uint32_t wbase = (uint32_t)((lane / LB) * ROWB + 16 * ((4 * (lane % LB)) ^ swz<D>(lane / LB)));
     const int j16 = lane & 15;
     uint32_t vbase[2];
 #pragma unroll
@@ -103,8 +109,9 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
     };
 
     const int end = min((w + 1) * p.per, p.start[a.B]);
-    int pos = w * p.per, b = 0;
-    while (p.start[b + 1] <= pos) ++b;
+    int pos = w * p.per;
+    // the stream of pos: one load of all starts and a ballot
+    int b = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < a.B && p.start[min(lane, LENS_IN_ARGS - 1) + 1] <= pos));
     for (; pos < end; ++b) {
         const int t_end = min(end, p.start[b + 1]) - p.start[b];
         const int n = a.lens_arg[b], nl = a.nl_arg[b], ts = a.text_arg[b];
@@ -132,19 +139,22 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
         // raw tile: codes and scales
         u32x4 kc[2][KS], vc[NV];
         uint32_t ks[2], vs[NV];
-        auto load = [&](int t) {
-            const uint8_t *g = a.pool4 + ((int64_t)ld_uniform(ptab, t) * a.Hkv + kvh) * cache4_bytes(D);
+        auto load = [&](int page) {
+            // (wave-uniform base, 32-bit lane offsets)
+            const uint8_t *g = a.pool4 + ((int64_t)page * a.Hkv + kvh) * cache4_bytes(D);
+            const uint32_t ko = (uint32_t)(l32 * (D / 2) + 16 * hf), so = (uint32_t)(l32 * (D / 32));
+            const uint32_t vo = (uint32_t)(16 * lane), wo = (uint32_t)lane;
 #pragma unroll
             for (int mb = 0; mb < 2; ++mb) {
-                const int r = 32 * mb + l32;
 #pragma unroll
-                for (int s = 0; s < KS; ++s) kc[mb][s] = *(const u32x4 *)(g + r * (D / 2) + 32 * s + 16 * hf);
-                ks[mb] = D == 128 ? *(const uint32_t *)(g + SC + 4 * r) : *(const uint16_t *)(g + SC + 2 * r);
+                for (int s = 0; s < KS; ++s) kc[mb][s] = *(const u32x4 *)(g + 32 * mb * (D / 2) + 32 * s + ko);
+                if constexpr (D == 128) ks[mb] = *(const uint32_t *)(g + SC + 32 * mb * (D / 32) + so);
+                else ks[mb] = *(const uint16_t *)(g + SC + 32 * mb * (D / 32) + so);
             }
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                vc[i] = *(const u32x4 *)(g + HALFB + 1024 * i + 16 * lane);
-                vs[i] = g[HALFB + SC + 64 * i + lane];
+                vc[i] = *(const u32x4 *)(g + HALFB + 1024 * i + vo);
+                vs[i] = g[HALFB + SC + 64 * i + wo];
             }
         };
         // S^T, masked where the keys end, to the weights and O^T += V^T P^T
@@ -177,30 +187,40 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
                 ls = weights(m == -INFINITY ? 0.f : m);
             }
             l += ls;
+            constexpr int NP = F32 ? 3 : 1;   // (f32 outputs: all 24 bits of the weights, as attn_kernel)
+            constexpr int AHEAD = 4;          // V fragments read this many steps ahead
+            bf16x8 pf[NP], vf[AHEAD + 1];
 #pragma unroll
-            for (int k4 = 0; k4 < NK; ++k4) {
-                constexpr int NP = F32 ? 3 : 1;   // (f32 outputs: all 24 bits of the weights, as attn_kernel)
-                bf16x8 pf[NP];
+            for (int i = 0; i < AHEAD; ++i) vf[i] = vread(i / MD, i % MD);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float r = x[8 * k4 + e];
+            for (int i = 0; i < NK * MD; ++i) {
+                if (i + AHEAD < NK * MD) vf[(i + AHEAD) % (AHEAD + 1)] = vread((i + AHEAD) / MD, (i + AHEAD) % MD);
+                if (i % MD == 0) {
 #pragma unroll
-                    for (int c = 0; c < NP; ++c) {
-                        pf[c][e] = (__bf16)r;
-                        r -= (float)pf[c][e];
+                    for (int e = 0; e < 8; ++e) {
+                        float r = x[8 * (i / MD) + e];
+#pragma unroll
+                        for (int c = 0; c < NP; ++c) {
+                            pf[c][e] = (__bf16)r;
+                            r -= (float)pf[c][e];
+                        }
                     }
                 }
 #pragma unroll
-                for (int md = 0; md < MD; ++md) {
-                    const bf16x8 vf = vread(k4, md);
-#pragma unroll
-                    for (int c = 0; c < NP; ++c) o[md] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[c], o[md], 0, 0, 0);
-                }
+                for (int c = 0; c < NP; ++c)
+                    o[i % MD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % (AHEAD + 1)], pf[c], o[i % MD], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
         };
-        const int t0 = pos - p.start[b] + wave;
-        if (t0 < min(t_end, nct)) load(t0);
-        for (int t = t0; t < min(t_end, nct); t += 8) {
+        // Pages of the wave's next 64 tiles, one per lane: a scalar load of each
+        // would stand in front of its tile's loads.
+        const int t0 = pos - p.start[b] + wave, tc_end = min(t_end, nct);
+        auto pages = [&](int t) -> int { return ptab[max(min(t + 8 * lane, tc_end - 1), 0)]; };
+        int pgs = t0 < tc_end ? pages(t0) : 0;
+        if (t0 < tc_end) load(__builtin_amdgcn_readlane(pgs, 0));
+        for (int t = t0, it = 1; t < tc_end; t += 8, ++it) {
+            // (cheap to derive from: not to be held in registers over the loop)
+            asm volatile("" : "+v"(vbase[0]), "+v"(vbase[1]), "+v"(wbase));
             const int left = n - t * KT4;   // keys of the tile (64 but in the last)
             f32x16 S[2];
 #pragma unroll
@@ -231,21 +251,24 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
             }
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int r = (64 * i + lane) / (D / 32), c0 = 4 * (lane % (D / 32));
 #pragma unroll
-                for (int f = 0; f < 4; ++f)
-                    *(u32x4 *)(vt + r * ROWB + 16 * ((c0 + f) ^ swz<D>(r))) = unpack4(vc[i][f], vs[i]);
+                for (int f = 0; f < 4; ++f) *(u32x4 *)(vt + i * VR * ROWB + (wbase ^ (16 * f))) = unpack4(vc[i][f], vs[i]);
             }
             __builtin_amdgcn_sched_barrier(0);
-            if (t + 8 < min(t_end, nct)) load(t + 8);
+            if ((it & 63) == 0 && t + 8 < tc_end) pgs = pages(t + 8);
+            if (t + 8 < tc_end) load(__builtin_amdgcn_readlane(pgs, it & 63));
             __builtin_amdgcn_sched_barrier(0);
             attend(S, std::integral_constant<int, 64>{});
         }
         if (t_end > nct && (nct - (pos - p.start[b])) % 8 == wave) {
             // the new block, in bf16 (rows past its end repeat the last)
             f32x16 S[2];
-            const int64_t kr = min(l32, nl - 1);
-            const uint16_t *k = a.kc + b * a.kc_sb + kr * a.kc_st + (int64_t)kvh * a.kc_sh + 32 * hf;
+            // (the lane is hidden from the optimiser here and below, so that what
+            // these parts derive from it is not held in registers over the loop)
+            int ln = lane;
+            asm volatile("" : "+v"(ln));
+            const int64_t kr = min(ln & 31, nl - 1);
+            const uint16_t *k = a.kc + b * a.kc_sb + kr * a.kc_st + (int64_t)kvh * a.kc_sh + 32 * (ln >> 5);
 #pragma unroll
             for (int v = 0; v < 16; ++v) S[0][v] = 0.f;
 #pragma unroll
@@ -255,10 +278,11 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
                     S[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)(k + 64 * s + 8 * f), qf[s][f], S[0], 0, 0, 0);
 #pragma unroll
             for (int v = 0; v < 16; ++v)
-                if (8 * (v >> 2) + 4 * hf + (v & 3) >= kend) S[0][v] = -INFINITY;
+                if (8 * (v >> 2) + 4 * (ln >> 5) + (v & 3) >= kend) S[0][v] = -INFINITY;
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < 32 / RPW; ++i) {
-                const int r = i * RPW + lane / LPR, c = lane % LPR;
+                const int r = i * RPW + ln / LPR, c = ln % LPR;
                 const uint16_t *v = a.vc + b * a.vc_sb + (int64_t)min(r, nl - 1) * a.vc_st + (int64_t)kvh * a.vc_sh;
                 *(u32x4 *)(vt + r * ROWB + 16 * (c ^ swz<D>(r))) = *(const u32x4 *)(v + 8 * c);
             }
@@ -319,13 +343,16 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
             }
         }
         // the new block's part commits it
-        if (a.fuse_append && t_end > nct)
-            for (int u = tid; u < nl * (D / 8); u += 512) {
+        if (a.fuse_append && t_end > nct) {
+            int th = tid;
+            asm volatile("" : "+v"(th));
+            for (int u = th; u < nl * (D / 8); u += 512) {
                 const int t = u / (D / 8), c = u % (D / 8), at4 = n + t;
                 uint8_t *g = a.pool4 + ((int64_t)ptab[at4 >> 6] * a.Hkv + kvh) * cache4_bytes(D);
                 store_block4<D>(g, at4 & 63, c, *(const u32x4 *)(a.kc + b * a.kc_sb + (int64_t)t * a.kc_st + (int64_t)kvh * a.kc_sh + 8 * c));
                 store_block4<D>(g + HALFB, at4 & 63, c, *(const u32x4 *)(a.vc + b * a.vc_sb + (int64_t)t * a.vc_st + (int64_t)kvh * a.vc_sh + 8 * c));
             }
+        }
         pos = p.start[b] + t_end;
         __syncthreads();   // (the next part's tiles overwrite the sums)
     }
