@@ -440,19 +440,27 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     }
     // first row that sees any of these keys (key ends do not decrease)
     const int32_t *kend_b = a.kend + (WIN ? 2 : 1) * (int64_t)b * a.L;
-    // window: first row past r0 whose window starts behind key k (L: none)
-    auto window_end = [&](int r0, int k) -> int {
+    // window: the first row at or past r0 whose entry of a non-decreasing array
+    // is past k (L: none), by 64 probes at a time (two loads up to 4096 rows; the
+    // four binary searches of a work-group took 50 of them one after the other)
+    auto first_past = [&](const int32_t *x, int r0, int k) -> int {
         int lo = r0, hi = a.L;
         while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (ld_uniform(kend_b, (int64_t)a.L + mid) > k) hi = mid; else lo = mid + 1;
+            const int step = (hi - lo + 63) / 64, i = lo + (lane + 1) * step - 1;
+            const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < hi && x[min(i, a.L - 1)] <= k));
+            hi = min(hi, lo + (n + 1) * step - 1);
+            lo = min(lo + n * step, hi);
         }
         return lo;
     };
     int lo = 0, hi = a.L - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (ld_uniform(kend_b, mid) > kw0) hi = mid; else lo = mid + 1;
+    if constexpr (WIN) {
+        lo = first_past(kend_b, 0, kw0);
+    } else {
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (ld_uniform(kend_b, mid) > kw0) hi = mid; else lo = mid + 1;
+        }
     }
     const int i0 = lo;
     // Chunks of 32 query rows counted from the sequence end, down to row i0,
@@ -463,7 +471,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     // none of these keys, so the masking zeroes their terms.
     // A split takes a contiguous share [first, total) of the chunks; group grp
     // takes chunks first + grp, first + grp + 2, ...
-    const int last = WIN && kw0 >= a.sinks ? window_end(i0, min(kw0 + 127, a.L - 1)) : a.L;   // end of those rows
+    const int last = WIN && kw0 >= a.sinks ? first_past(kend_b + a.L, i0, min(kw0 + 127, a.L - 1)) : a.L;   // end of those rows
     const int nch = (last - i0 + 31) / 32;
     const int first = (int)((int64_t)a.G * nch * split / nsplit);
     const int total = (int)((int64_t)a.G * nch * (split + 1) / nsplit);
@@ -475,6 +483,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     {
         const int kl = min(kw0 + 32 * sub + 31, a.L - 1);
         int mlo = i0, mhi = a.L;
+        if constexpr (WIN) mlo = mhi = first_past(kend_b, i0, kl);
         while (mlo < mhi) {
             const int mid = (mlo + mhi) >> 1;
             if (ld_uniform(kend_b, mid) > kl) mhi = mid; else mlo = mid + 1;
@@ -485,7 +494,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     int il = a.L;
     if constexpr (WIN) {
         const int k0 = max(kw0 + 32 * sub, a.sinks);
-        if (k0 < kw0 + 32 * sub + 32) il = window_end(i0, k0);
+        if (k0 < kw0 + 32 * sub + 32) il = first_past(kend_b + a.L, i0, k0);
     }
     // Q and dO rows of one chunk go straight to LDS: wave-wide load i of wave
     // `sub` fills rows 4 RPW i + RPW sub .. + RPW - 1 of the tile, from a
