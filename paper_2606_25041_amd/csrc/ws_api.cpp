@@ -599,9 +599,11 @@ size_t bwd_workspace(int batch, int hq, int hkv, int seq) {
 // dK/dV work-groups of a windowed launch: the key tiles of the sinks are seen by
 // every later row and the others by about `rows` rows each, so the sinks' tiles
 // are split into more parts; both kinds are where the items would leave the
-// chip idle.  The least modelled time (in steps of two chunks, as plan_bwd):
-// the longest part, or the mean load of a unit and 0.3 of the longest, plus the
-// cost of the partial sums.  max_parts: room for partial sums.
+// chip idle.  The least modelled time (in steps of two chunks, as plan_bwd): a
+// longest-first dispatch of the parts, plus the cost of the partial sums.  (The
+// parts of a kind are alike, so one round more counts in full: 12 units of 174
+// tokens, window 500, 8 KV heads, modelled by the mean load: 288 parts on 256
+// units, 123 us.)  max_parts: room for partial sums.
 struct BwdWindowPlan {
     int sink_tiles = 0, sink_parts = 1, tile_parts = 1, tiles = 0;
     int64_t parts() const {   // slots of partial sums (0: nothing is split)
@@ -629,16 +631,22 @@ BwdWindowPlan plan_bwd_window(int num_cus, int batch, int hq, int hkv, int seq, 
             if (at.parts() > max_parts) continue;
             const double s = sink_steps / sp + FIXED + (sp > 1 ? PART : 0), t = tile_steps / tp + FIXED + (tp > 1 ? PART : 0);
             const int64_t ns = p.sink_tiles * sp, nt = rest * tp;
-            const double longest = std::max(ns ? s : 0, nt ? t : 0), mean = (ns * s + nt * t) * ngrp / num_cus;
-            double cost = std::max(longest, mean + ((ns + nt) * ngrp > num_cus ? 0.3 * longest : 0));
+            ItemGroup parts[2] = {{(int)(10 * s), (int)std::min<int64_t>(ns * ngrp, INT32_MAX / 2)},
+                                  {(int)(10 * t), (int)std::min<int64_t>(nt * ngrp, INT32_MAX / 2)}};
+            if (parts[0].size < parts[1].size) std::swap(parts[0], parts[1]);
+            // (many rounds: their mean, which the dispatch would only count out)
+            const bool many = (ns + nt) * ngrp > 64 * (int64_t)num_cus;
+            double cost = many ? (ns * s + nt * t) * ngrp / num_cus + std::max(s, t)
+                        : dispatch_time(num_cus, parts[0].n ? parts : parts + 1, parts[0].n && parts[1].n ? 2 : 1) / 10.0;
+            cost += 0.05 * std::max(ns ? s : 0, nt ? t : 0);   // (an even end)
             if (at.parts()) cost += SUM + PART * ((sp > 1 ? ns : 0) + (tp > 1 ? nt : 0)) * ngrp / num_cus;
             if (tp == 1 && sp == 1) best = unsplit = cost;
-            if (cost < 0.97 * best) {
+            if (cost < 0.99 * best) {
                 best = cost;
                 p = at;
             }
         }
-    return best < 0.9 * unsplit ? p : whole;   // (a split has to win 10 %)
+    return best < 0.99 * unsplit ? p : whole;
 }
 
 // Rows that see an average key tile past the sinks: the rows of every 128 keys
@@ -946,9 +954,12 @@ size_t ws_prefill_window_bwd_workspace_bytes(int32_t batch, int32_t num_q_heads,
     if (batch <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads || seq_len <= 0 ||
         sinks < 0 || window < 0)
         return 0;
-    const BwdWindowPlan p = plan_bwd_window(CHIP_CUS, batch, num_q_heads, num_kv_heads, seq_len, Window{sinks, window},
-                                            std::min<int64_t>((int64_t)window + 128, seq_len), INT64_MAX);
-    return bwd_part_offset(batch, num_q_heads, seq_len, true) + p.parts() * bwd_part_bytes(batch, num_kv_heads);
+    // (blocks of one token to blocks of 768: the call knows which, and takes what fits)
+    int64_t parts = 0;
+    for (int64_t block = 0; block <= 768; block += 128)
+        parts = std::max(parts, plan_bwd_window(CHIP_CUS, batch, num_q_heads, num_kv_heads, seq_len, Window{sinks, window},
+                                                std::min<int64_t>((int64_t)window + 128 + block, seq_len), INT64_MAX).parts());
+    return bwd_part_offset(batch, num_q_heads, seq_len, true) + parts * bwd_part_bytes(batch, num_kv_heads);
 }
 
 }  // extern "C"
