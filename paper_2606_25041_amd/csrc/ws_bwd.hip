@@ -134,15 +134,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int k_hi = token_key_end(win, min(q0 + 127, a.L - 1), lane);
     const int kfull = token_key_end(win, q0, lane);
     const int my_kend = lane_key_end(win, min(q0 + 32 * wave, a.L - 1), rc, lane);
-    int my_klo = 0, lo_max = 0, nst = 0, gap = 0;
+    int my_klo = 0, nst = 0, gap = 0;
     if constexpr (WIN) {
         const int first = max(token_anchor(win, q0, lane) - a.window, 0) / 64;
-        lo_max = token_anchor(win, min(q0 + 127, a.L - 1), lane) - a.window;
         my_klo = lane_anchor(win, min(q0 + 32 * wave, a.L - 1), rc, lane) - a.window;
         nst = min((int)(((uint32_t)a.sinks + 63) / 64), first);
         gap = first - nst;
     }
     auto tile_of = [&](int u) -> int { return WIN && u >= nst ? u + gap : u; };
+    // this wave's first key end and last window start: masks where they cut
+    int w_full = kfull, w_last = 0;
+    if constexpr (WIN) {
+        w_full = __builtin_amdgcn_readlane(my_kend, 0);
+        w_last = __builtin_amdgcn_readlane(my_klo, 31);
+    }
     const float lse2 = a.lse[((int64_t)b * a.Hq + h) * a.L + rc] * 1.4426950408889634f;
     const float c2 = a.scale_log2;
 
@@ -256,12 +261,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         // some row's end only (a real branch: the compiler would otherwise
         // turn this rare path into selects executed on every tile)
         auto mask = [&](int h) {
-            if ((t + 1) * 64 > kfull || (WIN && t * 64 < lo_max && (t + 1) * 64 > a.sinks)) {
+            if ((t + 1) * 64 > w_full || (WIN && t * 64 < w_last && (t + 1) * 64 > a.sinks)) {
                 asm volatile("" ::: "memory");
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int key = t * 64 + h * 32 + 8 * (v >> 2) + 4 * hf + (v & 3);
-                    if (key >= my_kend || (WIN && key < my_klo && key >= a.sinks)) S[h][v] = 0.f;
+                    if ((key >= my_kend) | (WIN && ((key < my_klo) & (key >= a.sinks)))) S[h][v] = 0.f;
                 }
             }
         };

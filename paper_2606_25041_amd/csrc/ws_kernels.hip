@@ -342,23 +342,19 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         k_hi = token_key_end(win, q_last, lane);
         kfull = token_key_end(win, q0, lane);
     }
-    // window: the first and last row's klo, at least 0 (first <= own key < k_hi),
+    // window: the first row's klo, at least 0 (it is not past the row's own key),
     // the live tiles and their mapping
-    int lo_min = 0, lo_max = 0, nst = 0, gap = 0;
+    int lo_min = 0, nst = 0, gap = 0;
     if constexpr (WIN) {
         if (step) {
             const int t0 = (int)fastdiv((uint32_t)q0, fd_gq);
-            const int t1 = (int)fastdiv((uint32_t)(min(q0 + QT, (int)nrows) - 1), fd_gq);
             lo_min = n_pool + (t0 >= ts ? t0 : 0);
-            lo_max = n_pool + (t1 >= ts ? t1 : 0);
         } else {
             lo_min = token_anchor(win, q0, lane);
-            lo_max = token_anchor(win, min(q0 + QT, a.Lq) - 1, lane);
         }
-        lo_min = max(lo_min - a.window, 0);
-        lo_max = max(lo_max - a.window, 0);
+        lo_min = __builtin_amdgcn_readfirstlane(max(lo_min - a.window, 0));
         const int first = lo_min / KT;
-        nst = min((int)(((uint32_t)a.sinks + KT - 1) / KT), first);
+        nst = __builtin_amdgcn_readfirstlane(min((int)(((uint32_t)a.sinks + KT - 1) / KT), first));
         gap = first - nst;
     }
     auto tile_of = [&](int u) -> int { return WIN && u >= nst ? u + gap : u; };
@@ -402,6 +398,20 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         if constexpr (WIN && step) klo[n] = n_pool + (tok[n] >= ts ? tok[n] : 0) - a.window;
         else if constexpr (WIN)
             klo[n] = lane_anchor(win, min(q0 + rblk * 32 * NB + 32 * n, (int)nrows - 1), tok[n], lane) - a.window;
+    }
+
+    // Windows: a wave masks the tiles that an edge of its own rows cuts.  Of a
+    // 256-row tile's keys most are an edge of some row (2.8k tokens in blocks of 174,
+    // window 777: 11 of 20 tiles), of a wave's 32 rows two or three (that call 112
+    // -> 89 us).  From the key ends and window starts of the wave's first and last
+    // row, as live tiles u: [cut_lo, cut_hi), where the sinks end or a window starts,
+    // and those from cut_end on.  (Skipping the tiles that none of a wave's rows see
+    // too: 87 us there, but 2 % more where an item runs many tiles.)
+    int cut_lo = 0, cut_hi = 0, cut_end = 0;
+    if constexpr (WIN) {
+        cut_lo = a.sinks / KT;
+        cut_hi = (max(__builtin_amdgcn_readlane(klo[0], 31), 0) + KT - 1) / KT - gap;
+        cut_end = __builtin_amdgcn_readlane(kend[0], 0) / KT - gap;
     }
 
     // ---- direct-to-LDS tile loads -----------------------------------------
@@ -681,7 +691,8 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
                 for (int v = 0; v < 16; ++v) {
                     const int key = kt + mb * 32 + (v >> 2) * 8 + 4 * hf + (v & 3);
                     const int end = C4 && kt < n_new ? n_pool : kend[n];
-                    if (key >= end || (WIN && key < klo[n] && key >= a.sinks)) sc[n][mb][v] = -INFINITY;
+                    // (| and &: no branch per element)
+                    if ((key >= end) | (WIN && ((key < klo[n]) & (key >= a.sinks)))) sc[n][mb][v] = -INFINITY;
                 }
     };
     // Running max (log2 domain) from a tile's in-lane max, with lazy rescale:
@@ -766,8 +777,8 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     };
     // softmax of a tile: mask, running max, P weights and their sum
     auto softmax = [&](int t, Tile &sc, Weights &pf) {
-        const int kt = tile_of(t) * KT;
-        if (kt + KT > kfull || (WIN && kt < lo_max && kt + KT > a.sinks) || (C4 && kt < n_new && kt + KT > n_pool)) {
+        const int kt = t * KT;
+        if (WIN ? t >= cut_end || (t >= cut_lo && t < cut_hi) : kt + KT > kfull || (C4 && kt < n_new && kt + KT > n_pool)) {
             // (a real branch: the compiler would otherwise turn this rare
             // path into selects executed on every tile)
             asm volatile("" ::: "memory");
