@@ -88,9 +88,9 @@ int ws_kv_append_4bit(const ws_paged_kv4 *kv, int32_t batch, const int32_t *cach
                       int32_t new_len, ws_tensor4 k_new, ws_tensor4 v_new, void *stream) {
     if (!new_lens_host != !new_lens_dev) return fail(WS_ERR_NULL, "new_lens: give both copies or neither");
     if (int rc = check_paged4(kv)) return rc;
-    if (!cache_lens_host || !cache_lens_dev) return fail(WS_ERR_NULL, "cache_lens pointer is NULL");
     if (batch < 0 || new_len < 0) return fail(WS_ERR_SHAPE, "batch %d, new_len %d", (int)batch, (int)new_len);
     if (batch == 0 || new_len == 0) return ok();  // nothing is read or written
+    if (!cache_lens_host || !cache_lens_dev) return fail(WS_ERR_NULL, "cache_lens pointer is NULL");
     if (batch > 65535) return fail(WS_ERR_SHAPE, "batch %d exceeds 65535", (int)batch);
     if (int rc = check_tensor("k_new", k_new, false)) return rc;
     if (int rc = check_tensor("v_new", v_new, false)) return rc;
@@ -110,9 +110,9 @@ int ws_kv_append_4bit(const ws_paged_kv4 *kv, int32_t batch, const int32_t *cach
 int ws_kv_read_4bit(const ws_paged_kv4 *kv, int32_t batch, const int32_t *starts_host, const int32_t *starts_dev,
                     int32_t length, ws_tensor4 k, ws_tensor4 v, void *stream) {
     if (int rc = check_paged4(kv)) return rc;
-    if (!starts_host || !starts_dev) return fail(WS_ERR_NULL, "starts pointer is NULL");
     if (batch < 0 || length < 0) return fail(WS_ERR_SHAPE, "batch %d, length %d", (int)batch, (int)length);
     if (batch == 0 || length == 0) return ok();
+    if (!starts_host || !starts_dev) return fail(WS_ERR_NULL, "starts pointer is NULL");
     if (batch > 65535) return fail(WS_ERR_SHAPE, "batch %d exceeds 65535", (int)batch);
     if (int rc = check_tensor("k", k, false)) return rc;
     if (int rc = check_tensor("v", v, false)) return rc;
@@ -154,10 +154,10 @@ int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_n
     if (!nl_host != !nl_dev) return fail(WS_ERR_NULL, "new_lens: give both copies or neither");
     if (!text_host != !text_dev) return fail(WS_ERR_NULL, "text_starts: give both copies or neither");
     if (int rc = check_paged4(kv)) return rc;
-    if (!cache_lens_host || !cache_lens_dev) return fail(WS_ERR_NULL, "cache_lens pointer is NULL");
     if (batch < 0 || new_len < 0 || num_q_heads <= 0)
         return fail(WS_ERR_SHAPE, "batch %d, new_len %d, num_q_heads %d", (int)batch, (int)new_len, (int)num_q_heads);
     if (batch == 0 || new_len == 0) return ok();  // no query row: nothing is read or written
+    if (!cache_lens_host || !cache_lens_dev) return fail(WS_ERR_NULL, "cache_lens pointer is NULL");
     if (int rc = check_tensor("q", q, false)) return rc;
     if (int rc = check_kv_tensor("k_new", k_new)) return rc;
     if (int rc = check_kv_tensor("v_new", v_new)) return rc;

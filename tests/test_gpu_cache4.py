@@ -177,3 +177,23 @@ def test_step(case):
         assert torch.equal(out[b, :n], again[b, :n]) and torch.equal(lse[b, :, :n], lse2[b, :, :n]), b
         commit(want_pool, cache.page_table_host[b], D, c, kn[b, :n], vn[b, :n])
     assert _same_pool(cache.pool, want_pool)
+
+
+@pytest.mark.parametrize("Lq", (2, 40))
+def test_a_pool_past_4_gib(Lq):
+    gs.say(f"[gpu] 4-bit pool past 4 GiB, {Lq} new tokens")
+    pages, Hq, Hkv, D, n = 65000, 16, 8, 128, 1000
+    per = -(-(n + Lq) // 64)
+    table = torch.arange(pages - per, pages).flip(0)[None]
+    cache = ws.PagedCache4.allocate(pages, Hkv, D, table, device=DEV)
+    k, v = _randn(1, 1, n, Hkv, D), _randn(2, 1, n, Hkv, D)
+    ws.kv_append(cache, _pair([0]), k, v)
+    rk, rv = ws.kv_read(cache, _pair([0]), n)
+    assert torch.equal(rk, cache4_ref.rounded(k)) and torch.equal(rv, cache4_ref.rounded(v))
+    q, kn, vn = _randn(3, 1, Lq, Hq, D), _randn(4, 1, Lq, Hkv, D), _randn(5, 1, Lq, Hkv, D)
+    out = ws.block_causal_attn_fwd(q, kn, vn, cache, _pair([n]), fuse_append=True)
+    lo, hi = ref.step_ranges(n, Lq, None, 2 ** 31)
+    want = ref.attend(q[0], torch.cat((rk[0], kn[0])), torch.cat((rv[0], vn[0])), lo, hi, 0, D ** -0.5)
+    ref.check("out", out[0], want["out"])
+    gk, _ = ws.kv_read(cache, _pair([n]), Lq)
+    assert torch.equal(gk, cache4_ref.rounded(kn))

@@ -224,3 +224,60 @@ def test_gradients(case, room):
         for name, x in zip(("dq", "dk", "dv"), got):
             assert x.dtype == (torch.bfloat16 if bf16 else torch.float32)
             ref.check(f"{name} {b}", x[b], want[name], bf16=bf16)
+
+
+def test_a_billion_tokens_behind_the_window():
+    """A session of 2^30 + 77 tokens of which the sinks and the window are left,
+    in the last pages of a pool past 4 GiB."""
+    gs.say("[gpu] window step at position 2^30")
+    n, window, sinks, Hq, Hkv, D, Lq, pages = 2 ** 30 + 77, 1000, 70, 8, 8, 128, 5, 40000
+    live = [(0, min(sinks, 64)), (64, sinks)] + [(p, min(p + 64, n)) for p in range((n - window) // 64 * 64, n, 64)]
+    table = torch.full((1, (n + Lq + 63) // 64), -1, dtype=torch.int32)
+    k_pool = torch.empty(pages, Hkv, 64, D, dtype=torch.bfloat16, device=DEV)
+    v_pool = torch.empty_like(k_pool)
+    ks, vs, at = [], [], []
+    for i, (s, e) in enumerate(live):
+        page = pages - 1 - i
+        table[0, s // 64] = page
+        k_pool[page], v_pool[page] = float("nan"), float("nan")
+        lo = max(s, 0 if s < sinks else n - window)
+        k, v = _randn(2 * i, e - lo, Hkv, D), _randn(2 * i + 1, e - lo, Hkv, D)
+        k_pool[page, :, lo - s:e - s], v_pool[page, :, lo - s:e - s] = k.transpose(0, 1), v.transpose(0, 1)
+        ks.append(k), vs.append(v), at.extend(range(lo, e))
+    q, kn, vn = _randn(91, 1, Lq, Hq, D), _randn(92, 1, Lq, Hkv, D), _randn(93, 1, Lq, Hkv, D)
+    cache = ws.PagedCache(k_pool, v_pool, table)
+    out, lse = ws.block_causal_attn_fwd(q, kn, vn, cache, _pair([n]), text_starts=_pair([2]), window=window, sinks=sinks,
+                                        want_lse=True)
+    torch.cuda.synchronize()
+    # the same with the gap left out: positions behind it move down
+    lo, hi = ref.step_ranges(n, Lq, 2, window)
+    gap = n - window - sinks
+    assert at == list(range(sinks)) + list(range(n - window, n))
+    want = ref.attend(q[0], torch.cat(ks + [kn[0]]), torch.cat(vs + [vn[0]]), lo - gap, hi - gap, sinks, D ** -0.5)
+    ref.check("out", out[0], want["out"])
+    ref.check("lse", lse[0], want["lse"])
+
+
+@pytest.mark.parametrize("mistake", ("window + 1", "window - 1", "sinks + 1", "sinks - 1", "block anchor", "none"))
+def test_the_bounds_catch_a_shifted_window(mistake):
+    """The reference with a planted mistake does not pass (and without one it
+    does): one key more or less, or a token-causal token's window counted from
+    its block."""
+    B, L, H, D, window, sinks = 1, 200, 1, 64, 20, 5
+    q, k, v = _randn(1, B, L, H, D), _randn(2, B, L, H, D), _randn(3, B, L, H, D)
+    off, starts = [0, 60, 130, L], [40, 130, 150]
+    out, lse = ws.block_causal_prefill(q, k, v, _pair([off]), text_starts=_pair([starts]), window=window, sinks=sinks,
+                                       want_lse=True, out_dtype=torch.float32)
+    lo, hi = ref.ranges(off, starts, window)
+    if mistake == "block anchor":
+        lo = ref.ranges(off, None, window)[0]
+    lo = lo - {"window + 1": 1, "window - 1": -1}.get(mistake, 0)
+    s = sinks + {"sinks + 1": 1, "sinks - 1": -1}.get(mistake, 0)
+    want = ref.attend(q[0], k[0], v[0], lo, hi, s, D ** -0.5, f32=True)
+    wrong = []
+    for name, got in (("out", out[0]), ("lse", lse[0])):
+        try:
+            ref.check(name, got, want[name])
+        except AssertionError:
+            wrong.append(name)
+    assert wrong == ([] if mistake == "none" else ["out", "lse"])
