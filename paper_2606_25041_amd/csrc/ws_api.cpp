@@ -375,14 +375,15 @@ int64_t window_keys(const Window &w, int batch, int new_len, const int32_t *cach
 // the same; a stream with one split writes its output itself and needs none.
 // slot_bytes: output values of one partial slot.
 bool plan_ragged(ws::RaggedPlan &r, int num_cus, const StepPlan &uni, int batch, int hq, int hkv, int lq,
-                 const int32_t *cache_lens, const int32_t *nl, const int32_t *text, int64_t slot_bytes) {
+                 const int32_t *cache_lens, const int32_t *nl, const int32_t *text, int64_t slot_bytes, bool whole_tiles) {
     if (batch < 2 || batch > ws::LENS_IN_ARGS || split_override()) return false;
     const int64_t qt = uni.shape.qtile(), G = hq / hkv;
     struct Stream { int tiles, q, b; } st[ws::LENS_IN_ARGS];
     bool differ = false;
     for (int b = 0; b < batch; ++b) {
         const int n = nl ? nl[b] : lq;
-        st[b] = {(int)(((int64_t)cache_lens[b] + n + 63) / 64), (int)((G * n + qt - 1) / qt), b};
+        const int64_t tiles = whole_tiles ? ((int64_t)cache_lens[b] + 63) / 64 + (n + 63) / 64 : ((int64_t)cache_lens[b] + n + 63) / 64;
+        st[b] = {(int)tiles, (int)((G * n + qt - 1) / qt), b};
         differ = differ || st[b].tiles != st[0].tiles || st[b].q != st[0].q;
     }
     if (!differ) return false;
@@ -486,6 +487,13 @@ bool plan_ragged(ws::RaggedPlan &r, int num_cus, const StepPlan &uni, int batch,
     r.per_class = (r.n_items + r.deal - 1) / r.deal;
     r.fd_class = ws::fastdiv_make((uint32_t)r.per_class);
     return true;
+}
+
+void ragged_work(AttnArgs &a, const RaggedPlan &r) {
+    a.per_group = r.deal * r.per_class;
+    a.fd_group = ws::fastdiv_make((uint32_t)a.per_group);
+    a.n_work = a.Hkv * a.per_group;
+    a.per_xcd = (a.n_work + ws::NUM_XCD - 1) / ws::NUM_XCD;
 }
 
 // Partials are kept in blocks of 32 packed rows per (stream, KV head).
@@ -1250,13 +1258,8 @@ int step_impl(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new, const ws_paged_k
     ws::RaggedPlan rag;
     const int64_t slot_bytes = (int64_t)a.Hkv * a.nrb * 32 * kv->head_dim * (a.out_f32 ? 4 : 2);
     const bool ragged = !win && plan_ragged(rag, cus, plan, batch, num_q_heads, kv->num_kv_heads, new_len, cache_lens_host,
-                                    nl_host, text_host, slot_bytes);
-    if (ragged) {
-        a.per_group = rag.deal * rag.per_class;
-        a.fd_group = ws::fastdiv_make((uint32_t)a.per_group);
-        a.n_work = a.Hkv * a.per_group;
-        a.per_xcd = (a.n_work + ws::NUM_XCD - 1) / ws::NUM_XCD;
-    }
+                                    nl_host, text_host, slot_bytes, false);
+    if (ragged) ragged_work(a, rag);
     if (int e = ws::launch_attention(a, ragged ? &rag : nullptr, kv->head_dim, plan.shape, stream))
         return fail(WS_ERR_HIP, "attention launch failed (hip error %d)", e);
     if ((ragged ? rag.max_nsplit : plan.nsplit) > 1)

@@ -53,27 +53,36 @@ int64_t tile_keys(int batch, int new_len, const int32_t *cache_lens, const int32
 
 // A step of few packed rows: tiles in one line per KV head, an even share for
 // each work-group, one work-group per compute unit (its LDS tiles allow one);
-// a share is at least a tile per wave.
+// a share is at least a tile per wave.  Every 32 rows read the cache again
+// (mostly from an XCD's L2) and unpack it, where the common kernel's 256 rows share
+// one reading, so the common kernel is the faster from about 200 rows on (4 x
+// 131072 tokens, GQA 64/8 x 128: 40 rows 202 us against 393, 64 rows 209 and 395,
+// 96 rows 294 and 403, 128 rows 367 and 411, 256 rows 676 and 587; one stream of
+// 4096: 256 rows 20 and 24).
 bool few_rows(int batch, int G, int new_len) { return batch <= LENS_IN_ARGS && (int64_t)G * new_len <= FEW_ROWS; }
 
-Few4Plan plan_few(int num_cus, int batch, int hkv, int new_len, const int32_t *cache_lens, const int32_t *nl) {
+Few4Plan plan_few(int num_cus, int batch, int hkv, int G, int new_len, const int32_t *cache_lens, const int32_t *nl) {
     Few4Plan p{};
+    p.nrb = (G * new_len + 31) / 32;
     int64_t at = 0;
     for (int b = 0; b < batch; ++b) {
         p.start[b] = (int32_t)at;
-        at += ((int64_t)cache_lens[b] + 63) / 64 + ((nl ? nl[b] : new_len) + 63) / 64;
+        at += ((int64_t)cache_lens[b] + 63) / 64 + ((nl ? nl[b] : new_len) + 31) / 32;
     }
     p.start[batch] = (int32_t)at;   // (at most 32 streams of 2^25 tiles)
-    const int64_t most = std::max(1, num_cus / hkv);
+    const int64_t most = std::max(1, num_cus / (hkv * p.nrb));
     p.per = (int32_t)std::max<int64_t>((at + most - 1) / most, 8);
     p.nwg = (int32_t)((at + p.per - 1) / p.per);
     p.fd_per = fastdiv_make((uint32_t)p.per);
+    p.fd_hkv = fastdiv_make((uint32_t)hkv);
+    p.fd_nrb = fastdiv_make((uint32_t)p.nrb);
     return p;
 }
 
-// Partials: a part of 32 rows x D and the rows' (m, l), f32, per KV head.
+// Partials: a part of 32 rows x D and the rows' (m, l), f32, per KV head and row
+// block.
 size_t few_workspace(const Few4Plan &p, int batch, int hkv, int d) {
-    return p.nwg <= 1 ? 0 : (size_t)(p.nwg + batch) * hkv * 32 * (d + 2) * sizeof(float);
+    return p.nwg <= 1 ? 0 : (size_t)(p.nwg + batch) * hkv * p.nrb * 32 * (d + 2) * sizeof(float);
 }
 
 }  // namespace
@@ -138,8 +147,8 @@ size_t ws_step_workspace_bytes_4bit(int32_t batch, int32_t num_q_heads, int32_t 
     int cus = 0;
     if (current_device_cus(&cus)) return 0;
     if (few_rows(batch, num_q_heads / num_kv_heads, new_len))
-        return few_workspace(plan_few(cus, batch, num_kv_heads, new_len, cache_lens_host, new_lens_host), batch,
-                             num_kv_heads, 128);
+        return few_workspace(plan_few(cus, batch, num_kv_heads, num_q_heads / num_kv_heads, new_len, cache_lens_host,
+                                      new_lens_host), batch, num_kv_heads, 128);
     const StepPlan p = plan_step(cus, batch, num_q_heads, num_kv_heads, new_len,
                                  tile_keys(batch, new_len, cache_lens_host, new_lens_host), new_lens_host);
     return step_workspace(p, batch, num_q_heads, num_kv_heads, new_len);
@@ -190,7 +199,7 @@ int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_n
     StepPlan plan{};
     size_t need;
     if (few) {
-        line = plan_few(cus, batch, kv->num_kv_heads, new_len, cache_lens_host, nl_host);
+        line = plan_few(cus, batch, kv->num_kv_heads, G, new_len, cache_lens_host, nl_host);
         need = few_workspace(line, batch, kv->num_kv_heads, 128);
     } else {
         plan = plan_step(cus, batch, num_q_heads, kv->num_kv_heads, new_len,
@@ -223,7 +232,7 @@ int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_n
     a.nqt = plan.nqt;
     if (few) {
         a.part_o = (float *)workspace;
-        a.part_ml = a.part_o + (size_t)(line.nwg + batch) * a.Hkv * 32 * kv->head_dim;
+        a.part_ml = a.part_o + (size_t)(line.nwg + batch) * a.Hkv * line.nrb * 32 * kv->head_dim;
     } else if (plan.nsplit > 1) {
         a.part_o = (float *)workspace;
         a.part_ml = a.part_o + (size_t)plan.nsplit * batch * a.Hkv * a.nrb * 32 * kv->head_dim;
@@ -250,10 +259,16 @@ int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_n
         return ok();
     }
     if (!finish_work(a)) return fail(WS_ERR_SHAPE, "too many work items");
-    if (int e = launch_attention(a, nullptr, kv->head_dim, plan.shape, stream))
+    // streams of different lengths: per-stream splits
+    RaggedPlan rag;
+    const int64_t slot_bytes = (int64_t)a.Hkv * a.nrb * 32 * kv->head_dim * (a.out_f32 ? 4 : 2);
+    const bool ragged = plan_ragged(rag, cus, plan, batch, num_q_heads, kv->num_kv_heads, new_len, cache_lens_host,
+                                    nl_host, text_host, slot_bytes, true);
+    if (ragged) ragged_work(a, rag);
+    if (int e = launch_attention(a, ragged ? &rag : nullptr, kv->head_dim, plan.shape, stream))
         return fail(WS_ERR_HIP, "attention launch failed (hip error %d)", e);
-    if (plan.nsplit > 1)
-        if (int e = launch_combine(a, nullptr, kv->head_dim, stream))
+    if ((ragged ? rag.max_nsplit : plan.nsplit) > 1)
+        if (int e = launch_combine(a, ragged ? &rag : nullptr, kv->head_dim, stream))
             return fail(WS_ERR_HIP, "combine launch failed (hip error %d)", e);
     return ok();
 }

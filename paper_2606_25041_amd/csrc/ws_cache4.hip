@@ -54,10 +54,11 @@ int launch_cache4(const Cache4Args &a, hipStream_t st) {
     return (int)hipGetLastError();
 }
 
-// Steps of at most 32 packed rows (a thinker's decode steps) over a 4-bit cache.
+// Steps of few packed rows (a thinker's decode steps) over a 4-bit cache.
 //
-// One work-group = an even share of a KV head's line of tiles (Few4Plan), its 8
-// waves each a tile of 64 keys in turn, with no barrier between them:
+// One work-group = 32 rows and an even share of a KV head's line of tiles
+// (Few4Plan), its 8 waves each a tile of 64 keys in turn, with no barrier between
+// them:
 //  * K codes come from global memory straight into the A operand's registers: a
 //    lane holds key l % 32 and, for dims 64 s + 32 (l / 32) + [0, 32), one 16-byte
 //    load and one scale.  Unpacked to bf16 they are four fragments of S^T = K Q^T;
@@ -82,7 +83,11 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
     constexpr float RESCALE = 8.f;        // lazy rescale (log2 units)
     __shared__ __attribute__((aligned(1024))) char smem[8 * TILEB];
     __shared__ float2 sml[8][32];
-    const int kvh = (int)(blockIdx.x % (uint32_t)a.Hkv), w = (int)(blockIdx.x / (uint32_t)a.Hkv);
+    // (row blocks of the same tiles next to each other: with a multiple of 8 KV
+    // heads they share an XCD's L2)
+    const uint32_t wr = fastdiv(blockIdx.x, p.fd_hkv);
+    const int kvh = (int)(blockIdx.x - wr * (uint32_t)a.Hkv);
+    const int w = (int)fastdiv(wr, p.fd_nrb), rb = (int)wr - w * p.nrb;
     const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     char *vt = smem + wave * TILEB;
@@ -117,7 +122,7 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
         const int n = a.lens_arg[b], nl = a.nl_arg[b], ts = a.text_arg[b];
         const int nct = (n + KT4 - 1) / KT4;
         const int32_t *ptab = a.page_table + (int64_t)b * a.max_pages;
-        const int row = min(l32, a.nrows - 1);
+        const int row = min(32 * rb + l32, a.nrows - 1);
         const int tok = (int)fastdiv((uint32_t)row, a.fd_gq), hq = kvh * a.G + (row - tok * a.G);
         const int kend = min(nl, max(ts, tok + 1));   // of the new block
         // Q fragments: dims 64 s + 32 hf + 8 f + [0, 8)
@@ -260,14 +265,16 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
             __builtin_amdgcn_sched_barrier(0);
             attend(S, std::integral_constant<int, 64>{});
         }
-        if (t_end > nct && (nct - (pos - p.start[b])) % 8 == wave) {
-            // the new block, in bf16 (rows past its end repeat the last)
+        // the new block's tokens [nt, nt + 32), in bf16 (rows past its end repeat
+        // the last)
+        for (int t = t0 < nct ? t0 + (nct - t0 + 7) / 8 * 8 : t0; t < t_end; t += 8) {
+            const int nt = 32 * (t - nct);
             f32x16 S[2];
             // (the lane is hidden from the optimiser here and below, so that what
             // these parts derive from it is not held in registers over the loop)
             int ln = lane;
             asm volatile("" : "+v"(ln));
-            const int64_t kr = min(ln & 31, nl - 1);
+            const int64_t kr = min(nt + (ln & 31), nl - 1);
             const uint16_t *k = a.kc + b * a.kc_sb + kr * a.kc_st + (int64_t)kvh * a.kc_sh + 32 * (ln >> 5);
 #pragma unroll
             for (int v = 0; v < 16; ++v) S[0][v] = 0.f;
@@ -278,12 +285,12 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
                     S[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)(k + 64 * s + 8 * f), qf[s][f], S[0], 0, 0, 0);
 #pragma unroll
             for (int v = 0; v < 16; ++v)
-                if (8 * (v >> 2) + 4 * (ln >> 5) + (v & 3) >= kend) S[0][v] = -INFINITY;
+                if (nt + 8 * (v >> 2) + 4 * (ln >> 5) + (v & 3) >= kend) S[0][v] = -INFINITY;
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < 32 / RPW; ++i) {
                 const int r = i * RPW + ln / LPR, c = ln % LPR;
-                const uint16_t *v = a.vc + b * a.vc_sb + (int64_t)min(r, nl - 1) * a.vc_st + (int64_t)kvh * a.vc_sh;
+                const uint16_t *v = a.vc + b * a.vc_sb + (int64_t)min(nt + r, nl - 1) * a.vc_st + (int64_t)kvh * a.vc_sh;
                 *(u32x4 *)(vt + r * ROWB + 16 * (c ^ swz<D>(r))) = *(const u32x4 *)(v + 8 * c);
             }
             attend(S, std::integral_constant<int, 32>{});
@@ -315,8 +322,8 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
             L += x.y == 0.f ? 0.f : x.y * fast_exp2(x.x - M);
         }
         const bool whole = p.start[b + 1] - p.start[b] == t_end - (pos - p.start[b]);   // the stream's only part
-        const int64_t at = (int64_t)(w + b) * a.Hkv + kvh;
-        if (l32 < a.nrows && tok < nl) {
+        const int64_t at = ((int64_t)(w + b) * a.Hkv + kvh) * p.nrb + rb;
+        if (32 * rb + l32 < a.nrows && tok < nl) {
 #pragma unroll
             for (int mg = wave; mg < 4 * MD; mg += 8) {
                 f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -342,12 +349,13 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
                 else if (a.lse) a.lse[((int64_t)b * a.Hq + hq) * a.Lq + tok] = (M + __builtin_amdgcn_logf(L)) * 0.69314718055994531f;
             }
         }
-        // the new block's part commits it
-        if (a.fuse_append && t_end > nct) {
+        // the parts of the new block commit their tokens
+        if (a.fuse_append && rb == 0 && t_end > nct) {
+            const int from = 32 * max(pos - p.start[b] - nct, 0), count = min(32 * (t_end - nct), nl) - from;
             int th = tid;
             asm volatile("" : "+v"(th));
-            for (int u = th; u < nl * (D / 8); u += 512) {
-                const int t = u / (D / 8), c = u % (D / 8), at4 = n + t;
+            for (int u = th; u < count * (D / 8); u += 512) {
+                const int t = from + u / (D / 8), c = u % (D / 8), at4 = n + t;
                 uint8_t *g = a.pool4 + ((int64_t)ptab[at4 >> 6] * a.Hkv + kvh) * cache4_bytes(D);
                 store_block4<D>(g, at4 & 63, c, *(const u32x4 *)(a.kc + b * a.kc_sb + (int64_t)t * a.kc_st + (int64_t)kvh * a.kc_sh + 8 * c));
                 store_block4<D>(g + HALFB, at4 & 63, c, *(const u32x4 *)(a.vc + b * a.vc_sb + (int64_t)t * a.vc_st + (int64_t)kvh * a.vc_sh + 8 * c));
@@ -364,18 +372,19 @@ __global__ __launch_bounds__(512) void few4_kernel(const AttnArgs a, const Few4P
 // taken eight at a time, their loads in flight together.
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void few4_merge_kernel(const AttnArgs a, const Few4Plan p) {
-    constexpr int PER = D / 32;   // work-groups per (stream, KV head)
+    constexpr int PER = D / 32;   // work-groups per (stream, KV head, row block)
     const int item = (int)(blockIdx.x % PER) * 256 + threadIdx.x;
-    const int bh = blockIdx.x / PER, b = bh / a.Hkv, kvh = bh - b * a.Hkv;
-    const int lane = item & 63, mg = item >> 6, row = lane & 31;
+    const uint32_t br = blockIdx.x / PER, bh = fastdiv(br, p.fd_nrb);
+    const int rb = (int)(br - bh * (uint32_t)p.nrb), b = (int)fastdiv(bh, p.fd_hkv), kvh = (int)bh - b * a.Hkv;
+    const int lane = item & 63, mg = item >> 6, row = 32 * rb + (lane & 31);
     if (row >= a.nrows) return;
     const int tok = (int)fastdiv((uint32_t)row, a.fd_gq), hq = kvh * a.G + (row - tok * a.G);
     if (tok >= a.nl_arg[b]) return;
     const int first = (int)fastdiv((uint32_t)p.start[b], p.fd_per), last = (int)fastdiv((uint32_t)p.start[b + 1] - 1, p.fd_per);
     if (first == last) return;   // written whole
-    const int64_t at = (int64_t)(first + b) * a.Hkv + kvh;
+    const int64_t at = ((int64_t)(first + b) * a.Hkv + kvh) * p.nrb + rb, step = (int64_t)a.Hkv * p.nrb;
     const float *po = a.part_o + at * (32 * D) + item * 4;
-    const float2 *pm = (const float2 *)a.part_ml + at * 32 + row;
+    const float2 *pm = (const float2 *)a.part_ml + at * 32 + (lane & 31);
     const int ns = last - first + 1;
     float M = -INFINITY, L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -385,8 +394,8 @@ __global__ __launch_bounds__(256) void few4_merge_kernel(const AttnArgs a, const
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int s = min(s0 + i, ns - 1);
-            ml[i] = pm[(int64_t)s * a.Hkv * 32];
-            x[i] = *(const f32x4 *)(po + (int64_t)s * a.Hkv * (32 * D));
+            ml[i] = pm[s * step * 32];
+            x[i] = *(const f32x4 *)(po + s * step * (32 * D));
         }
         float top = M;
 #pragma unroll
@@ -418,12 +427,12 @@ __global__ __launch_bounds__(256) void few4_merge_kernel(const AttnArgs a, const
 
 template <int D, bool F32>
 int launch_few4_t(const AttnArgs &a, const Few4Plan &p, hipStream_t st) {
-    hipLaunchKernelGGL((few4_kernel<D, F32>), dim3((unsigned)(a.Hkv * p.nwg)), dim3(512), 0, st, a, p);
+    hipLaunchKernelGGL((few4_kernel<D, F32>), dim3((unsigned)(a.Hkv * p.nrb * p.nwg)), dim3(512), 0, st, a, p);
     if (int e = (int)hipGetLastError()) return e;
     bool parts = false;
     for (int b = 0; b < a.B; ++b) parts = parts || p.start[b] / p.per != (p.start[b + 1] - 1) / p.per;
     if (parts)
-        hipLaunchKernelGGL((few4_merge_kernel<D, F32>), dim3((unsigned)(a.B * a.Hkv * (D / 32))), dim3(256), 0, st, a, p);
+        hipLaunchKernelGGL((few4_merge_kernel<D, F32>), dim3((unsigned)(a.B * a.Hkv * p.nrb * (D / 32))), dim3(256), 0, st, a, p);
     return (int)hipGetLastError();
 }
 

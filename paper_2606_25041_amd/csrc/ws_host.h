@@ -40,6 +40,13 @@ StepPlan plan_step(int num_cus, int batch, int hq, int hkv, int lq, int64_t max_
 size_t step_workspace(const StepPlan &p, int batch, int hq, int hkv, int lq);
 // Tuning override of the split count (0: none).
 int split_override();
+// Splits of a step over streams of different lengths, each with a count of its
+// own, within uni's partial slots (slot_bytes: output values of one); false: one
+// count is as good.  whole_tiles: a stream's cache and new block share no tile.
+bool plan_ragged(RaggedPlan &r, int num_cus, const StepPlan &uni, int batch, int hq, int hkv, int lq,
+                 const int32_t *cache_lens, const int32_t *nl, const int32_t *text, int64_t slot_bytes, bool whole_tiles);
+// Work items of a step as that plan counts them.
+void ragged_work(AttnArgs &a, const RaggedPlan &r);
 // Work items and dividers of a launch; false when it would not fit.
 bool finish_work(AttnArgs &a);
 

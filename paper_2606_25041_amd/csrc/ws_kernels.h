@@ -185,16 +185,19 @@ struct Cache4Args {
     int32_t B, Ln, Hkv, D;
 };
 
-// A step of at most FEW_ROWS packed rows per (stream, KV head) over a 4-bit
-// cache (beside the AttnArgs).  The tiles of all streams, each a cache page or
-// the new block behind them, stand in one line; work-group w of a KV head takes
-// tiles [w * per, (w + 1) * per) of it, so that all read the same amount whatever
-// the streams' lengths.  The part of a work-group in a stream has the partial
-// slot w + stream (both grow along the line, one of them at every part).
-constexpr int FEW_ROWS = 32;
+// A step of few packed rows per (stream, KV head) over a 4-bit cache (beside the
+// AttnArgs), in blocks of 32 rows.  The tiles of all streams, each a cache page
+// or 32 tokens of the new block behind them, stand in one line; work-group w of
+// a KV head and row block takes tiles [w * per, (w + 1) * per) of it, so that all
+// read the same amount whatever the streams' lengths.  The part of a work-group
+// in a stream has the partial slot w + stream (both grow along the line, one of
+// them at every part).
+constexpr int FEW_ROWS = 128;          // at most this many
 struct Few4Plan {
     int32_t per;                       // tiles of a work-group
-    int32_t nwg;                       // work-groups of a KV head
+    int32_t nwg;                       // work-groups of a KV head and row block
+    int32_t nrb;                       // row blocks
+    FastDiv fd_hkv, fd_nrb;
     FastDiv fd_per;                    // divider by per
     int32_t start[LENS_IN_ARGS + 1];   // first tile of each stream, and the end
 };

@@ -120,11 +120,13 @@ __device__ __forceinline__ void append_share4(const AttnArgs &a, int b, int kvh,
 // the others' code through the instruction cache, where short launches spend
 // their time.  Prefill of 2 x 16384 tokens 3.93 -> 3.76 ms; its loop still reads
 // five spilled scalars back per tile.
-enum Kind { PREFILL_CONTIGUOUS, PREFILL_PAGED, STEP, STEP_SPLIT, STEP_RAGGED, STEP_CACHE4 };
+enum Kind { PREFILL_CONTIGUOUS, PREFILL_PAGED, STEP, STEP_SPLIT, STEP_RAGGED, STEP_CACHE4, STEP_CACHE4_RAGGED };
 
 // STEP_SPLIT: every item writes partials, none rows of the output.
 // STEP_RAGGED: the streams have their own split counts (rp).
-// STEP_CACHE4: the cache is held in 4 bits (ws_cache4.h).
+// STEP_CACHE4(_RAGGED): the cache is held in 4 bits (ws_cache4.h).
+constexpr bool is_ragged(int kind) { return kind == STEP_RAGGED || kind == STEP_CACHE4_RAGGED; }
+constexpr bool is_cache4(int kind) { return kind == STEP_CACHE4 || kind == STEP_CACHE4_RAGGED; }
 struct NoPlan {};
 template <bool RAGGED>
 using Plan = std::conditional_t<RAGGED, RaggedPlan, NoPlan>;
@@ -150,10 +152,10 @@ using Plan = std::conditional_t<RAGGED, RaggedPlan, NoPlan>;
 // rounding (output off by 2.3e-3 of its norm instead of 2.9e-3; the last
 // rounding alone makes 1.7e-3).
 template <int D, int NW, int NB, int KIND, bool F32, int KG, bool WIN = false>
-__global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const Plan<KIND == STEP_RAGGED> rp) {
-    constexpr bool step = KIND == STEP || KIND == STEP_SPLIT || KIND == STEP_RAGGED || KIND == STEP_CACHE4;
-    constexpr bool C4 = KIND == STEP_CACHE4;
-    constexpr bool RAGGED = KIND == STEP_RAGGED;
+__global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const Plan<is_ragged(KIND)> rp) {
+    constexpr bool C4 = is_cache4(KIND);
+    constexpr bool step = KIND == STEP || KIND == STEP_SPLIT || KIND == STEP_RAGGED || C4;
+    constexpr bool RAGGED = is_ragged(KIND);
     static_assert(!WIN || (!RAGGED && KIND != STEP_SPLIT && !C4), "windows: one split count, one step instance");
     constexpr bool P3 = (WIN || C4) && F32;
     constexpr bool HALF = (WIN || C4) && !F32;
@@ -1422,7 +1424,7 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {
 }
 
 template <int D, int KIND, int KG, bool WIN = false>
-int launch_attn_t(const AttnArgs &a, const Plan<KIND == STEP_RAGGED> &rp, hipStream_t st) {
+int launch_attn_t(const AttnArgs &a, const Plan<is_ragged(KIND)> &rp, hipStream_t st) {
     const dim3 grid(a.per_xcd * NUM_XCD), block(8 * 64);
     if (a.out_f32)
         hipLaunchKernelGGL((attn_kernel<D, 8, 1, KIND, true, KG, WIN>), grid, block, 0, st, a, rp);
@@ -1443,7 +1445,8 @@ int launch_attn_d(const AttnArgs &a, const RaggedPlan *rag, TileShape shape, hip
         return a.mode == MODE_STEP ? launch_attn_t<D, STEP, 1, true>(a, NoPlan{}, st)
              : a.paged ? launch_prefill_t<D, PREFILL_PAGED, true>(a, shape.kg, st)
                        : launch_prefill_t<D, PREFILL_CONTIGUOUS, true>(a, shape.kg, st);
-    if (a.pool4) return launch_attn_t<D, STEP_CACHE4, 1>(a, NoPlan{}, st);
+    if (a.pool4)
+        return rag ? launch_attn_t<D, STEP_CACHE4_RAGGED, 1>(a, *rag, st) : launch_attn_t<D, STEP_CACHE4, 1>(a, NoPlan{}, st);
     return rag ? launch_attn_t<D, STEP_RAGGED, 1>(a, *rag, st)
          : a.mode == MODE_STEP ? shape.parts_only ? launch_attn_t<D, STEP_SPLIT, 1>(a, NoPlan{}, st)
                                                   : launch_attn_t<D, STEP, 1>(a, NoPlan{}, st)
@@ -1480,6 +1483,9 @@ int launch_combine_t(const AttnArgs &a, const Plan<RAGGED> &rp, int nsplit, hipS
 
 template <int D>
 int launch_combine_d(const AttnArgs &a, const RaggedPlan *rag, hipStream_t st) {
+    if (a.pool4 && rag)
+        return a.has_new_lens ? launch_combine_t<D, true, true, true>(a, *rag, rag->max_nsplit, st)
+                              : launch_combine_t<D, false, true, true>(a, *rag, rag->max_nsplit, st);
     if (a.has_window || a.pool4)
         return a.has_new_lens ? launch_combine_t<D, true, false, true>(a, NoPlan{}, a.nsplit, st)
                               : launch_combine_t<D, false, false, true>(a, NoPlan{}, a.nsplit, st);

@@ -123,8 +123,10 @@ int probe_step4(int batch, int hq, int hkv, int d, int new_len, const int32_t *l
             const int first = start[b] / *per, last = (start[b + 1] - 1) / *per;
             if (first != last) slots = last + b + 1;
         }
-        if (slots) *used = ((char *)a.part_ml - g_mem) + slots * hkv * 32 * 2 * 4;
-        if (slots && (char *)a.part_o + slots * hkv * 32 * d * 4 > (char *)a.part_ml) return -1;   // rows behind the sums
+        const int nrb = g_seen.few.nrb;
+        if (nrb * 32 < hq / hkv * new_len || (nrb - 1) * 32 >= hq / hkv * new_len) return -1;
+        if (slots) *used = ((char *)a.part_ml - g_mem) + slots * hkv * nrb * 32 * 2 * 4;
+        if (slots && (char *)a.part_o + slots * hkv * nrb * 32 * d * 4 > (char *)a.part_ml) return -1;   // rows behind the sums
     } else if (g_seen.launched == 1 && a.nsplit > 1) {
         *used = ((char *)a.part_ml - g_mem) + (int64_t)a.nsplit * batch * hkv * a.nrb * 32 * 2 * 4;
     }

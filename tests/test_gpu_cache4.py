@@ -138,6 +138,13 @@ STEPS = [
     (1, 1, 64, 1, [0], None, None, True),
     (1, 1, 128, 64, [64], None, [0], True),
     (40, 8, 128, 6, [6000, 5999], None, [0, 3], False),
+    # several row blocks of the few-row kernel, a new block of several tiles
+    (1, 1, 128, 128, [300, 5, 64], None, [100, 0, 128], False),
+    (4, 2, 64, 60, [3000, 70], [33, 60], [0, 30], True),
+    # streams of very different lengths
+    (16, 2, 128, 40, [9000, 17, 40, 0, 5], None, [3] * 5, False),
+    (24, 24, 128, 200, [4000, 300, 30], [200, 33, 64], None, True),
+    (12, 4, 64, 90, [20000, 300, 300, 8], [90, 33, 64, 1], [80, 33, 0, 0], False),
 ]
 
 

@@ -128,12 +128,15 @@ def test_4bit_steps_stay_in_the_workspace():
             rc, kind, per, nwg, start, used, need = _step4(lens, hkv * G, hkv, d, new)
             assert rc == 0 and used <= need, (cus, lens, hkv, G, new, d)
             seen.add(kind)
-            few = b <= 32 and G * new <= 32
-            assert kind == (2 if few else 1)
-            if few:   # the line holds every stream's pages and new block, the work-groups all of it
-                assert start[0] == 0 and (np.diff(start) == [-(-n // 64) + 1 for n in lens]).all()
+            if b > 32 or G * new > 128:
+                assert kind == 1
+            if b <= 32 and G * new <= 32:
+                assert kind == 2
+            if kind == 2:   # the line holds every stream's pages and new block, the work-groups all of it
+                assert start[0] == 0 and (np.diff(start) == [-(-n // 64) + -(-new // 32) for n in lens]).all()
                 assert (nwg - 1) * per < start[b] <= nwg * per and per >= 8
-                assert nwg * hkv <= max(cus, hkv)
+                nrb = -(-G * new // 32)
+                assert nwg * hkv * nrb <= max(cus, hkv * nrb)
             if need:
                 assert _step4(lens, hkv * G, hkv, d, new, need - 1)[0] == 9
     _lib().probe_cus(256)
