@@ -42,12 +42,18 @@ Cache4Args token_args(const ws_paged_kv4 *kv, int32_t batch, const int32_t *star
     return a;
 }
 
-// Keys of the longest stream in whole tiles: the cache's and the new block's
-// are not mixed in one.
-int64_t tile_keys(int batch, int new_len, const int32_t *cache_lens, const int32_t *nl) {
+// Tiles of a stream: the cache's keys and the new block's are not mixed in one.
+int64_t tiles_of(int64_t cache_len, int64_t new_len) { return (cache_len + 63) / 64 + (new_len + 63) / 64; }
+
+// Keys of the longest stream in whole tiles; tiles: of each of at most
+// LENS_IN_ARGS streams.
+int64_t tile_keys(int batch, int new_len, const int32_t *cache_lens, const int32_t *nl, int64_t *tiles) {
     int64_t most = 0;
-    for (int b = 0; b < batch; ++b)
-        most = std::max<int64_t>(most, ((int64_t)cache_lens[b] + 63) / 64 + ((nl ? nl[b] : new_len) + 63) / 64);
+    for (int b = 0; b < batch; ++b) {
+        const int64_t n = tiles_of(cache_lens[b], nl ? nl[b] : new_len);
+        if (batch <= LENS_IN_ARGS) tiles[b] = n;
+        most = std::max(most, n);
+    }
     return 64 * most;
 }
 
@@ -149,9 +155,10 @@ size_t ws_step_workspace_bytes_4bit(int32_t batch, int32_t num_q_heads, int32_t 
     if (few_rows(batch, num_q_heads / num_kv_heads, new_len))
         return few_workspace(plan_few(cus, batch, num_kv_heads, num_q_heads / num_kv_heads, new_len, cache_lens_host,
                                       new_lens_host), batch, num_kv_heads, 128);
-    const StepPlan p = plan_step(cus, batch, num_q_heads, num_kv_heads, new_len,
-                                 tile_keys(batch, new_len, cache_lens_host, new_lens_host), new_lens_host);
-    return step_workspace(p, batch, num_q_heads, num_kv_heads, new_len);
+    int64_t tiles[LENS_IN_ARGS];
+    const int64_t keys = tile_keys(batch, new_len, cache_lens_host, new_lens_host, tiles);
+    const StepPlan p = plan_step(cus, batch, num_q_heads, num_kv_heads, new_len, keys, new_lens_host);
+    return step_workspace(plan_room(p, batch, tiles), batch, num_q_heads, num_kv_heads, new_len);
 }
 
 int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new, const ws_paged_kv4 *kv,
@@ -196,15 +203,17 @@ int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_n
         return fail(WS_ERR_HIP, "cannot query the device's compute units (hip error %d)", e);
     const bool few = few_rows(batch, G, new_len);
     Few4Plan line{};
-    StepPlan plan{};
+    StepPlan plan{}, room{};
+    int64_t tiles[LENS_IN_ARGS];
     size_t need;
     if (few) {
         line = plan_few(cus, batch, kv->num_kv_heads, G, new_len, cache_lens_host, nl_host);
         need = few_workspace(line, batch, kv->num_kv_heads, 128);
     } else {
-        plan = plan_step(cus, batch, num_q_heads, kv->num_kv_heads, new_len,
-                         tile_keys(batch, new_len, cache_lens_host, nl_host), nl_host);
-        need = step_workspace(plan, batch, num_q_heads, kv->num_kv_heads, new_len);
+        const int64_t keys = tile_keys(batch, new_len, cache_lens_host, nl_host, tiles);
+        plan = plan_step(cus, batch, num_q_heads, kv->num_kv_heads, new_len, keys, nl_host);
+        room = plan_room(plan, batch, tiles);
+        need = step_workspace(room, batch, num_q_heads, kv->num_kv_heads, new_len);
     }
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
         return fail(WS_ERR_WORKSPACE, "workspace needs %zu bytes (16-byte aligned), got %zu", need,
@@ -233,9 +242,9 @@ int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_n
     if (few) {
         a.part_o = (float *)workspace;
         a.part_ml = a.part_o + (size_t)(line.nwg + batch) * a.Hkv * line.nrb * 32 * kv->head_dim;
-    } else if (plan.nsplit > 1) {
+    } else if (room.nsplit > 1) {
         a.part_o = (float *)workspace;
-        a.part_ml = a.part_o + (size_t)plan.nsplit * batch * a.Hkv * a.nrb * 32 * kv->head_dim;
+        a.part_ml = a.part_o + (size_t)room.nsplit * batch * a.Hkv * a.nrb * 32 * kv->head_dim;
     }
     if (text_host) {
         a.text_starts = text_dev;
@@ -262,8 +271,9 @@ int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_n
     // streams of different lengths: per-stream splits
     RaggedPlan rag;
     const int64_t slot_bytes = (int64_t)a.Hkv * a.nrb * 32 * kv->head_dim * (a.out_f32 ? 4 : 2);
-    const bool ragged = plan_ragged(rag, cus, plan, batch, num_q_heads, kv->num_kv_heads, new_len, cache_lens_host,
-                                    nl_host, text_host, slot_bytes, true);
+    const bool ragged = plan_ragged(rag, cus, room, batch, num_q_heads, kv->num_kv_heads, new_len, cache_lens_host,
+                                    nl_host, text_host, slot_bytes, tiles,
+                                    plain_time(cus, plan, batch, kv->num_kv_heads, G, new_len, tiles, nl_host));
     if (ragged) ragged_work(a, rag);
     if (int e = launch_attention(a, ragged ? &rag : nullptr, kv->head_dim, plan.shape, stream))
         return fail(WS_ERR_HIP, "attention launch failed (hip error %d)", e);

@@ -29,6 +29,10 @@ int check_page_range(const int32_t *table, int32_t max_pages, int32_t num_pages,
 // kernels index them in 32-bit arithmetic)
 constexpr int64_t WS_MAX_STEP_ROWS = ((int64_t)1 << 30);
 
+// Per-item fixed cost (prologue, epilogue, partial stores) in units of one
+// 64-key tile of the loop, for the split models.
+constexpr int64_t SPLIT_FIXED_TILES = 4;
+
 struct StepPlan {
     TileShape shape;
     int nqt;
@@ -42,9 +46,17 @@ size_t step_workspace(const StepPlan &p, int batch, int hq, int hkv, int lq);
 int split_override();
 // Splits of a step over streams of different lengths, each with a count of its
 // own, within uni's partial slots (slot_bytes: output values of one); false: one
-// count is as good.  whole_tiles: a stream's cache and new block share no tile.
+// count is as good.  tiles: 64-key tiles of each stream (NULL: those of its cache
+// and new block).  against: the time to beat, in tiles (0: one count's items dealt
+// out evenly).
 bool plan_ragged(RaggedPlan &r, int num_cus, const StepPlan &uni, int batch, int hq, int hkv, int lq,
-                 const int32_t *cache_lens, const int32_t *nl, const int32_t *text, int64_t slot_bytes, bool whole_tiles);
+                 const int32_t *cache_lens, const int32_t *nl, const int32_t *text, int64_t slot_bytes,
+                 const int64_t *tiles, int against);
+// Time of the common launch order, in tiles of each stream (at most LENS_IN_ARGS).
+int plain_time(int num_cus, const StepPlan &p, int batch, int hkv, int G, int new_len, const int64_t *tiles,
+               const int32_t *nl);
+// The plan whose partial slots a step has room for.
+StepPlan plan_room(const StepPlan &uni, int batch, const int64_t *tiles);
 // Work items of a step as that plan counts them.
 void ragged_work(AttnArgs &a, const RaggedPlan &r);
 // Work items and dividers of a launch; false when it would not fit.

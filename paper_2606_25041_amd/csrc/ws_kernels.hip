@@ -156,7 +156,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     constexpr bool C4 = is_cache4(KIND);
     constexpr bool step = KIND == STEP || KIND == STEP_SPLIT || KIND == STEP_RAGGED || C4;
     constexpr bool RAGGED = is_ragged(KIND);
-    static_assert(!WIN || (!RAGGED && KIND != STEP_SPLIT && !C4), "windows: one split count, one step instance");
+    static_assert(!WIN || (KIND != STEP_SPLIT && !C4), "windows: STEP and STEP_RAGGED");
     constexpr bool P3 = (WIN || C4) && F32;
     constexpr bool HALF = (WIN || C4) && !F32;
     constexpr int NT = NW * 64;
@@ -1442,7 +1442,8 @@ int launch_prefill_t(const AttnArgs &a, int key_groups, hipStream_t st) {
 template <int D>
 int launch_attn_d(const AttnArgs &a, const RaggedPlan *rag, TileShape shape, hipStream_t st) {
     if (a.has_window)
-        return a.mode == MODE_STEP ? launch_attn_t<D, STEP, 1, true>(a, NoPlan{}, st)
+        return rag ? launch_attn_t<D, STEP_RAGGED, 1, true>(a, *rag, st)
+             : a.mode == MODE_STEP ? launch_attn_t<D, STEP, 1, true>(a, NoPlan{}, st)
              : a.paged ? launch_prefill_t<D, PREFILL_PAGED, true>(a, shape.kg, st)
                        : launch_prefill_t<D, PREFILL_CONTIGUOUS, true>(a, shape.kg, st);
     if (a.pool4)
@@ -1483,7 +1484,7 @@ int launch_combine_t(const AttnArgs &a, const Plan<RAGGED> &rp, int nsplit, hipS
 
 template <int D>
 int launch_combine_d(const AttnArgs &a, const RaggedPlan *rag, hipStream_t st) {
-    if (a.pool4 && rag)
+    if ((a.has_window || a.pool4) && rag)
         return a.has_new_lens ? launch_combine_t<D, true, true, true>(a, *rag, rag->max_nsplit, st)
                               : launch_combine_t<D, false, true, true>(a, *rag, rag->max_nsplit, st);
     if (a.has_window || a.pool4)

@@ -16,6 +16,7 @@ struct Seen {
     ws::AttnArgs attn;
     ws::BwdArgs bwd;
     ws::Few4Plan few;
+    ws::RaggedPlan rag;
     int kg, ragged, launched, combined;
 } g_seen;
 alignas(256) char g_mem[256];   // stands for every device pointer
@@ -29,6 +30,7 @@ namespace ws {
 int launch_attention(const AttnArgs &a, const RaggedPlan *rag, int, TileShape shape, void *) {
     g_seen.attn = a;
     g_seen.ragged = rag != nullptr;
+    if (rag) g_seen.rag = *rag;
     g_seen.kg = shape.kg;
     return g_seen.launched = 1, 0;
 }
@@ -127,8 +129,15 @@ int probe_step4(int batch, int hq, int hkv, int d, int new_len, const int32_t *l
         if (nrb * 32 < hq / hkv * new_len || (nrb - 1) * 32 >= hq / hkv * new_len) return -1;
         if (slots) *used = ((char *)a.part_ml - g_mem) + slots * hkv * nrb * 32 * 2 * 4;
         if (slots && (char *)a.part_o + slots * hkv * nrb * 32 * d * 4 > (char *)a.part_ml) return -1;   // rows behind the sums
-    } else if (g_seen.launched == 1 && a.nsplit > 1) {
-        *used = ((char *)a.part_ml - g_mem) + (int64_t)a.nsplit * batch * hkv * a.nrb * 32 * 2 * 4;
+    } else if (g_seen.launched == 1 && (g_seen.ragged || a.nsplit > 1)) {
+        int64_t slots = (int64_t)a.nsplit * batch;   // one past the last slot written
+        if (g_seen.ragged) {
+            slots = 0;
+            for (int b = 0; b < batch; ++b)
+                if (g_seen.rag.ns[b] > 1) slots = std::max<int64_t>(slots, g_seen.rag.slot[b] + g_seen.rag.ns[b]);
+        }
+        if (slots) *used = ((char *)a.part_ml - g_mem) + slots * hkv * a.nrb * 32 * 2 * 4;
+        if (slots && (char *)a.part_o + slots * hkv * a.nrb * 32 * d * 4 > (char *)a.part_ml) return -1;
     }
     return rc;
 }

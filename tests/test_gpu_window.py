@@ -71,6 +71,11 @@ STEPS = [
     (3, 1, 128, 90, [4000, 300], None, None, 50, 2 ** 31 - 1, True),        # all sinks
     (8, 1, 128, 5, [20000] * 3 + [40, 1] * 16, None, [0] * 35, 300, 65, False),   # lengths from memory
     (8, 8, 64, 520, [130], None, [500], 64, 64, False),
+    # streams whose live keys differ much
+    (16, 2, 128, 40, [9000, 17, 40, 0, 5], None, None, 4000, 64, False),
+    (24, 24, 128, 200, [4000, 300, 30], [200, 33, 64], None, 2 ** 20, 3, True),
+    (12, 4, 64, 90, [20000, 300, 300, 8], [90, 33, 64, 1], [80, 33, 0, 0], 9000, 100, False),
+    (64, 8, 128, 243, [7000, 3011, 1400, 190], [145, 110, 163, 243], [140, 110, 160, 240], 3500, 65, False),
 ]
 
 
