@@ -506,17 +506,33 @@ int plain_time(int num_cus, const StepPlan &p, int batch, int hkv, int G, int ne
     if (batch > ws::LENS_IN_ARGS) return 0;
     const int64_t per_group = (int64_t)p.nqt * p.nsplit, qt = p.shape.qtile();
     const int64_t per = ((int64_t)batch * hkv * per_group + ws::NUM_XCD - 1) / ws::NUM_XCD;
-    int64_t sum[ws::NUM_XCD] = {}, longest = 0;
+    int64_t count[ws::NUM_XCD][ws::LENS_IN_ARGS] = {};   // items of each stream
     for (int64_t g = 0; g < (int64_t)batch * hkv; ++g) {
         const int b = (int)(nl ? g % batch : g / hkv), n = nl ? nl[b] : new_len;
-        const int64_t size = (tiles[b] + p.nsplit - 1) / p.nsplit + SPLIT_FIXED_TILES;
         const int64_t first = g * per_group, real = ((int64_t)G * n + qt - 1) / qt * p.nsplit;   // (padding's items come last)
-        longest = std::max(longest, size);
         for (int64_t x = first / per; x < ws::NUM_XCD && x * per < first + real; ++x)
-            sum[x] += size * (std::min((x + 1) * per, first + real) - std::max(x * per, first));
+            count[x][b] += std::min((x + 1) * per, first + real) - std::max(x * per, first);
     }
-    const int64_t most = *std::max_element(sum, sum + ws::NUM_XCD) / std::max(1, num_cus / ws::NUM_XCD);
-    return (int)std::min<int64_t>(std::max(longest, most), INT32_MAX / 64);
+    const int cus = std::max(1, num_cus / ws::NUM_XCD);
+    int most = 0;
+    for (const auto &of : count) {
+        ItemGroup grp[ws::LENS_IN_ARGS];
+        int64_t n = 0, load = 0;
+        int groups = 0;
+        for (int b = 0; b < batch; ++b) {
+            if (!of[b]) continue;
+            const int size = (int)((tiles[b] + p.nsplit - 1) / p.nsplit + SPLIT_FIXED_TILES);
+            grp[groups++] = {size, (int)std::min<int64_t>(of[b], INT32_MAX / ws::LENS_IN_ARGS)};
+            n += of[b];
+            load += of[b] * size;
+        }
+        if (!groups) continue;
+        std::sort(grp, grp + groups, [](const ItemGroup &x, const ItemGroup &y) { return x.size > y.size; });
+        // (very many items: their rounds are even enough)
+        const int64_t t = n > 64 * (int64_t)cus ? load / cus : dispatch_time(cus, grp, groups);
+        most = std::max(most, (int)std::min<int64_t>(t, INT32_MAX / 64));
+    }
+    return most;
 }
 
 void ragged_work(AttnArgs &a, const RaggedPlan &r) {
