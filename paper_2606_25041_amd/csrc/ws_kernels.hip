@@ -375,10 +375,13 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     // with the tile loads), so no page-table read sits in front of them.
     const int32_t *ptab = a.page_table + (int64_t)b * a.max_pages;
     const int tp_end = min(t_end, (n_pool + KT - 1) / KT);   // tiles with cache rows
+    // (windows: of the tiles that some row sees cached keys of; the table need not
+    // reach the others)
+    const int tseen_end = ((WIN && lo_min >= n_pool ? min(n_pool, a.sinks) : n_pool) + KT - 1) / KT;
     auto page_glb = [&](int t) -> int {
         if constexpr (WIN) {
             const int u = tile_of(t);
-            return KIND != PREFILL_CONTIGUOUS && t < t_end && u < (n_pool + KT - 1) / KT ? ld_uniform(ptab, u) : 0;
+            return KIND != PREFILL_CONTIGUOUS && t < t_end && u < tseen_end ? ld_uniform(ptab, u) : 0;
         }
         return KIND != PREFILL_CONTIGUOUS && t < tp_end ? ld_uniform(ptab, t) : 0;
     };

@@ -263,6 +263,26 @@ def test_a_billion_tokens_behind_the_window():
     ref.check("lse", lse[0], want["lse"])
 
 
+@pytest.mark.parametrize("n,Lq,sinks", ((6400, 1, 0), (6401, 70, 0), (6463, 33, 65), (6400, 200, 128)))
+def test_a_window_of_no_cached_tokens_needs_the_sinks_pages_only(n, Lq, sinks):
+    """window 0 without a commit: the table ends with the sinks' pages."""
+    Hq, Hkv, D = 4, 2, 128
+    pages = -(-sinks // 64)
+    table = torch.arange(max(pages, 1), dtype=torch.int32)[None] if pages else torch.full((1, 1), -1, dtype=torch.int32)
+    cache = ws.PagedCache.allocate(max(pages, 1), Hkv, D, table, device=DEV, fill_bits=0x7FC1)
+    k, v = _randn(1, sinks, Hkv, D), _randn(2, sinks, Hkv, D)
+    for page in range(pages):
+        m = min(64, sinks - 64 * page)
+        cache.k_pool[page, :, :m] = k[64 * page:64 * page + m].transpose(0, 1)
+        cache.v_pool[page, :, :m] = v[64 * page:64 * page + m].transpose(0, 1)
+    q, kn, vn = _randn(3, 1, Lq, Hq, D), _randn(4, 1, Lq, Hkv, D), _randn(5, 1, Lq, Hkv, D)
+    out, lse = ws.block_causal_attn_fwd(q, kn, vn, cache, _pair([n]), window=0, sinks=sinks, want_lse=True)
+    at = torch.full((Lq,), sinks, dtype=torch.long)   # the sinks, then the block
+    want = ref.attend(q[0], torch.cat([k, kn[0]]), torch.cat([v, vn[0]]), at, at + Lq, sinks, D ** -0.5)
+    ref.check("out", out[0], want["out"])
+    ref.check("lse", lse[0], want["lse"])
+
+
 @pytest.mark.parametrize("mistake", ("window + 1", "window - 1", "sinks + 1", "sinks - 1", "block anchor", "none"))
 def test_the_bounds_catch_a_shifted_window(mistake):
     """The reference with a planted mistake does not pass (and without one it
