@@ -955,7 +955,7 @@ size_t ws_step_workspace_bytes_window(int32_t batch, int32_t num_q_heads, int32_
     if ((int64_t)(num_q_heads / num_kv_heads) * new_len > WS_MAX_STEP_ROWS) return 0;
     for (int b = 0; b < batch; ++b) {
         const int32_t nl = new_lens_host ? new_lens_host[b] : new_len;
-        if (cache_lens_host[b] < 0 || nl < 1 || nl > new_len || (int64_t)cache_lens_host[b] + nl > INT32_MAX) return 0;
+        if (cache_lens_host[b] < 0 || nl < 1 || nl > new_len || (int64_t)cache_lens_host[b] + nl > INT32_MAX - 128) return 0;
     }
     int cus = 0;
     if (ws::current_device_cus(&cus)) return 0;
@@ -1220,7 +1220,8 @@ int step_impl(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new, const ws_paged_k
         }
         if (n + nl > max_k) max_k = n + nl;
     }
-    if (max_k > INT32_MAX) return fail(WS_ERR_SHAPE, "too many keys");
+    // (windows: the table may be all but empty, so key positions can come near 2^31; a tile past them must not)
+    if (max_k > INT32_MAX - (win ? 128 : 0)) return fail(WS_ERR_SHAPE, "too many keys");
     if (text_host)
         for (int b = 0; b < batch; ++b)
             if (text_host[b] < 0 || text_host[b] > new_len)

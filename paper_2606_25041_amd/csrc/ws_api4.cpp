@@ -24,6 +24,8 @@ int check_paged4(const ws_paged_kv4 *kv) {
 }
 
 int check_pages4(const ws_paged_kv4 *kv, int b, int64_t from, int64_t to) {
+    // (the kernels count positions in 32 bits; pages may be shared, so memory is no limit)
+    if (to > INT32_MAX - 128) return fail(WS_ERR_SHAPE, "stream %d: too many tokens", b);
     return check_page_range(kv->page_table_host, kv->max_pages_per_seq, kv->num_pages, b, from, to);
 }
 
@@ -76,7 +78,7 @@ Few4Plan plan_few(int num_cus, int batch, int hkv, int G, int new_len, const int
         at += ((int64_t)cache_lens[b] + 63) / 64 + ((nl ? nl[b] : new_len) + 31) / 32;
     }
     p.start[batch] = (int32_t)at;   // (at most 32 streams of 2^25 tiles)
-    const int64_t most = std::max(1, num_cus / (hkv * p.nrb));
+    const int64_t most = std::max<int64_t>(1, num_cus / ((int64_t)hkv * p.nrb));
     p.per = (int32_t)std::max<int64_t>((at + most - 1) / most, 8);
     p.nwg = (int32_t)((at + p.per - 1) / p.per);
     p.fd_per = fastdiv_make((uint32_t)p.per);
@@ -208,6 +210,8 @@ int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_n
     size_t need;
     if (few) {
         line = plan_few(cus, batch, kv->num_kv_heads, G, new_len, cache_lens_host, nl_host);
+        if ((int64_t)line.nwg * kv->num_kv_heads * line.nrb > 1 << 22)   // (threads of a launch are counted in 32 bits)
+            return fail(WS_ERR_SHAPE, "too many work items");
         need = few_workspace(line, batch, kv->num_kv_heads, 128);
     } else {
         const int64_t keys = tile_keys(batch, new_len, cache_lens_host, nl_host, tiles);

@@ -163,6 +163,8 @@ def test_4bit_append_and_read_refusals(lib):
         h.table[1, 1] = 5
         h.lens[0] = -1
         assert f() == SHAPE
+        h.lens[0] = 2 ** 31 - 140   # (with 16 tokens: past 2^31 - 129)
+        assert f(desc=h.desc(True, max_pages_per_seq=1 << 26)) == SHAPE
         h.lens[0] = 10
     assert append(new=(h.new.ctypes.data, None)) == NULL
     h.new[0] = 17

@@ -141,3 +141,15 @@ def test_4bit_steps_stay_in_the_workspace():
                 assert _step4(lens, hkv * G, hkv, d, new, need - 1)[0] == 9
     _lib().probe_cus(256)
     assert seen == {1, 2}
+
+
+def test_positions_and_heads_past_32_bits_are_refused():
+    OK, SHAPE, limit = 0, 2, 2 ** 31 - 1 - 128
+    table = np.full((1, 1), -1)   # nothing of the cache is seen
+    for n, want in ((limit - 3, OK), (limit - 2, SHAPE), (2 ** 31 - 1, SHAPE)):
+        assert _step_window([n], table, 6, 0, 0, 0)[::2] == (want, 0), n
+    # (heads x row blocks past 2^32: the share of a head was a division by zero)
+    lib = _lib()
+    lib.ws_step_workspace_bytes_4bit.restype = ctypes.c_size_t
+    lens = np.array([100], np.int32)
+    assert lib.ws_step_workspace_bytes_4bit(1, 1 << 30, 1 << 30, 128, ctypes.c_void_p(lens.ctypes.data), None) == 0
