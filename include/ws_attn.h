@@ -76,6 +76,8 @@
  * - Sums are held in f32 before they are normalised, with weights up to 2^8 a
  *   key: values (and gradients' operands) whose sum over the visible keys times
  *   2^8 passes 2^128 give infinities or NaN.
+ * - A key or value that is not finite and that some row of a call sees may also
+ *   make rows of the same stream and KV head NaN that do not see it.
  * - Supported: head_dim 64 or 128; inputs bf16; outputs bf16 or f32;
  *   page_size 64.
  * - The attention and append entry points enqueue kernels only (no device

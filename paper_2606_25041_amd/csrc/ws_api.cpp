@@ -373,7 +373,8 @@ int64_t window_keys(const Window &w, int batch, int new_len, const int32_t *cach
 // the same; a stream with one split writes its output itself and needs none.
 // slot_bytes: output values of one partial slot.
 bool plan_ragged(ws::RaggedPlan &r, int num_cus, const StepPlan &uni, int batch, int hq, int hkv, int lq,
-                 const int32_t *cache_lens, const int32_t *nl, const int32_t *text, int64_t slot_bytes, const int64_t *tiles, int against) {
+                 const int32_t *cache_lens, const int32_t *nl, const int32_t *text, int64_t slot_bytes, const int64_t *tiles, int against,
+                 int *time) {
     if (batch < 2 || batch > ws::LENS_IN_ARGS || split_override()) return false;
     const int64_t qt = uni.shape.qtile(), G = hq / hkv;
     struct Stream { int tiles, q, b; } st[ws::LENS_IN_ARGS];
@@ -483,6 +484,7 @@ bool plan_ragged(ws::RaggedPlan &r, int num_cus, const StepPlan &uni, int batch,
     while (r.deal > 1 && hkv * (r.deal / 2) % ws::NUM_XCD == 0) r.deal /= 2;
     r.per_class = (r.n_items + r.deal - 1) / r.deal;
     r.fd_class = ws::fastdiv_make((uint32_t)r.per_class);
+    if (time) *time = best;
     return true;
 }
 
@@ -503,7 +505,7 @@ StepPlan plan_room(const StepPlan &uni, int batch, const int64_t *tiles) {
 // 0.93 dealt out).
 int plain_time(int num_cus, const StepPlan &p, int batch, int hkv, int G, int new_len, const int64_t *tiles,
                const int32_t *nl) {
-    if (batch > ws::LENS_IN_ARGS) return 0;
+    if (batch > ws::LENS_IN_ARGS || (int64_t)batch * hkv > 1 << 16) return 0;
     const int64_t per_group = (int64_t)p.nqt * p.nsplit, qt = p.shape.qtile();
     const int64_t per = ((int64_t)batch * hkv * per_group + ws::NUM_XCD - 1) / ws::NUM_XCD;
     int64_t count[ws::NUM_XCD][ws::LENS_IN_ARGS] = {};   // items of each stream

@@ -61,14 +61,7 @@ int64_t tile_keys(int batch, int new_len, const int32_t *cache_lens, const int32
 
 // A step of few packed rows: tiles in one line per KV head, an even share for
 // each work-group, one work-group per compute unit (its LDS tiles allow one);
-// a share is at least a tile per wave.  Every 32 rows read the cache again
-// (mostly from an XCD's L2) and unpack it, where the common kernel's 256 rows share
-// one reading, so the common kernel is the faster from about 200 rows on (4 x
-// 131072 tokens, GQA 64/8 x 128: 40 rows 202 us against 393, 64 rows 209 and 395,
-// 96 rows 294 and 403, 128 rows 367 and 411, 256 rows 676 and 587; one stream of
-// 4096: 256 rows 20 and 24).
-bool few_rows(int batch, int G, int new_len) { return batch <= LENS_IN_ARGS && (int64_t)G * new_len <= FEW_ROWS; }
-
+// a share is at least a tile per wave.
 Few4Plan plan_few(int num_cus, int batch, int hkv, int G, int new_len, const int32_t *cache_lens, const int32_t *nl) {
     Few4Plan p{};
     p.nrb = (G * new_len + 31) / 32;
@@ -85,6 +78,43 @@ Few4Plan plan_few(int num_cus, int batch, int hkv, int G, int new_len, const int
     p.fd_hkv = fastdiv_make((uint32_t)hkv);
     p.fd_nrb = fastdiv_make((uint32_t)p.nrb);
     return p;
+}
+
+// Whether a step runs as one of few rows (line: its plan).  Every 32 rows of it
+// read the cache again (mostly from an XCD's L2) and unpack it, where the common
+// kernel's 256 rows share one reading; but its work divides evenly, and over all
+// compute units where the common kernel has at most 32 splits per stream.  Both
+// times in units of 0.17 us: a tile of a work-group's share 0.34 us, a stream's
+// part in it 4, its launch 3, the merge 5; of the common kernel's T tiles by its plan each
+// 1.7 us up to 128 rows in one common count of splits (half its waves idle), else
+// 2.2.  Few rows against the common kernel: 4 x 131072 tokens, GQA 64/8 x 128: 40
+// rows 202 us and 393, 160 rows 480 and 537, 256 rows 689 and 616; MHA 24: 150
+// rows 1.39 ms and 1.58, 200 rows 2.49 and 1.71 (168 of 256 compute units); one
+// stream, 8/1 x 128: 256 rows 41 us and 168; 32 streams of 100 tokens, 64/8, one
+// token each: 27 and 11.  Of 809 steps of 1 to 520 rows over one to 32 streams
+// (few rows up to 128, the common kernel past them, against this choice) 72 run
+// more than 1.5 times as fast, 8 below 0.95 (least 0.82).
+bool few_rows(int num_cus, int batch, int hq, int hkv, int new_len, const int32_t *cache_lens, const int32_t *nl,
+              Few4Plan &line) {
+    const int G = hq / hkv, rows = G * new_len;
+    if (batch > LENS_IN_ARGS || (int64_t)G * new_len > FEW_ROWS) return false;
+    line = plan_few(num_cus, batch, hkv, G, new_len, cache_lens, nl);
+    int64_t parts = 1;   // of one work-group
+    for (int b = 0, from = 0; b < batch; ++b) {   // (streams from .. b lie in one share, or touch it)
+        while (line.start[b] / line.per > (line.start[from + 1] - 1) / line.per) ++from;
+        parts = std::max<int64_t>(parts, b - from + 1);
+    }
+    const int64_t groups = (int64_t)line.nwg * hkv * line.nrb;
+    const int64_t few = (groups + num_cus - 1) / num_cus * (2 * (int64_t)line.per + 16 + 24 * parts) + (line.nwg > 1 ? 30 : 0);
+    int64_t tiles[LENS_IN_ARGS];
+    const int64_t keys = tile_keys(batch, new_len, cache_lens, nl, tiles);
+    const StepPlan p = plan_step(num_cus, batch, hq, hkv, new_len, keys, nl);
+    int t = plain_time(num_cus, p, batch, hkv, G, new_len, tiles, nl);
+    if (!t) return false;   // (more heads than a plan looks at)
+    RaggedPlan rag;
+    const bool dealt = plan_ragged(rag, num_cus, plan_room(p, batch, tiles), batch, hq, hkv, new_len, cache_lens, nl, nullptr,
+                                   (int64_t)hkv * line.nrb * 32 * 128 * 2, tiles, t, &t);
+    return few <= 13 * SPLIT_FIXED_TILES + (rows <= 128 && !dealt ? 10 : 13) * (t - SPLIT_FIXED_TILES) + (p.nsplit > 1 ? 30 : 0);
 }
 
 // Partials: a part of 32 rows x D and the rows' (m, l), f32, per KV head and row
@@ -154,9 +184,9 @@ size_t ws_step_workspace_bytes_4bit(int32_t batch, int32_t num_q_heads, int32_t 
     }
     int cus = 0;
     if (current_device_cus(&cus)) return 0;
-    if (few_rows(batch, num_q_heads / num_kv_heads, new_len))
-        return few_workspace(plan_few(cus, batch, num_kv_heads, num_q_heads / num_kv_heads, new_len, cache_lens_host,
-                                      new_lens_host), batch, num_kv_heads, 128);
+    Few4Plan line;
+    if (few_rows(cus, batch, num_q_heads, num_kv_heads, new_len, cache_lens_host, new_lens_host, line))
+        return few_workspace(line, batch, num_kv_heads, 128);
     int64_t tiles[LENS_IN_ARGS];
     const int64_t keys = tile_keys(batch, new_len, cache_lens_host, new_lens_host, tiles);
     const StepPlan p = plan_step(cus, batch, num_q_heads, num_kv_heads, new_len, keys, new_lens_host);
@@ -203,15 +233,12 @@ int ws_block_causal_attn_fwd_4bit(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_n
     int cus = 0;
     if (int e = current_device_cus(&cus))
         return fail(WS_ERR_HIP, "cannot query the device's compute units (hip error %d)", e);
-    const bool few = few_rows(batch, G, new_len);
     Few4Plan line{};
+    const bool few = few_rows(cus, batch, num_q_heads, kv->num_kv_heads, new_len, cache_lens_host, nl_host, line);
     StepPlan plan{}, room{};
     int64_t tiles[LENS_IN_ARGS];
     size_t need;
     if (few) {
-        line = plan_few(cus, batch, kv->num_kv_heads, G, new_len, cache_lens_host, nl_host);
-        if ((int64_t)line.nwg * kv->num_kv_heads * line.nrb > 1 << 22)   // (threads of a launch are counted in 32 bits)
-            return fail(WS_ERR_SHAPE, "too many work items");
         need = few_workspace(line, batch, kv->num_kv_heads, 128);
     } else {
         const int64_t keys = tile_keys(batch, new_len, cache_lens_host, nl_host, tiles);

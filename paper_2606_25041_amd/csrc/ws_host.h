@@ -48,11 +48,12 @@ int split_override();
 // own, within uni's partial slots (slot_bytes: output values of one); false: one
 // count is as good.  tiles: 64-key tiles of each stream (NULL: those of its cache
 // and new block).  against: the time to beat, in tiles (0: one count's items dealt
-// out evenly).
+// out evenly).  time: the plan's, in tiles.
 bool plan_ragged(RaggedPlan &r, int num_cus, const StepPlan &uni, int batch, int hq, int hkv, int lq,
                  const int32_t *cache_lens, const int32_t *nl, const int32_t *text, int64_t slot_bytes,
-                 const int64_t *tiles, int against);
-// Time of the common launch order, in tiles of each stream (at most LENS_IN_ARGS).
+                 const int64_t *tiles, int against, int *time = nullptr);
+// Time of the common launch order, in tiles of each stream (0: more streams than
+// LENS_IN_ARGS or very many heads).
 int plain_time(int num_cus, const StepPlan &p, int batch, int hkv, int G, int new_len, const int64_t *tiles,
                const int32_t *nl);
 // The plan whose partial slots a step has room for.

@@ -192,7 +192,7 @@ struct Cache4Args {
 // read the same amount whatever the streams' lengths.  The part of a work-group
 // in a stream has the partial slot w + stream (both grow along the line, one of
 // them at every part).
-constexpr int FEW_ROWS = 128;          // at most this many
+constexpr int FEW_ROWS = 512;          // at most this many
 struct Few4Plan {
     int32_t per;                       // tiles of a work-group
     int32_t nwg;                       // work-groups of a KV head and row block

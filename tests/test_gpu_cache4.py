@@ -145,6 +145,15 @@ STEPS = [
     (16, 2, 128, 40, [9000, 17, 40, 0, 5], None, [3] * 5, False),
     (24, 24, 128, 200, [4000, 300, 30], [200, 33, 64], None, True),
     (12, 4, 64, 90, [20000, 300, 300, 8], [90, 33, 64, 1], [80, 33, 0, 0], False),
+    # the few-row kernel with up to 16 row blocks
+    (8, 1, 128, 60, [9000], None, [13], False),
+    (8, 1, 64, 50, [9000, 33, 0], [50, 1, 20], [40, 0, 20], True),
+    (16, 4, 64, 128, [5000], None, None, True),
+    (40, 8, 128, 100, [4096], None, None, False),
+    # the common kernel on few rows: many short streams
+    (16, 8, 128, 1, [100, 3, 64, 0] * 8, None, None, False),
+    (16, 2, 64, 5, [100, 3, 64, 0] * 8, [5, 1, 3, 2] * 8, [0, 1, 3, 1] * 8, True),
+    (24, 24, 128, 100, [1200] * 4, None, None, False),
 ]
 
 

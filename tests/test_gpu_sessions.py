@@ -332,3 +332,43 @@ def test_empty_calls():
     assert ws.block_causal_prefill(q1, k1, k1, _pair([[0, 0]]), window=0, sinks=0).shape == q1.shape
     dq, dk, dv = ws.block_causal_prefill_bwd(q1, k1, k1, q1, q1, torch.empty(1, 4, 0, device=DEV), _pair([[0, 0]]), window=2)
     assert dq.shape == q1.shape and dk.shape == k1.shape and dv.shape == k1.shape
+
+
+@pytest.mark.parametrize("four", (False, True))
+def test_refused_calls_change_nothing(four):
+    """The last check of each call fails (the page of a committed token, the
+    workspace): outputs, log-sum-exp, gradients and pools keep their bytes."""
+    Hq, Hkv, D, Lq = 8, 2, 128, 40
+    table = torch.tensor([[0, 1, 9]], dtype=torch.int32)   # 3 pages in the pool; page 9 is that of positions 128..
+    if four:
+        cache = ws.PagedCache4.allocate(3, Hkv, D, table, device=DEV)
+        cache.pool.fill_(7)
+        pools = [cache.pool]
+    else:
+        cache = ws.PagedCache.allocate(3, Hkv, D, table, device=DEV, fill_bits=0x4040)
+        pools = [cache.k_pool, cache.v_pool]
+    q, k, v = _randn(1, 1, Lq, Hq, D), _randn(2, 1, Lq, Hkv, D), _randn(3, 1, Lq, Hkv, D)
+    out, lse = torch.full_like(q, 7.0), torch.full((1, Hq, Lq), 3.0, device=DEV)
+    grads = [torch.full_like(x, 5.0) for x in (q, k, v)]
+    kept = [out, lse, *grads, *pools]
+    before = [t.clone() for t in kept]
+    win = {} if four else dict(window=50, sinks=3)
+    off, small = _pair([[0, Lq]]), torch.empty(64, dtype=torch.uint8, device=DEV)
+    calls = {"WS_ERR_PAGE": lambda: ws.block_causal_attn_fwd(q, k, v, cache, _pair([100]), fuse_append=True, out=out, lse=lse, **win)}
+    if four:
+        with pytest.raises(ws.WsError) as e:
+            ws.kv_append(cache, _pair([100]), k, v)
+        assert e.value.name == "WS_ERR_PAGE"
+        with pytest.raises(ws.WsError) as e:
+            ws.kv_read(cache, _pair([100]), Lq, k=grads[1], v=grads[2])
+        assert e.value.name == "WS_ERR_PAGE"
+    else:
+        calls["WS_ERR_WORKSPACE"] = lambda: ws.block_causal_prefill_bwd(
+            q, k, v, q, q, lse, off, dq=grads[0], dk=grads[1], dv=grads[2], workspace=small, **win)
+    for name, call in calls.items():
+        with pytest.raises(ws.WsError) as e:
+            call()
+        assert e.value.name == name
+    torch.cuda.synchronize()
+    for t, was in zip(kept, before):
+        assert torch.equal(t.view(torch.uint8), was.view(torch.uint8))

@@ -127,11 +127,9 @@ def test_4bit_steps_stay_in_the_workspace():
             d = g.choice((64, 128))
             rc, kind, per, nwg, start, used, need = _step4(lens, hkv * G, hkv, d, new)
             assert rc == 0 and used <= need, (cus, lens, hkv, G, new, d)
-            seen.add(kind)
-            if b > 32 or G * new > 128:
+            seen.add((kind, G * new <= 128))
+            if b > 32 or G * new > 512:
                 assert kind == 1
-            if b <= 32 and G * new <= 32:
-                assert kind == 2
             if kind == 2:   # the line holds every stream's pages and new block, the work-groups all of it
                 assert start[0] == 0 and (np.diff(start) == [-(-n // 64) + -(-new // 32) for n in lens]).all()
                 assert (nwg - 1) * per < start[b] <= nwg * per and per >= 8
@@ -140,7 +138,7 @@ def test_4bit_steps_stay_in_the_workspace():
             if need:
                 assert _step4(lens, hkv * G, hkv, d, new, need - 1)[0] == 9
     _lib().probe_cus(256)
-    assert seen == {1, 2}
+    assert seen == {(1, False), (1, True), (2, False), (2, True)}
 
 
 def test_positions_and_heads_past_32_bits_are_refused():
