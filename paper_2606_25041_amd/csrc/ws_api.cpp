@@ -1,4 +1,5 @@
-// C ABI of libwsattn: host-side validation and launch planning.
+// C ABI of libwsattn: host-side validation and launch planning (the 4-bit
+// cache's entry points: ws_api4.cpp).
 //
 // Plain C++ (no HIP headers): every argument is checked here before any
 // device work is enqueued, so a rejected call leaves all device memory

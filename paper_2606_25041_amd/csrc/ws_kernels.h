@@ -1,6 +1,7 @@
 // Internal interface between the host-side validation/planning code
-// (ws_api.cpp, no HIP headers) and the gfx950 kernels (ws_kernels.hip for
-// attention, merge and append; ws_bwd.hip for the gradients).
+// (ws_api.cpp and ws_api4.cpp, no HIP headers) and the gfx950 kernels
+// (ws_kernels.hip for attention, merge and append; ws_cache4.hip for the 4-bit
+// cache; ws_bwd.hip for the gradients).
 #pragma once
 
 #include <stddef.h>
@@ -207,8 +208,8 @@ struct Few4Plan {
 constexpr int BWD_MAX_SPLIT_TILES = 128;
 constexpr int BWD_MAX_SPLITS = 16;
 
-// Gradients of the whole-sequence path (contiguous K/V).  bf16 inputs,
-// f32 gradients; element strides.
+// Gradients of the whole-sequence path (contiguous K/V).  bf16 inputs, f32
+// gradients (windowed: f32 or bf16); element strides.
 struct BwdArgs {
     const uint16_t *q, *k, *v, *o, *dout;
     int64_t q_sb, q_st, q_sh;

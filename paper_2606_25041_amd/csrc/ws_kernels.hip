@@ -6,9 +6,10 @@
 // Sec. 2.4) whose tokens see the segment only up to themselves.  The step
 // kernel runs the current unit against its full-history cache (Sec. 2.4);
 // the prefill kernel covers whole sequences (Sec. 2.4, system prefill); the
-// append kernel commits a KV slice to the paged cache (Sec. 2.4).  The
-// gradient kernels, which serve training in the same causal format
-// (Sec. 2.3), are in ws_bwd.hip.
+// append kernel commits a KV slice to the paged cache (Sec. 2.4).  Both take a
+// sliding window with sinks, and the step a cache held in 4 bits, whose append,
+// read-back and steps of few rows are in ws_cache4.hip.  The gradient kernels,
+// which serve training in the same causal format (Sec. 2.3), are in ws_bwd.hip.
 //
 // Attention kernel design (one work-group = one work item: a tile of 256
 // query rows of one (stream, KV head) group and one KV split, 8 waves x 32
