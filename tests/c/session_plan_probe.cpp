@@ -1,0 +1,79 @@
+// Which kernel, and which plan of it, a windowed call or a step over a 4-bit
+// cache reaches: window_probe.cpp's recording launchers behind calls that take
+// the output type, the new blocks' lengths and a prefill's blocks.
+#include "window_probe.cpp"
+
+namespace {
+// out: kernel (1 the common one, 2 the few-row one; 0 nothing launched), f32
+// output, per-stream splits, most splits of a stream, whether partials are merged
+void report_step(int batch, int *out) {
+    const ws::AttnArgs &a = g_seen.attn;
+    int most = 1;
+    if (g_seen.launched == 2) {
+        for (int b = 0; b < batch; ++b)
+            most = std::max(most, (g_seen.few.start[b + 1] - 1) / g_seen.few.per - g_seen.few.start[b] / g_seen.few.per + 1);
+    } else {
+        most = g_seen.ragged ? g_seen.rag.max_nsplit : a.nsplit;
+    }
+    out[0] = g_seen.launched;
+    out[1] = a.out_f32;
+    out[2] = g_seen.ragged;
+    out[3] = most;
+    out[4] = g_seen.combined;
+}
+}  // namespace
+
+extern "C" {
+
+int reach_step4(int batch, int hq, int hkv, int d, int new_len, const int32_t *lens, const int32_t *nl, int f32, int *out) {
+    int64_t pages = 1;
+    for (int b = 0; b < batch; ++b) pages = std::max<int64_t>(pages, lens[b] / 64 + 1);
+    const std::vector<int32_t> table((size_t)(batch * pages), 0);
+    const int32_t *dev = (const int32_t *)g_mem;
+    const ws_paged_kv4 kv{g_mem, dev, table.data(), 1, WS_PAGE_SIZE, (int32_t)pages, hkv, d};
+    const ws_tensor4 q = tensor(WS_DTYPE_BF16, new_len, hq, d), k = tensor(WS_DTYPE_BF16, new_len, hkv, d);
+    const ws_tensor4 o = tensor(f32 ? WS_DTYPE_F32 : WS_DTYPE_BF16, new_len, hq, d);
+    memset(&g_seen, 0, sizeof g_seen);
+    const int64_t need = (int64_t)ws_step_workspace_bytes_4bit(batch, hq, hkv, new_len, lens, nl);
+    const int rc = ws_block_causal_attn_fwd_4bit(q, k, k, &kv, lens, dev, nl, nl ? dev : nullptr, nullptr, nullptr, batch,
+                                                 new_len, hq, 0.1f, 0, o, nullptr, g_mem, (size_t)need, nullptr);
+    report_step(batch, out);
+    return rc;
+}
+
+int reach_step_window(int batch, int hq, int hkv, int d, int new_len, const int32_t *lens, const int32_t *nl, int sinks,
+                      int window, int f32, int *out) {
+    int64_t pages = 1;
+    for (int b = 0; b < batch; ++b) pages = std::max<int64_t>(pages, lens[b] / 64 + 1);
+    const std::vector<int32_t> table((size_t)(batch * pages), 0);
+    const int32_t *dev = (const int32_t *)g_mem;
+    const ws_paged_kv kv{g_mem, g_mem, dev, table.data(), 1, WS_PAGE_SIZE, (int32_t)pages, hkv, d};
+    const ws_tensor4 q = tensor(WS_DTYPE_BF16, new_len, hq, d), k = tensor(WS_DTYPE_BF16, new_len, hkv, d);
+    const ws_tensor4 o = tensor(f32 ? WS_DTYPE_F32 : WS_DTYPE_BF16, new_len, hq, d);
+    memset(&g_seen, 0, sizeof g_seen);
+    const int64_t need = (int64_t)ws_step_workspace_bytes_window(batch, hq, hkv, new_len, lens, nl, sinks, window);
+    const int rc = ws_block_causal_attn_fwd_window(q, k, k, &kv, lens, dev, nl, nl ? dev : nullptr, nullptr, nullptr, batch,
+                                                   new_len, hq, sinks, window, 0.1f, 0, o, nullptr, g_mem, (size_t)need,
+                                                   nullptr);
+    report_step(batch, out);
+    return rc;
+}
+
+// kg: key groups of a work-group (1: 256-row tiles, 2: 128-row tiles)
+int reach_prefill_window(int batch, int hq, int hkv, int d, int seq, int nb, const int32_t *offsets, const int32_t *text,
+                         int sinks, int window, int paged, int f32, int *kg) {
+    const int32_t *dev = (const int32_t *)g_mem;
+    const int pages = (seq + 63) / 64;
+    const std::vector<int32_t> table((size_t)batch * pages, 0);
+    const ws_paged_kv kv{g_mem, g_mem, dev, table.data(), 1, WS_PAGE_SIZE, pages, hkv, d};
+    const ws_tensor4 q = tensor(WS_DTYPE_BF16, seq, hq, d), none{nullptr, WS_DTYPE_BF16, 0, 0, 0};
+    const ws_tensor4 k = paged ? none : tensor(WS_DTYPE_BF16, seq, hkv, d);
+    const ws_tensor4 o = tensor(f32 ? WS_DTYPE_F32 : WS_DTYPE_BF16, seq, hq, d);
+    memset(&g_seen, 0, sizeof g_seen);
+    const int rc = ws_block_causal_prefill_window(q, k, k, paged ? &kv : nullptr, offsets, dev, text, text ? dev : nullptr,
+                                                  batch, seq, nb, hq, hkv, d, sinks, window, 0.1f, o, nullptr, nullptr);
+    *kg = g_seen.kg;
+    return rc;
+}
+
+}  // extern "C"
