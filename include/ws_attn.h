@@ -177,7 +177,9 @@ const char *ws_last_error(void);
  * cache_lens[b] + t of stream b.  k_new / v_new: bf16 [batch][new_len]
  * [num_kv_heads][head_dim].  cache_lens_host / cache_lens_dev: int32
  * [batch], the same values on host (validated) and device.  The cache
- * lengths are not updated; the caller adds new_len afterwards.
+ * lengths are not updated; the caller adds new_len afterwards.  Only the new
+ * positions' pages have to exist: the table's other entries may hold anything
+ * (a session behind a sliding window gives earlier pages back).
  * Errors: WS_ERR_NULL, WS_ERR_SHAPE (batch/new_len < 0, cache_lens < 0),
  * WS_ERR_UNSUPPORTED, WS_ERR_ALIGN, WS_ERR_CAPACITY, WS_ERR_PAGE, WS_ERR_HIP.
  */

@@ -100,11 +100,16 @@ int check_paged(const ws_paged_kv *kv) {
     return WS_OK;
 }
 
+int check_capacity(int32_t max_pages, int b, int64_t tokens) {
+    if (tokens > (int64_t)max_pages * WS_PAGE_SIZE)
+        return fail(WS_ERR_CAPACITY, "stream %d needs %lld tokens but holds at most %lld", b,
+                    (long long)tokens, (long long)max_pages * WS_PAGE_SIZE);
+    return WS_OK;
+}
+
 int check_page_range(const int32_t *table, int32_t max_pages, int32_t num_pages, int b, int64_t from, int64_t to) {
     if (from >= to) return WS_OK;
-    if (to > (int64_t)max_pages * WS_PAGE_SIZE)
-        return fail(WS_ERR_CAPACITY, "stream %d needs %lld tokens but holds at most %lld", b,
-                    (long long)to, (long long)max_pages * WS_PAGE_SIZE);
+    if (int rc = check_capacity(max_pages, b, to)) return rc;
     const int64_t pages = (to + WS_PAGE_SIZE - 1) / WS_PAGE_SIZE;
     const int32_t *row = table + (int64_t)b * max_pages;
     for (int64_t p = from / WS_PAGE_SIZE; p < pages; ++p)
@@ -1161,7 +1166,10 @@ int append_impl(const ws_paged_kv *kv, int32_t batch, const int32_t *cache_lens_
         if (cache_lens_host[b] < 0) return fail(WS_ERR_SHAPE, "cache_lens[%d] = %d", b, (int)cache_lens_host[b]);
         if (nl_host && (nl_host[b] < 0 || nl_host[b] > new_len))
             return fail(WS_ERR_SHAPE, "new_lens[%d] = %d outside [0, new_len %d]", b, (int)nl_host[b], (int)new_len);
-        if (int rc = check_pages(kv, b, (int64_t)cache_lens_host[b] + (nl_host ? nl_host[b] : new_len))) return rc;
+        // (only the new tokens' pages: earlier ones may have left a window and be gone)
+        const int64_t from = cache_lens_host[b], to = from + (nl_host ? nl_host[b] : new_len);
+        if (int rc = check_capacity(kv->max_pages_per_seq, b, to)) return rc;
+        if (int rc = check_page_range(kv->page_table_host, kv->max_pages_per_seq, kv->num_pages, b, from, to)) return rc;
     }
     ws::AppendArgs a{};
     a.kn = (const uint16_t *)k_new.ptr;
