@@ -1169,6 +1169,8 @@ int append_impl(const ws_paged_kv *kv, int32_t batch, const int32_t *cache_lens_
         // (only the new tokens' pages: earlier ones may have left a window and be gone)
         const int64_t from = cache_lens_host[b], to = from + (nl_host ? nl_host[b] : new_len);
         if (int rc = check_capacity(kv->max_pages_per_seq, b, to)) return rc;
+        // (the kernel counts positions in 32 bits; pages may be shared, so memory is no limit)
+        if (to > INT32_MAX) return fail(WS_ERR_SHAPE, "stream %d: too many tokens", b);
         if (int rc = check_page_range(kv->page_table_host, kv->max_pages_per_seq, kv->num_pages, b, from, to)) return rc;
     }
     ws::AppendArgs a{};

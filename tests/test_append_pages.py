@@ -45,3 +45,14 @@ def test_pages_that_left_the_window_may_be_gone(varlen):
     if varlen:   # a stream that commits nothing needs no page
         assert append(np.full((2, 102), -1), lens, new, [0, 0]) in (OK, HIP)
         assert append(table[:, :99], lens, new, [0, 0]) == CAPACITY
+
+
+def test_positions_past_32_bits_are_refused():
+    """The kernel counts positions in 32 bits (pages may be shared, so memory is
+    no limit): 2^25 pages of one physical page."""
+    table = np.zeros((1, 2 ** 25 + 1), np.int32)
+    last = 2 ** 31 - 1
+    assert append(table, [last - 5], 5) in (OK, HIP)
+    assert append(table, [last - 5], 6) == SHAPE
+    assert append(table, [last - 5], 6, [5]) in (OK, HIP)
+    assert append(table, [last - 5], 6, [6]) == SHAPE
