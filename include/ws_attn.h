@@ -270,6 +270,7 @@ int ws_block_causal_attn_fwd_noalloc(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 
  *   block_offsets_host / _dev: int32 [batch][num_blocks + 1], same values
  *   out:  bf16 or f32 [batch][seq_len][num_q_heads][head_dim]
  *   lse:  NULL or device f32 [batch][num_q_heads][seq_len]
+ * seq_len must not exceed 2^31 - 257 (WS_ERR_SHAPE).
  * Errors: WS_ERR_NULL, WS_ERR_SHAPE, WS_ERR_UNSUPPORTED, WS_ERR_ALIGN,
  * WS_ERR_HEADS, WS_ERR_OFFSETS, WS_ERR_CAPACITY, WS_ERR_PAGE, WS_ERR_HIP.
  */
@@ -407,6 +408,7 @@ int ws_block_causal_prefill_text(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v,
  *               unsplit
  * The gradients are deterministic (fixed summation order for a given shape,
  * device and size of workspace; no atomics).
+ * seq_len must be below 2^30 (WS_ERR_SHAPE).
  * Errors: WS_ERR_NULL, WS_ERR_SHAPE, WS_ERR_UNSUPPORTED, WS_ERR_ALIGN,
  * WS_ERR_HEADS, WS_ERR_OFFSETS, WS_ERR_WORKSPACE, WS_ERR_HIP.
  */

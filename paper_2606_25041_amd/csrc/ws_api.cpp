@@ -35,6 +35,9 @@ int ok() {
 constexpr int WS_MAX_SPLITS = ws::MAX_SPLITS;
 static_assert(WS_NOALLOC_SCRATCH_BYTES == ws::NOALLOC_SCRATCH_BYTES, "one scratch size");
 constexpr int WS_MAX_HEAD_DIM = 128;
+// Tokens of a whole-sequence call: the ends of query and key tiles behind the
+// last token stay below 2^31; the gradients address 4 bytes a token in 32 bits.
+constexpr int32_t WS_MAX_SEQ = INT32_MAX - 256, WS_MAX_BWD_SEQ = (1 << 30) - 1;
 
 int env_int(const char *name, int dflt) {
     const char *s = std::getenv(name);
@@ -797,7 +800,8 @@ const char *ws_last_error(void) { return g_err; }
 size_t ws_workspace_bytes(int32_t op, int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
                           int32_t max_q, int32_t max_k) {
     if (op == WS_OP_PREFILL_BWD) {
-        if (batch <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads || max_q <= 0)
+        if (batch <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads || max_q <= 0 ||
+            max_q > WS_MAX_BWD_SEQ)
             return 0;
         return bwd_workspace(batch, num_q_heads, num_kv_heads, max_q);
     }
@@ -1015,7 +1019,7 @@ int ws_block_causal_prefill_window_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v,
 size_t ws_prefill_window_bwd_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
                                              int32_t seq_len, int32_t sinks, int32_t window) {
     if (batch <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads || seq_len <= 0 ||
-        sinks < 0 || window < 0)
+        seq_len > WS_MAX_BWD_SEQ || sinks < 0 || window < 0)
         return 0;
     // (blocks of one token to blocks of 768: the call knows which, and takes what fits)
     int64_t parts = 0;
@@ -1039,6 +1043,7 @@ int bwd_impl(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 o, ws_tensor4 
         return fail(WS_ERR_SHAPE, "batch %d, seq_len %d, num_blocks %d, heads %d/%d", (int)batch, (int)seq_len,
                     (int)num_blocks, (int)num_q_heads, (int)num_kv_heads);
     if (int rc = check_window(win)) return rc;
+    if (seq_len > WS_MAX_BWD_SEQ) return fail(WS_ERR_SHAPE, "seq_len %d exceeds %d", (int)seq_len, (int)WS_MAX_BWD_SEQ);
     if (batch == 0 || seq_len == 0) return ok();
     if (int rc = check_tensor("q", q, false)) return rc;
     if (int rc = check_tensor("k", k, false)) return rc;
@@ -1342,6 +1347,7 @@ int prefill_impl(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const ws_paged_kv *kv
         return fail(WS_ERR_SHAPE, "batch %d, seq_len %d, num_blocks %d, heads %d/%d", (int)batch, (int)seq_len,
                     (int)num_blocks, (int)num_q_heads, (int)num_kv_heads);
     if (int rc = check_window(win)) return rc;
+    if (seq_len > WS_MAX_SEQ) return fail(WS_ERR_SHAPE, "seq_len %d exceeds %d", (int)seq_len, (int)WS_MAX_SEQ);
     if (batch == 0 || seq_len == 0) return ok();  // no token: nothing is read or written
     const bool paged = !k.ptr && !v.ptr;
     if (paged) {

@@ -63,7 +63,7 @@ int reach_step_window(int batch, int hq, int hkv, int d, int new_len, const int3
 int reach_prefill_window(int batch, int hq, int hkv, int d, int seq, int nb, const int32_t *offsets, const int32_t *text,
                          int sinks, int window, int paged, int f32, int *kg) {
     const int32_t *dev = (const int32_t *)g_mem;
-    const int pages = (seq + 63) / 64;
+    const int pages = paged ? (int)(((int64_t)seq + 63) / 64) : 1;
     const std::vector<int32_t> table((size_t)batch * pages, 0);
     const ws_paged_kv kv{g_mem, g_mem, dev, table.data(), 1, WS_PAGE_SIZE, pages, hkv, d};
     const ws_tensor4 q = tensor(WS_DTYPE_BF16, seq, hq, d), none{nullptr, WS_DTYPE_BF16, 0, 0, 0};
@@ -74,6 +74,30 @@ int reach_prefill_window(int batch, int hq, int hkv, int d, int seq, int nb, con
                                                   batch, seq, nb, hq, hkv, d, sinks, window, 0.1f, o, nullptr, nullptr);
     *kg = g_seen.kg;
     return rc;
+}
+
+// A prefill without a window, contiguous.
+int reach_prefill(int batch, int hq, int hkv, int d, int seq, int nb, const int32_t *offsets, const int32_t *text) {
+    const int32_t *dev = (const int32_t *)g_mem;
+    const ws_tensor4 q = tensor(WS_DTYPE_BF16, seq, hq, d), k = tensor(WS_DTYPE_BF16, seq, hkv, d);
+    if (text)
+        return ws_block_causal_prefill_text(q, k, k, nullptr, offsets, dev, text, dev, batch, seq, nb, hq, hkv, d, 0.1f, q,
+                                            nullptr, nullptr);
+    return ws_block_causal_prefill(q, k, k, nullptr, offsets, dev, batch, seq, nb, hq, hkv, d, 0.1f, q, nullptr, nullptr);
+}
+
+// Gradients with all the workspace one could ask for.
+int reach_bwd(int batch, int hq, int hkv, int d, int seq, int nb, const int32_t *offsets, int windowed, int window) {
+    const int32_t *dev = (const int32_t *)g_mem;
+    const ws_tensor4 q = tensor(WS_DTYPE_BF16, seq, hq, d), k = tensor(WS_DTYPE_BF16, seq, hkv, d);
+    const ws_tensor4 dq = tensor(WS_DTYPE_F32, seq, hq, d), dk = tensor(WS_DTYPE_F32, seq, hkv, d);
+    const float *lse = (const float *)g_mem;
+    const size_t room = (size_t)1 << 40;
+    if (windowed)
+        return ws_block_causal_prefill_window_bwd(q, k, k, q, q, lse, offsets, dev, nullptr, nullptr, batch, seq, nb, hq, hkv,
+                                                  d, 0, window, 0.1f, dq, dk, dk, g_mem, room, nullptr);
+    return ws_block_causal_prefill_bwd(q, k, k, q, q, lse, offsets, dev, nullptr, nullptr, batch, seq, nb, hq, hkv, d, 0.1f,
+                                       dq, dk, dk, g_mem, room, nullptr);
 }
 
 }  // extern "C"
