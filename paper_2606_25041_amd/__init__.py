@@ -304,9 +304,18 @@ def _lens(cache_lens, device):
     return host, host.to(device)
 
 
+def _check_pair(name, host, dev):
+    """The library reads packed int32 arrays, one on either side."""
+    if host.dtype != torch.int32 or dev.dtype != torch.int32 or not host.is_contiguous() or not dev.is_contiguous():
+        raise ValueError(f"{name}: int32 contiguous arrays expected")
+    if host.device.type != "cpu" or not dev.is_cuda:
+        raise ValueError(f"{name} must be a (host, device) pair")
+
+
 def _check_lens(host, dev, B):
     if host.shape != (B,) or dev.shape != (B,) or host.dtype != torch.int32 or dev.dtype != torch.int32:
         raise ValueError("cache_lens must be int32 [B] on host and device")
+    _check_pair("cache_lens", host, dev)
 
 
 def _check_table(cache, B):
@@ -422,9 +431,24 @@ def _int32_pair(x, shape, device):
         dev = host.to(device)
     host = host.reshape(shape)
     dev = dev.reshape(shape)
-    if host.dtype != torch.int32 or dev.dtype != torch.int32 or not host.is_contiguous() or not dev.is_contiguous():
-        raise ValueError("int32 contiguous arrays expected")
+    _check_pair("lengths and starts", host, dev)
     return host, dev
+
+
+def _offsets(block_offsets, device):
+    """(host, device) int32 block offsets and the number of blocks."""
+    if isinstance(block_offsets, tuple):
+        host, dev = block_offsets
+    else:
+        host = torch.as_tensor(block_offsets, dtype=torch.int32).cpu().contiguous()
+        dev = host.to(device)
+    return host, dev, host.shape[-1] - 1
+
+
+def _check_offsets(host, dev, B, nb):
+    if tuple(host.shape) != (B, nb + 1) or tuple(dev.shape) != (B, nb + 1):
+        raise ValueError("block_offsets must be [B][num_blocks + 1]")
+    _check_pair("block_offsets", host, dev)
 
 
 def block_causal_attn_fwd(q, k_new, v_new, cache, cache_lens, scale=None, fuse_append=False,
@@ -584,12 +608,7 @@ def block_causal_prefill(q, k, v, block_offsets, scale=None, cache=None, num_kv_
             _check(rc)
         return (out, lse) if want_lse else out
     B, L, Hq, D = q.shape
-    if isinstance(block_offsets, tuple):
-        off_h, off_d = block_offsets
-    else:
-        off_h = torch.as_tensor(block_offsets, dtype=torch.int32).cpu().contiguous()
-        off_d = off_h.to(q.device)
-    nb = off_h.shape[-1] - 1
+    off_h, off_d, nb = _offsets(block_offsets, q.device)
     if k is not None:
         hkv = k.shape[2]
     else:
@@ -607,8 +626,7 @@ def block_causal_prefill(q, k, v, block_offsets, scale=None, cache=None, num_kv_
         _check_table(cache, B)
     _shape("out", out, (B, L, Hq, D))
     _shape("lse", lse, (B, Hq, L))
-    if tuple(off_h.shape) != (B, nb + 1) or tuple(off_d.shape) != (B, nb + 1):
-        raise ValueError("block_offsets must be [B][num_blocks + 1]")
+    _check_offsets(off_h, off_d, B, nb)
     desc = cache.desc() if cache is not None else None
     kvp = ctypes.byref(desc) if desc is not None else None
     if window is not None:
@@ -653,19 +671,13 @@ def block_causal_prefill_bwd(q, k, v, o, dout, lse, block_offsets, scale=None, t
         return got[1:]
     B, L, Hq, D = q.shape
     hkv = k.shape[2]
-    if isinstance(block_offsets, tuple):
-        off_h, off_d = block_offsets
-    else:
-        off_h = torch.as_tensor(block_offsets, dtype=torch.int32).cpu().contiguous()
-        off_d = off_h.to(q.device)
-    nb = off_h.shape[-1] - 1
+    off_h, off_d, nb = _offsets(block_offsets, q.device)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
     for name, t, shp in (("k", k, (B, L, hkv, D)), ("v", v, (B, L, hkv, D)), ("o", o, (B, L, Hq, D)),
                          ("dout", dout, (B, L, Hq, D)), ("lse", lse, (B, Hq, L))):
         _shape(name, t, shp)
-    if tuple(off_h.shape) != (B, nb + 1) or tuple(off_d.shape) != (B, nb + 1):
-        raise ValueError("block_offsets must be [B][num_blocks + 1]")
+    _check_offsets(off_h, off_d, B, nb)
     if dq is None:
         dq = torch.empty((B, L, Hq, D), dtype=grad_dtype, device=q.device)
     if dk is None:

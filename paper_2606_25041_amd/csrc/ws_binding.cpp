@@ -121,11 +121,10 @@ bool token_tensor(const at::Tensor *t, std::initializer_list<int64_t> shape, ws_
 
 struct Ints {
     const int32_t *host = nullptr, *dev = nullptr;
-    const at::Tensor *h = nullptr;
 };
 
-// a (host, device) pair of int32 arrays of the given shape (packed: any shape
-// of that many contiguous elements); None gives null pointers (so an empty
+// a (host, device) pair of contiguous int32 arrays of the given shape (packed:
+// of any shape of that many elements); None gives null pointers (so an empty
 // array, whose pointers are null too, is declined)
 bool int_pair(PyObject *o, std::initializer_list<int64_t> shape, bool packed, Ints &x) {
     if (o == Py_None) return true;
@@ -136,12 +135,11 @@ bool int_pair(PyObject *o, std::initializer_list<int64_t> shape, bool packed, In
     if (numel == 0) return false;
     for (const at::Tensor *p : t) {
         if (!p || p->scalar_type() != at::kInt) return false;
-        if (packed ? (p->numel() != numel || !p->is_contiguous()) : !shaped(*p, shape)) return false;
+        if (!p->is_contiguous() || (packed ? p->numel() != numel : !shaped(*p, shape))) return false;
     }
     if (!t[0]->is_cpu() || !t[1]->is_cuda()) return false;
     x.host = (const int32_t *)t[0]->data_ptr();
     x.dev = (const int32_t *)t[1]->data_ptr();
-    x.h = t[0];
     return true;
 }
 
@@ -402,7 +400,7 @@ PyObject *step_of(PyObject *const *a, const Window &win, bool four = false) {
             wn = wsp->numel();
         } else if (!noalloc) {
             int32_t most = 0;
-            for (int64_t b = 0; b < B; ++b) most = std::max(most, lens.host[b * lens.h->stride(0)]);
+            for (int64_t b = 0; b < B; ++b) most = std::max(most, lens.host[b]);
             wn = four ? abi4.step_bytes(B, H, hkv, L, lens.host, nl.host)
                : win.window >= 0 ? wabi.step_bytes(B, H, hkv, L, lens.host, nl.host, win.sinks, win.window)
                : nl.host ? abi.workspace_bytes_varlen(B, H, hkv, L, lens.host, nl.host)
