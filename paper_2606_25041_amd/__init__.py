@@ -224,6 +224,13 @@ def _shape(name, t, shape):
         raise ValueError(f"{name} must be a device tensor")
 
 
+def _check_lse(lse, shape):
+    """The library takes a pointer to packed f32 values."""
+    _shape("lse", lse, shape)
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous()):
+        raise ValueError("lse must be contiguous f32")
+
+
 def _stream():
     return torch.cuda.current_stream().cuda_stream
 
@@ -494,7 +501,7 @@ def block_causal_attn_fwd(q, k_new, v_new, cache, cache_lens, scale=None, fuse_a
     _shape("k_new", k_new, (B, Lq, cache.num_kv_heads, D))
     _shape("v_new", v_new, (B, Lq, cache.num_kv_heads, D))
     _shape("out", out, (B, Lq, Hq, D))
-    _shape("lse", lse, (B, Hq, Lq))
+    _check_lse(lse, (B, Hq, Lq))
     if D != cache.head_dim:
         raise ValueError("q head_dim differs from the cache's")
     _check_lens(host, dev, B)
@@ -575,7 +582,7 @@ def block_causal_attn_fwd_noalloc(q, k_new, v_new, cache, cache_lens, out, lse=N
     _shape("k_new", k_new, (B, Lq, cache.num_kv_heads, D))
     _shape("v_new", v_new, (B, Lq, cache.num_kv_heads, D))
     _shape("out", out, (B, Lq, Hq, D))
-    _shape("lse", lse, (B, Hq, Lq))
+    _check_lse(lse, (B, Hq, Lq))
     if D != cache.head_dim:
         raise ValueError("q head_dim differs from the cache's")
     _check_lens(host, dev, B)
@@ -625,7 +632,7 @@ def block_causal_prefill(q, k, v, block_offsets, scale=None, cache=None, num_kv_
     else:
         _check_table(cache, B)
     _shape("out", out, (B, L, Hq, D))
-    _shape("lse", lse, (B, Hq, L))
+    _check_lse(lse, (B, Hq, L))
     _check_offsets(off_h, off_d, B, nb)
     desc = cache.desc() if cache is not None else None
     kvp = ctypes.byref(desc) if desc is not None else None
@@ -675,8 +682,9 @@ def block_causal_prefill_bwd(q, k, v, o, dout, lse, block_offsets, scale=None, t
     if scale is None:
         scale = 1.0 / math.sqrt(D)
     for name, t, shp in (("k", k, (B, L, hkv, D)), ("v", v, (B, L, hkv, D)), ("o", o, (B, L, Hq, D)),
-                         ("dout", dout, (B, L, Hq, D)), ("lse", lse, (B, Hq, L))):
+                         ("dout", dout, (B, L, Hq, D))):
         _shape(name, t, shp)
+    _check_lse(lse, (B, Hq, L))
     _check_offsets(off_h, off_d, B, nb)
     if dq is None:
         dq = torch.empty((B, L, Hq, D), dtype=grad_dtype, device=q.device)

@@ -231,6 +231,8 @@ bool given(PyObject *o, std::initializer_list<int64_t> shape, at::Tensor &t) {
     return true;
 }
 
+bool packed_f32(const at::Tensor &t) { return t.scalar_type() == at::kFloat && t.is_contiguous(); }
+
 // A new output of the given shape where the caller gave none
 void allocate(at::Tensor &t, std::initializer_list<int64_t> shape, at::ScalarType type, const at::Tensor &like) {
     if (!t.defined()) t = at::empty(at::IntArrayRef(shape), like.options().dtype(type));
@@ -383,7 +385,7 @@ PyObject *step_of(PyObject *const *a, const Window &win, bool four = false) {
     at::Tensor out, lse, own;
     const bool with_lse = want_lse || a[10] != Py_None;
     if (!given(a[7], {B, L, H, D}, out) || (out.defined() && !token_tensor(&out, {B, L, H, D}, od)) ||
-        !given(a[10], {B, H, L}, lse))
+        !given(a[10], {B, H, L}, lse) || (lse.defined() && !packed_f32(lse)))
         Py_RETURN_NONE;
     const int flags = fuse ? WS_FUSE_APPEND : 0;
     int rc;
@@ -496,7 +498,7 @@ PyObject *prefill_of(PyObject *const *a, const Window &win) {
     at::Tensor out, lse;
     const bool with_lse = want_lse || a[10] != Py_None;
     if (!given(a[7], {B, L, H, D}, out) || (out.defined() && !token_tensor(&out, {B, L, H, D}, od)) ||
-        !given(a[10], {B, H, L}, lse))
+        !given(a[10], {B, H, L}, lse) || (lse.defined() && !packed_f32(lse)))
         Py_RETURN_NONE;
     const ws_paged_kv *kvp = a[5] != Py_None ? &kv : nullptr;
     int rc;
@@ -543,7 +545,7 @@ PyObject *prefill_bwd_of(PyObject *const *a, const Window &win, at::ScalarType g
     float scale;
     if (!token_tensor(q, {B, L, H, D}, qd) || !token_tensor(k, {B, L, hkv, D}, kd) ||
         !token_tensor(tensor(a[2]), {B, L, hkv, D}, vd) || !token_tensor(tensor(a[3]), {B, L, H, D}, od) ||
-        !token_tensor(tensor(a[4]), {B, L, H, D}, dd) || !lse->is_cuda() || !shaped(*lse, {B, H, L}) ||
+        !token_tensor(tensor(a[4]), {B, L, H, D}, dd) || !lse->is_cuda() || !shaped(*lse, {B, H, L}) || !packed_f32(*lse) ||
         !scale_of(a[7], D, scale) || !PyTuple_CheckExact(a[6]) || PyTuple_GET_SIZE(a[6]) != 2)
         Py_RETURN_NONE;
     const at::Tensor *oh = tensor(PyTuple_GET_ITEM(a[6], 0));
