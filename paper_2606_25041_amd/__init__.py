@@ -328,6 +328,15 @@ def _check_lens(host, dev, B):
 def _check_table(cache, B):
     if cache.page_table_host.shape[0] < B or cache.page_table.shape != cache.page_table_host.shape:
         raise ValueError("page table has fewer rows than the batch")
+    _check_pair("page table", cache.page_table_host, cache.page_table)
+    pools, size = ((cache.pool,), 1) if isinstance(cache, PagedCache4) else ((cache.k_pool, cache.v_pool), 2)
+    if not all(p.is_cuda and p.is_contiguous() and p.element_size() == size for p in pools):
+        raise ValueError("cache pools must be contiguous device tensors of their type")
+
+
+def _check_workspace(workspace):
+    if workspace is not None and (not workspace.is_cuda or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous device tensor")
 
 
 def workspace_bytes(op, batch, num_q_heads, num_kv_heads, max_q, max_k):
@@ -498,6 +507,7 @@ def block_causal_attn_fwd(q, k_new, v_new, cache, cache_lens, scale=None, fuse_a
         out = torch.empty((B, Lq, Hq, D), dtype=out_dtype, device=q.device)
     if want_lse and lse is None:
         lse = torch.empty((B, Hq, Lq), dtype=torch.float32, device=q.device)
+    _shape("q", q, (B, Lq, Hq, D))
     _shape("k_new", k_new, (B, Lq, cache.num_kv_heads, D))
     _shape("v_new", v_new, (B, Lq, cache.num_kv_heads, D))
     _shape("out", out, (B, Lq, Hq, D))
@@ -519,6 +529,7 @@ def block_causal_attn_fwd(q, k_new, v_new, cache, cache_lens, scale=None, fuse_a
         need = workspace_bytes(WS_OP_STEP, B, Hq, cache.num_kv_heads, Lq, int(host.max().item()) + Lq)
     else:
         need = step_workspace_bytes_varlen(B, Hq, cache.num_kv_heads, Lq, host, nl[0])
+    _check_workspace(workspace)
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     ws_ptr = _ptr(workspace)
@@ -579,6 +590,7 @@ def block_causal_attn_fwd_noalloc(q, k_new, v_new, cache, cache_lens, out, lse=N
     host, dev = cache_lens
     if scale is None:
         scale = 1.0 / math.sqrt(D)
+    _shape("q", q, (B, Lq, Hq, D))
     _shape("k_new", k_new, (B, Lq, cache.num_kv_heads, D))
     _shape("v_new", v_new, (B, Lq, cache.num_kv_heads, D))
     _shape("out", out, (B, Lq, Hq, D))
@@ -626,6 +638,7 @@ def block_causal_prefill(q, k, v, block_offsets, scale=None, cache=None, num_kv_
         out = torch.empty((B, L, Hq, D), dtype=out_dtype, device=q.device)
     if want_lse and lse is None:
         lse = torch.empty((B, Hq, L), dtype=torch.float32, device=q.device)
+    _shape("q", q, (B, L, Hq, D))
     if k is not None or v is not None:
         _shape("k", k, (B, L, hkv, D))
         _shape("v", v, (B, L, hkv, D))
@@ -681,7 +694,7 @@ def block_causal_prefill_bwd(q, k, v, o, dout, lse, block_offsets, scale=None, t
     off_h, off_d, nb = _offsets(block_offsets, q.device)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
-    for name, t, shp in (("k", k, (B, L, hkv, D)), ("v", v, (B, L, hkv, D)), ("o", o, (B, L, Hq, D)),
+    for name, t, shp in (("q", q, (B, L, Hq, D)), ("k", k, (B, L, hkv, D)), ("v", v, (B, L, hkv, D)), ("o", o, (B, L, Hq, D)),
                          ("dout", dout, (B, L, Hq, D))):
         _shape(name, t, shp)
     _check_lse(lse, (B, Hq, L))
@@ -699,6 +712,7 @@ def block_causal_prefill_bwd(q, k, v, o, dout, lse, block_offsets, scale=None, t
     if B > 0 and L > 0:
         need = workspace_bytes(WS_OP_PREFILL_BWD, B, Hq, hkv, L, L) if window is None else \
             library().ws_prefill_window_bwd_workspace_bytes(B, Hq, hkv, L, sinks, window)
+    _check_workspace(workspace)
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     th = td = None

@@ -152,6 +152,16 @@ struct NoGil {
 PyObject *names[7];   // attribute names of PagedCache, in the order below
 PyObject *pool_name;  // PagedCache4: "pool" in place of the first two
 
+// a contiguous device tensor (of elements of `size` bytes; 0: any)
+bool packed(const at::Tensor *t, int64_t size) {
+    return t && t->is_cuda() && t->is_contiguous() && (!size || (int64_t)t->element_size() == size);
+}
+// both copies of a page table of at least `batch` rows
+bool table(const at::Tensor *h, const at::Tensor *d, int64_t batch) {
+    return h && d && h->dim() == 2 && h->size(0) >= batch && d->sizes() == h->sizes() && h->scalar_type() == at::kInt &&
+           d->scalar_type() == at::kInt && h->is_contiguous() && d->is_contiguous() && h->is_cpu() && d->is_cuda();
+}
+
 // The paged cache's descriptor, with its table checked for `batch` rows.  The
 // cache's tensors are held: without the GIL another thread may replace them.
 struct Paged : ws_paged_kv {
@@ -170,8 +180,8 @@ bool paged(PyObject *cache, int64_t batch, Paged &d) {
         vp = tensor(v[1]);
         th = tensor(v[2]);
         td = tensor(v[3]);
-        ok = k && vp && th && td && th->dim() == 2 && th->size(0) >= batch && td->sizes() == th->sizes() &&
-             PyLong_CheckExact(v[4]) && PyLong_CheckExact(v[5]) && PyLong_CheckExact(v[6]);
+        ok = packed(k, 2) && packed(vp, 2) && table(th, td, batch) && PyLong_CheckExact(v[4]) && PyLong_CheckExact(v[5]) &&
+             PyLong_CheckExact(v[6]);
     }
     if (ok) {
         static_cast<ws_paged_kv &>(d) = ws_paged_kv{k->data_ptr(), vp->data_ptr(), (const int32_t *)td->data_ptr(), (const int32_t *)th->data_ptr(),
@@ -195,8 +205,8 @@ bool paged4(PyObject *cache, int64_t batch, Paged4 &d) {
     if (!ok) PyErr_Clear();
     if (ok) {
         const at::Tensor *p = tensor(v[0]), *th = tensor(v[1]), *td = tensor(v[2]);
-        ok = p && th && td && p->is_cuda() && th->dim() == 2 && th->size(0) >= batch && td->sizes() == th->sizes() &&
-             PyLong_CheckExact(v[3]) && PyLong_CheckExact(v[4]) && PyLong_CheckExact(v[5]);
+        ok = packed(p, 1) && table(th, td, batch) && PyLong_CheckExact(v[3]) && PyLong_CheckExact(v[4]) &&
+             PyLong_CheckExact(v[5]);
         if (ok) {
             static_cast<ws_paged_kv4 &>(d) =
                 ws_paged_kv4{p->data_ptr(), (const int32_t *)td->data_ptr(), (const int32_t *)th->data_ptr(),
@@ -381,7 +391,7 @@ PyObject *step_of(PyObject *const *a, const Window &win, bool four = false) {
     const at::ScalarType type = a[7] == Py_None ? dtype_of(a[8]) : at::kBFloat16;
     if (type != at::kBFloat16 && type != at::kFloat) Py_RETURN_NONE;
     const at::Tensor *wsp = a[11] == Py_None ? nullptr : tensor(a[11]);
-    if (a[11] != Py_None && !wsp) Py_RETURN_NONE;
+    if (a[11] != Py_None && !packed(wsp, 0)) Py_RETURN_NONE;
     at::Tensor out, lse, own;
     const bool with_lse = want_lse || a[10] != Py_None;
     if (!given(a[7], {B, L, H, D}, out) || (out.defined() && !token_tensor(&out, {B, L, H, D}, od)) ||
@@ -553,7 +563,7 @@ PyObject *prefill_bwd_of(PyObject *const *a, const Window &win, at::ScalarType g
     const int64_t nb = oh->size(1) - 1;
     if (nb < 0 || !int_pair(a[6], {B, nb + 1}, false, off) || !int_pair(a[8], {B, nb}, true, text)) Py_RETURN_NONE;
     const at::Tensor *wsp = a[12] == Py_None ? nullptr : tensor(a[12]);
-    if (a[12] != Py_None && !wsp) Py_RETURN_NONE;
+    if (a[12] != Py_None && !packed(wsp, 0)) Py_RETURN_NONE;
     at::Tensor dq, dk, dv, own;
     if (!given(a[9], {B, L, H, D}, dq) || (dq.defined() && !token_tensor(&dq, {B, L, H, D}, dqd)) ||
         !given(a[10], {B, L, hkv, D}, dk) || (dk.defined() && !token_tensor(&dk, {B, L, hkv, D}, dkd)) ||
