@@ -211,7 +211,8 @@ int ws_kv_append(const ws_paged_kv *kv, int32_t batch,
  *                kv->num_kv_heads, new_len, max_b cache_lens[b] + new_len)
  *                bytes (NULL allowed when that is 0); its contents on entry
  *                are ignored.
- * new_len x (num_q_heads / num_kv_heads) must not exceed 2^30 (WS_ERR_SHAPE).
+ * new_len x (num_q_heads / num_kv_heads) must not exceed 2^30, nor
+ * cache_lens[b] + new_len 2^31 - 129 (WS_ERR_SHAPE).
  * The library splits long caches into KV partitions merged by a second
  * launch.  The partition count is planned for the compute units of the
  * current device (queried once per device; ws_step_plan shows the plan for

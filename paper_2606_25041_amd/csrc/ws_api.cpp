@@ -1238,8 +1238,8 @@ int step_impl(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new, const ws_paged_k
         }
         if (n + nl > max_k) max_k = n + nl;
     }
-    // (windows: the table may be all but empty, so key positions can come near 2^31; a tile past them must not)
-    if (max_k > INT32_MAX - (win ? 128 : 0)) return fail(WS_ERR_SHAPE, "too many keys");
+    // (pages may be shared, or behind a window gone, so key positions can come near 2^31; a tile past them must not)
+    if (max_k > INT32_MAX - 128) return fail(WS_ERR_SHAPE, "too many keys");
     if (text_host)
         for (int b = 0; b < batch; ++b)
             if (text_host[b] < 0 || text_host[b] > new_len)

@@ -5,6 +5,7 @@ import ctypes
 import numpy as np
 import pytest
 
+import paper_2606_25041_amd as ws
 from tests import session_plan_probe as probe
 
 OK, SHAPE = 0, 2
@@ -44,3 +45,24 @@ def test_gradients(window):
         return lib.ws_workspace_bytes(3, 1, 1, 1, seq, seq)
     assert need(2 ** 30 - 1) >= 8 * (2 ** 30 - 1)
     assert need(2 ** 30) == need(2 ** 31 - 1) == 0
+
+
+@pytest.mark.parametrize("window", (None, 2 ** 31 - 1))
+def test_steps(window):
+    """The key tile that holds the last token ends below 2^31 (pages may be
+    shared, so memory is no limit: 2^25 table entries of one page)."""
+    lib, new, fake = probe._lib(), 3, 0x10000
+    lib.probe_cus(256)
+    table = np.zeros((1, 2 ** 25), np.int32)
+    kv = ws.PagedKVDesc(fake, fake, fake, table.ctypes.data, 1, 64, table.shape[1], 1, 64)
+    t = ws.Tensor4(fake, ws.WS_DTYPE_BF16, new * 64, 64, 64)
+    last = 2 ** 31 - 1 - 128
+    for n, want in ((last - new, OK), (last - new + 1, SHAPE), (2 ** 31 - 1 - new, SHAPE), (2 ** 31 - 1, SHAPE)):
+        lens = np.array([n], np.int32)
+        head = (t, t, t, ctypes.byref(kv), ctypes.c_void_p(lens.ctypes.data), ctypes.c_void_p(fake))
+        tail = (ctypes.c_float(0.1), 0, t, None, ctypes.c_void_p(fake), ctypes.c_size_t(1 << 40), None)
+        if window is None:
+            got = lib.ws_block_causal_attn_fwd(*head, 1, new, 1, *tail)
+        else:
+            got = lib.ws_block_causal_attn_fwd_window(*head, None, None, None, None, 1, new, 1, 0, window, *tail)
+        assert got == want, n
