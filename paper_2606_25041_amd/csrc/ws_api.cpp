@@ -15,7 +15,7 @@
 
 #include "ws_host.h"
 
-namespace ws {
+namespace ws __attribute__((visibility("hidden"))) {
 
 thread_local char g_err[512];
 
@@ -1031,7 +1031,7 @@ size_t ws_prefill_window_bwd_workspace_bytes(int32_t batch, int32_t num_q_heads,
 
 }  // extern "C"
 
-namespace ws {
+namespace ws __attribute__((visibility("hidden"))) {
 
 // Gradients of a whole sequence (win nullptr: no window).
 int bwd_impl(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 o, ws_tensor4 dout, const float *lse,

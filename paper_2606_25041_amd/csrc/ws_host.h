@@ -8,7 +8,8 @@
 #include "../../include/ws_attn.h"
 #include "ws_kernels.h"
 
-namespace ws {
+// (hidden: not for a program that the library is linked into)
+namespace ws __attribute__((visibility("hidden"))) {
 
 // The reason of a status for ws_last_error (this thread's); returns status.
 int fail(int status, const char *fmt, ...);
