@@ -245,7 +245,8 @@ int ws_block_causal_attn_fwd(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new,
  * WS_ERR_WORKSPACE.  Every call on a device shares that device's array and
  * nothing in it needs to start at zero (each call writes the partials it
  * reads); calls that may overlap on one device (unordered streams) race on
- * it and give undefined results, so order them.
+ * it and give undefined results, so order them.  Steps through a window or over
+ * a 4-bit cache have no such form: they take a workspace.
  */
 #define WS_NOALLOC_SCRATCH_BYTES ((size_t)32 << 20)
 int ws_block_causal_attn_fwd_noalloc(ws_tensor4 q, ws_tensor4 k_new, ws_tensor4 v_new,
@@ -408,7 +409,9 @@ int ws_block_causal_prefill_text(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v,
  *               (rounded up to 256) + 4 * batch * seq_len are enough to run,
  *               unsplit
  * The gradients are deterministic (fixed summation order for a given shape,
- * device and size of workspace; no atomics).
+ * device and size of workspace; no atomics).  P and dS enter their products
+ * rounded to bf16 (2^-8 of themselves) and the sums are f32: the gradients, f32
+ * ones too, have the accuracy of bf16 operands.
  * seq_len must be below 2^30 (WS_ERR_SHAPE).
  * Errors: WS_ERR_NULL, WS_ERR_SHAPE, WS_ERR_UNSUPPORTED, WS_ERR_ALIGN,
  * WS_ERR_HEADS, WS_ERR_OFFSETS, WS_ERR_WORKSPACE, WS_ERR_HIP.
@@ -433,7 +436,8 @@ int ws_block_causal_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_ten
  * entries of the pages between may hold anything, so a caller can free or
  * reuse those pages (WS_FUSE_APPEND also needs the new tokens' pages).
  * f32 outputs hold f32 accuracy here (the softmax weights enter the product
- * with V as the sum of three bf16 values).  Of a bf16 output that is merged from
+ * with V as the sum of three bf16 values; those of a bf16 output as one, off by
+ * at most 2^-8 of itself).  Of a bf16 output that is merged from
  * KV splits, elements below 2^-39 of their row's largest may be lost (the
  * partials are f16 values under one power of two per row).  workspace: at least
  * ws_step_workspace_bytes_window(...) bytes for the same arguments.
@@ -484,7 +488,7 @@ int ws_block_causal_prefill_window(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v,
  *   workspace:     ws_prefill_window_bwd_workspace_bytes(...) bytes, 16-byte
  *                  aligned; 8 * batch * num_q_heads * seq_len bytes (rounded
  *                  up to 256) + 8 * batch * seq_len are enough to run, unsplit
- * Deterministic, as ws_block_causal_prefill_bwd.
+ * Deterministic, and as exact, as ws_block_causal_prefill_bwd.
  */
 int ws_block_causal_prefill_window_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 o,
                                        ws_tensor4 dout, const float *lse,

@@ -674,7 +674,8 @@ def block_causal_prefill_bwd(q, k, v, o, dout, lse, block_offsets, scale=None, t
     [B][L][Hkv][d]).  o and lse are the forward's output and lse;
     text_starts, window and sinks as in ``block_causal_prefill``.
     grad_dtype: dtype of the gradients allocated here; bf16 with a window
-    only (the f32 sums rounded once)."""
+    only (the f32 sums rounded once).  f32 gradients have the accuracy of bf16
+    operands (the weights and their gradients enter the products in bf16)."""
     window, sinks = _window(window, sinks)
     if window is None:
         if grad_dtype != torch.float32:

@@ -60,8 +60,8 @@ int64_t tile_keys(int batch, int new_len, const int32_t *cache_lens, const int32
 }
 
 // A step of few packed rows: tiles in one line per KV head, an even share for
-// each work-group, one work-group per compute unit (its LDS tiles allow one);
-// a share is at least a tile per wave.
+// each work-group, one work-group per compute unit (its LDS tiles at head dim 128
+// and its registers at 64 allow one); a share is at least a tile per wave.
 Few4Plan plan_few(int num_cus, int batch, int hkv, int G, int new_len, const int32_t *cache_lens, const int32_t *nl) {
     Few4Plan p{};
     p.nrb = (G * new_len + 31) / 32;
@@ -85,15 +85,18 @@ Few4Plan plan_few(int num_cus, int batch, int hkv, int G, int new_len, const int
 // kernel's 256 rows share one reading; but its work divides evenly, and over all
 // compute units where the common kernel has at most 32 splits per stream.  Both
 // times in units of 0.17 us: a tile of a work-group's share 0.34 us, a stream's
-// part in it 4, its launch 3, the merge 5; of the common kernel's T tiles by its plan each
-// 1.7 us up to 128 rows in one common count of splits (half its waves idle), else
-// 2.2.  Few rows against the common kernel: 4 x 131072 tokens, GQA 64/8 x 128: 40
-// rows 202 us and 393, 160 rows 480 and 537, 256 rows 689 and 616; MHA 24: 150
-// rows 1.39 ms and 1.58, 200 rows 2.49 and 1.71 (168 of 256 compute units); one
-// stream, 8/1 x 128: 256 rows 41 us and 168; 32 streams of 100 tokens, 64/8, one
-// token each: 27 and 11.  Of 809 steps of 1 to 520 rows over one to 32 streams
-// (few rows up to 128, the common kernel past them, against this choice) 72 run
-// more than 1.5 times as fast, 8 below 0.95 (least 0.82).
+// part in it 4, its launch 3, the merge 5; of the common kernel's T tiles by its
+// plan each 1.7 us up to 128 rows in one common count of splits (half its waves
+// idle), else 2.2.  (Fitted at head dim 128 and bf16 output; the choice was timed
+// at 64 and with f32 output too, below.)  Few rows against the common kernel: 4 x
+// 131072 tokens, GQA 64/8 x 128: 40 rows 202 us and 393, 160 rows 480 and 537,
+// 256 rows 689 and 616; MHA 24: 150 rows 1.39 ms and 1.58, 200 rows 2.49 and 1.71
+// (168 of 256 compute units); one stream, 8/1 x 128: 256 rows 41 us and 168; 32
+// streams of 100 tokens, 64/8, one token each: 27 and 11.  Of 809 steps of 1 to
+// 520 rows over one to 32 streams (few rows up to 128, the common kernel past
+// them, against this choice) 73 run more than 1.5 times as fast, 8 below 0.95
+// (least 0.82); of the 135 at head dim 64 15 and one (0.87), of the 161 with f32
+// output 14 and none.
 bool few_rows(int num_cus, int batch, int hq, int hkv, int new_len, const int32_t *cache_lens, const int32_t *nl,
               Few4Plan &line) {
     const int G = hq / hkv, rows = G * new_len;

@@ -29,7 +29,10 @@ constexpr int AH = 2;         // LDS operand reads issued this many MFMAs ahead
 // (S = Q K^T with the keys as columns, so P and dS are B operands of
 // dV^T += dO^T P and dK^T += Q^T dS).  Each sums in a fixed order: the
 // gradients are deterministic, and dK/dV sum the G query heads of their KV
-// head inside one work-group.
+// head inside one work-group.  P and dS enter their products rounded to bf16
+// (2^-8 of themselves; in more bits each product would take two or three MFMAs
+// for one), and D_i comes from the bf16 output: sums are f32, but an f32 gradient
+// is as exact as bf16 operands make it, like a bf16 one before its last rounding.
 
 // byte offset of 16-byte chunk c of row r in an LDS tile of [rows][D] bf16
 // (the forward's swizzle)
@@ -346,7 +349,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // WIN (sliding window with sinks): a key is seen by the rows up to the last
 // whose window reaches it, so the chunks are counted from that row instead of
 // the sequence end; a key tile with sinks is seen to the end, and its parts
-// are separate work-groups (BwdArgs), the heaviest, dispatched first.
+// are separate work-groups (BwdArgs), the heaviest, dispatched first.  It spills 7
+// scalars at D = 128 (none without) and 87 at 64 (26 without).
 template <int D, bool WIN, bool BF16>
 __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     constexpr int ROWB = 2 * D, KK = D / 16, MD = D / 32;

@@ -69,6 +69,11 @@ int launch_cache4(const Cache4Args &a, hipStream_t st) {
 //  * A tile's loads are issued a whole tile ahead, into registers.
 // At the end of a stream's part the waves' sums meet in LDS; a stream of several
 // parts writes f32 partials, which few4_merge_kernel joins.
+// One work-group runs per compute unit: at 128 head dims its LDS (130 KiB) and
+// its 256 vector registers allow no second one (34 scalars are spilled, with f32
+// output four vector registers to scratch as well), at 64 its 212 to 218 vector
+// registers do not (12 scalars spilled).  The weights of a bf16 output enter the
+// product with V in bf16: 2^-8 each, the size of the output's own rounding.
 constexpr int KT4 = 64;
 
 template <int D, bool F32>

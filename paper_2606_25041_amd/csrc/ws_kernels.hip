@@ -62,7 +62,7 @@ constexpr int NSTAGE = 5;            // K/V tiles resident in the LDS ring (load
 constexpr int RAHEAD = 4;            // LDS operand reads issued this many MFMAs ahead
 
 // Partials of a bf16 output held as f16 (HALF): a row's values are divided by a
-// power of two that puts the largest in [2^14, 2^15), so they are off by 2^-12
+// power of two that puts the largest in [2^14, 2^15), so they are off by 2^-11
 // of themselves (or 2^-39 of the row's largest).  unit: the power of two
 // (held where both it and its reciprocal are normal); inv: the row's factor,
 // divided by it.  An infinity or a NaN stays one.
@@ -120,7 +120,9 @@ __device__ __forceinline__ void append_share4(const AttnArgs &a, int b, int kvh,
 // split step 22, per-stream 45 to 49; one kernel for all had 22) and none of
 // the others' code through the instruction cache, where short launches spend
 // their time.  Prefill of 2 x 16384 tokens 3.93 -> 3.76 ms; its loop still reads
-// five spilled scalars back per tile.
+// five spilled scalars back per tile.  Steps over a 4-bit cache spill 30 to 32
+// scalars, with per-stream splits 54 to 72, and at 128 head dims with f32 output
+// four vector registers to scratch as well; windowed kernels at most one scalar.
 enum Kind { PREFILL_CONTIGUOUS, PREFILL_PAGED, STEP, STEP_SPLIT, STEP_RAGGED, STEP_CACHE4, STEP_CACHE4_RAGGED };
 
 // STEP_SPLIT: every item writes partials, none rows of the output.
