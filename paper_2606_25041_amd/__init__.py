@@ -215,6 +215,11 @@ def _t4(t):
     return Tensor4(t.data_ptr(), dt, t.stride(0), t.stride(1), t.stride(2))
 
 
+def _here(t):
+    """On the current device, whose stream the library launches on."""
+    return t.is_cuda and t.device.index == torch.cuda.current_device()
+
+
 def _shape(name, t, shape):
     """Shapes are checked here because the C ABI only sees pointers and
     strides: a tensor smaller than the call implies would be read past its end."""
@@ -222,6 +227,8 @@ def _shape(name, t, shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t is not None and not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+    if t is not None and not _here(t):
+        raise ValueError(f"{name} must be on the current device")
 
 
 def _check_lse(lse, shape):
@@ -315,8 +322,8 @@ def _check_pair(name, host, dev):
     """The library reads packed int32 arrays, one on either side."""
     if host.dtype != torch.int32 or dev.dtype != torch.int32 or not host.is_contiguous() or not dev.is_contiguous():
         raise ValueError(f"{name}: int32 contiguous arrays expected")
-    if host.device.type != "cpu" or not dev.is_cuda:
-        raise ValueError(f"{name} must be a (host, device) pair")
+    if host.device.type != "cpu" or not _here(dev):
+        raise ValueError(f"{name} must be a (host, device) pair of the current device")
 
 
 def _check_lens(host, dev, B):
@@ -330,13 +337,13 @@ def _check_table(cache, B):
         raise ValueError("page table has fewer rows than the batch")
     _check_pair("page table", cache.page_table_host, cache.page_table)
     pools, size = ((cache.pool,), 1) if isinstance(cache, PagedCache4) else ((cache.k_pool, cache.v_pool), 2)
-    if not all(p.is_cuda and p.is_contiguous() and p.element_size() == size for p in pools):
-        raise ValueError("cache pools must be contiguous device tensors of their type")
+    if not all(_here(p) and p.is_contiguous() and p.element_size() == size for p in pools):
+        raise ValueError("cache pools must be contiguous tensors of their type on the current device")
 
 
 def _check_workspace(workspace):
-    if workspace is not None and (not workspace.is_cuda or not workspace.is_contiguous()):
-        raise ValueError("workspace must be a contiguous device tensor")
+    if workspace is not None and (not _here(workspace) or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous tensor on the current device")
 
 
 def workspace_bytes(op, batch, num_q_heads, num_kv_heads, max_q, max_k):

@@ -14,6 +14,7 @@
 #include <torch/csrc/utils/object_ptr.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 
 #include <algorithm>
@@ -107,11 +108,16 @@ const at::Tensor *tensor(PyObject *o) {
     return t.defined() && t.layout() == at::kStrided && t.has_storage() ? &t : nullptr;
 }
 
+// The current device, whose stream the library launches on: asked once a call
+thread_local c10::DeviceIndex device_now;
+void ask_device() { device_now = c10::hip::current_device(); }
+bool here(const at::Tensor &t) { return t.is_cuda() && t.device().index() == device_now; }
+
 bool shaped(const at::Tensor &t, std::initializer_list<int64_t> shape) { return t.sizes() == at::IntArrayRef(shape); }
 
-// descriptor of a [B][L][H][d] device tensor with a contiguous last dim
+// descriptor of a [B][L][H][d] tensor of the current device with a contiguous last dim
 bool token_tensor(const at::Tensor *t, std::initializer_list<int64_t> shape, ws_tensor4 &d) {
-    if (!t || !t->is_cuda() || !shaped(*t, shape) || t->stride(3) != 1) return false;
+    if (!t || !here(*t) || !shaped(*t, shape) || t->stride(3) != 1) return false;
     const auto dt = t->scalar_type();
     if (dt != at::kBFloat16 && dt != at::kFloat) return false;
     d = ws_tensor4{t->data_ptr(), dt == at::kBFloat16 ? WS_DTYPE_BF16 : WS_DTYPE_F32, t->stride(0), t->stride(1),
@@ -137,7 +143,7 @@ bool int_pair(PyObject *o, std::initializer_list<int64_t> shape, bool packed, In
         if (!p || p->scalar_type() != at::kInt) return false;
         if (!p->is_contiguous() || (packed ? p->numel() != numel : !shaped(*p, shape))) return false;
     }
-    if (!t[0]->is_cpu() || !t[1]->is_cuda()) return false;
+    if (!t[0]->is_cpu() || !here(*t[1])) return false;
     x.host = (const int32_t *)t[0]->data_ptr();
     x.dev = (const int32_t *)t[1]->data_ptr();
     return true;
@@ -152,14 +158,14 @@ struct NoGil {
 PyObject *names[7];   // attribute names of PagedCache, in the order below
 PyObject *pool_name;  // PagedCache4: "pool" in place of the first two
 
-// a contiguous device tensor (of elements of `size` bytes; 0: any)
+// a contiguous tensor of the current device (of elements of `size` bytes; 0: any)
 bool packed(const at::Tensor *t, int64_t size) {
-    return t && t->is_cuda() && t->is_contiguous() && (!size || (int64_t)t->element_size() == size);
+    return t && here(*t) && t->is_contiguous() && (!size || (int64_t)t->element_size() == size);
 }
 // both copies of a page table of at least `batch` rows
 bool table(const at::Tensor *h, const at::Tensor *d, int64_t batch) {
     return h && d && h->dim() == 2 && h->size(0) >= batch && d->sizes() == h->sizes() && h->scalar_type() == at::kInt &&
-           d->scalar_type() == at::kInt && h->is_contiguous() && d->is_contiguous() && h->is_cpu() && d->is_cuda();
+           d->scalar_type() == at::kInt && h->is_contiguous() && d->is_contiguous() && h->is_cpu() && here(*d);
 }
 
 // The paged cache's descriptor, with its table checked for `batch` rows.  The
@@ -236,7 +242,7 @@ bool scale_of(PyObject *o, int64_t d, float &s) {
 bool given(PyObject *o, std::initializer_list<int64_t> shape, at::Tensor &t) {
     if (o == Py_None) return true;
     const at::Tensor *p = tensor(o);
-    if (!p || !p->is_cuda() || !shaped(*p, shape)) return false;
+    if (!p || !here(*p) || !shaped(*p, shape)) return false;
     t = *p;
     return true;
 }
@@ -289,6 +295,7 @@ PyObject *result(int rc, std::initializer_list<at::Tensor> out) {
 // append(cache, lens, k_new, v_new, new_lens) -> status, or None
 PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
+    ask_device();
     if (n != 5) Py_RETURN_NONE;
     const at::Tensor *k = tensor(a[2]);
     if (!k || k->dim() != 4) Py_RETURN_NONE;
@@ -313,6 +320,7 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // append4(cache, lens, k_new, v_new, new_lens) -> status, or None
 PyObject *append4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
+    ask_device();
     if (n != 5) Py_RETURN_NONE;
     const at::Tensor *k = tensor(a[2]);
     if (!k || k->dim() != 4) Py_RETURN_NONE;
@@ -336,6 +344,7 @@ PyObject *append4(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // read4(cache, starts, length, k, v) -> (status, k, v), or None
 PyObject *read4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
+    ask_device();
     if (n != 5 || !PyTuple_CheckExact(a[1]) || PyTuple_GET_SIZE(a[1]) != 2 || !PyLong_CheckExact(a[2])) Py_RETURN_NONE;
     const at::Tensor *h = tensor(PyTuple_GET_ITEM(a[1], 0));
     if (!h || h->dim() != 1) Py_RETURN_NONE;
@@ -368,6 +377,7 @@ PyObject *read4(PyObject *, PyObject *const *a, Py_ssize_t n) {
 //   -> (status, out, lse), or None
 // (step_window: and window, sinks; step4: a PagedCache4)
 PyObject *step_of(PyObject *const *a, const Window &win, bool four = false) {
+    ask_device();
     const at::Tensor *q = tensor(a[0]);
     if (!q || q->dim() != 4) Py_RETURN_NONE;
     const int64_t B = q->size(0), L = q->size(1), H = q->size(2), D = q->size(3);
@@ -468,6 +478,7 @@ PyObject *step4(PyObject *, PyObject *const *a, Py_ssize_t n) {
 //         want_lse, lse, text_starts) -> (status, out, lse), or None
 // (prefill_window: and window, sinks)
 PyObject *prefill_of(PyObject *const *a, const Window &win) {
+    ask_device();
     const at::Tensor *q = tensor(a[0]);
     if (!q || q->dim() != 4) Py_RETURN_NONE;
     const int64_t B = q->size(0), L = q->size(1), H = q->size(2), D = q->size(3);
@@ -546,6 +557,7 @@ PyObject *prefill_window(PyObject *, PyObject *const *a, Py_ssize_t n) {
 //             workspace) -> (status, dq, dk, dv), or None
 // (prefill_window_bwd: and window, sinks, grad_dtype)
 PyObject *prefill_bwd_of(PyObject *const *a, const Window &win, at::ScalarType grads) {
+    ask_device();
     const at::Tensor *q = tensor(a[0]), *k = tensor(a[1]), *lse = tensor(a[5]);
     if (!q || q->dim() != 4 || !k || k->dim() != 4 || !lse) Py_RETURN_NONE;
     const int64_t B = q->size(0), L = q->size(1), H = q->size(2), D = q->size(3), hkv = k->size(2);
@@ -555,7 +567,7 @@ PyObject *prefill_bwd_of(PyObject *const *a, const Window &win, at::ScalarType g
     float scale;
     if (!token_tensor(q, {B, L, H, D}, qd) || !token_tensor(k, {B, L, hkv, D}, kd) ||
         !token_tensor(tensor(a[2]), {B, L, hkv, D}, vd) || !token_tensor(tensor(a[3]), {B, L, H, D}, od) ||
-        !token_tensor(tensor(a[4]), {B, L, H, D}, dd) || !lse->is_cuda() || !shaped(*lse, {B, H, L}) || !packed_f32(*lse) ||
+        !token_tensor(tensor(a[4]), {B, L, H, D}, dd) || !here(*lse) || !shaped(*lse, {B, H, L}) || !packed_f32(*lse) ||
         !scale_of(a[7], D, scale) || !PyTuple_CheckExact(a[6]) || PyTuple_GET_SIZE(a[6]) != 2)
         Py_RETURN_NONE;
     const at::Tensor *oh = tensor(PyTuple_GET_ITEM(a[6], 0));

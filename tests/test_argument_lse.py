@@ -8,9 +8,12 @@ import torch
 import paper_2606_25041_amd as ws
 
 
-def test_dtype_and_layout():
-    def on_device(t):   # (the shape check asks for a device tensor)
-        return types.SimpleNamespace(shape=t.shape, is_cuda=True, dtype=t.dtype, is_contiguous=t.is_contiguous)
+def test_dtype_and_layout(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+
+    def on_device(t):   # (the shape check asks for a tensor of the current device)
+        return types.SimpleNamespace(shape=t.shape, is_cuda=True, dtype=t.dtype, is_contiguous=t.is_contiguous,
+                                     device=types.SimpleNamespace(index=0))
     good = torch.zeros(2, 3, 5)
     ws._check_lse(None, (2, 3, 5))
     ws._check_lse(on_device(good), (2, 3, 5))
