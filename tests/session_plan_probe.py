@@ -60,3 +60,23 @@ def prefill_window(hq, hkv, d, offsets, starts, window, sinks, paged=False, f32=
     assert _lib().reach_prefill_window(off.shape[0], hq, hkv, d, int(off[0, -1]), off.shape[1] - 1, _ptr(off), _ptr(text),
                                        sinks, window, int(paged), int(f32), ctypes.byref(kg)) == 0
     return kg.value
+
+
+def step_window_workspace(hq, hkv, d, new, caches, lens, window, sinks, f32=False, cus=256, given=-1):
+    """Status, workspace bytes written and asked for, and the plan."""
+    _lib().probe_cus(cus)
+    c, n, out = _ints(caches), _ints(lens), (ctypes.c_int * 5)()
+    used, need = ctypes.c_int64(0), ctypes.c_int64(0)
+    rc = _lib().used_step_window(len(c), hq, hkv, d, new, _ptr(c), _ptr(n), sinks, window, int(f32), ctypes.c_int64(given),
+                                 ctypes.byref(used), ctypes.byref(need), out)
+    return rc, used.value, need.value, (bool(out[2]), out[3])
+
+
+def step4_workspace(hq, hkv, d, new, caches, lens, f32=False, cus=256, given=-1):
+    """The same of a step over a 4-bit cache (plan: few rows, per-stream splits)."""
+    _lib().probe_cus(cus)
+    c, n, out = _ints(caches), _ints(lens), (ctypes.c_int * 5)()
+    used, need = ctypes.c_int64(0), ctypes.c_int64(0)
+    rc = _lib().used_step4(len(c), hq, hkv, d, new, _ptr(c), _ptr(n), int(f32), ctypes.c_int64(given), ctypes.byref(used),
+                           ctypes.byref(need), out)
+    return rc, used.value, need.value, (out[0] == 2, bool(out[2]))

@@ -2,6 +2,7 @@
 kernel and kind of plan at both head dims and output types, on 256 compute
 units."""
 import itertools
+import random
 
 import numpy as np
 import pytest
@@ -47,3 +48,39 @@ def test_windowed_prefills(paged, seed):
             assert probe.prefill_window(hq, hkv, d, off, starts, window, sinks, paged, f32) == groups
             seen.add((groups, d, f32))
     assert len(seen) == 8
+
+
+def test_windowed_steps_stay_in_the_workspace():
+    g = random.Random(11)
+    seen = set()
+    for cus in (256, 304, 32, 1):
+        for _ in range(300):
+            hkv, G, new = g.choice((1, 2, 3, 8, 24, 64, 300)), g.choice((1, 3, 4, 8, 16)), g.choice((1, 1, 2, 3, 17, 128, 512))
+            b, d, f32 = g.choice((1, 1, 2, 4, 31, 32, 33)), g.choice((64, 128)), g.random() < .5
+            caches = [g.choice((0, 1, 63, 64, 65, int(np.exp(g.uniform(0, 12))))) for _ in range(b)]
+            lens = [g.randint(1, new) for _ in range(b)] if g.random() < .5 else None
+            window, sinks = (g.choice((0, 1, int(np.exp(g.uniform(0, 12))), 2 ** 31 - 1)) for _ in range(2))
+            args = (hkv * G, hkv, d, new, caches, lens, window, sinks, f32, cus)
+            rc, used, need, plan = probe.step_window_workspace(*args)
+            assert rc == 0 and used <= need, args
+            seen.add((plan[0], plan[1] > 1))
+            if need:
+                assert probe.step_window_workspace(*args, given=need - 1)[0] == 9
+    assert seen == {(False, False), (False, True), (True, False), (True, True)}
+
+
+def test_4bit_steps_of_blocks_of_different_lengths_stay_in_the_workspace():
+    g = random.Random(12)
+    seen = set()
+    for cus in (256, 304, 32, 1):
+        for _ in range(300):
+            hkv, G, new = g.choice((1, 2, 3, 8, 24, 64, 300)), g.choice((1, 3, 4, 8, 16)), g.choice((1, 2, 3, 17, 128, 512))
+            b, d, f32 = g.choice((1, 1, 2, 4, 31, 32, 33)), g.choice((64, 128)), g.random() < .5
+            caches = [g.choice((0, 1, 63, 64, 65, int(np.exp(g.uniform(0, 12))))) for _ in range(b)]
+            args = (hkv * G, hkv, d, new, caches, [g.randint(1, new) for _ in range(b)], f32, cus)
+            rc, used, need, plan = probe.step4_workspace(*args)
+            assert rc == 0 and used <= need, args
+            seen.add(plan)
+            if need:
+                assert probe.step4_workspace(*args, given=need - 1)[0] == 9
+    assert seen == {(True, False), (False, True), (False, False)}
