@@ -23,6 +23,8 @@ and a sliding window of the latest)
   kv_read(cache, starts, length) returns what it holds
   workspace_bytes(op, batch, num_q_heads, num_kv_heads, max_q, max_k)
   step_workspace_bytes_varlen(batch, num_q_heads, num_kv_heads, new_len, cache_lens, new_lens)
+  step_workspace_bytes_window(..., new_lens, sinks, window), step_workspace_bytes_4bit(..., new_lens),
+  prefill_window_bwd_workspace_bytes(batch, num_q_heads, num_kv_heads, seq_len, sinks, window)
   step_plan(batch, num_q_heads, num_kv_heads, new_len, cache_lens, new_lens=None, num_cus=0)
 """
 import ctypes
@@ -36,7 +38,8 @@ from . import build as _build
 
 __all__ = ["WsError", "PagedCache", "PagedCache4", "kv_append", "kv_read", "block_causal_attn_fwd", "block_causal_attn_fwd_noalloc",
            "block_causal_prefill", "block_causal_prefill_bwd", "workspace_bytes",
-           "step_workspace_bytes_varlen", "step_plan", "library",
+           "step_workspace_bytes_varlen", "step_workspace_bytes_window", "step_workspace_bytes_4bit",
+           "prefill_window_bwd_workspace_bytes", "step_plan", "library",
            "abi_version", "WS_OP_STEP", "WS_OP_PREFILL", "WS_OP_PREFILL_BWD", "PAGE_SIZE"]
 
 WS_DTYPE_BF16, WS_DTYPE_F32 = 1, 2
@@ -357,6 +360,29 @@ def step_workspace_bytes_varlen(batch, num_q_heads, num_kv_heads, new_len, cache
     nh = torch.as_tensor(new_lens, dtype=torch.int32).cpu().contiguous()
     return library().ws_step_workspace_bytes_varlen(batch, num_q_heads, num_kv_heads, new_len, ch.data_ptr(),
                                                     nh.data_ptr())
+
+
+def step_workspace_bytes_window(batch, num_q_heads, num_kv_heads, new_len, cache_lens, new_lens=None, sinks=0, window=0):
+    """Workspace bytes of a step through a window (host int32 arrays or tensors
+    of [batch]; new_lens None: every block holds new_len tokens)."""
+    window, sinks = _window(window, sinks)
+    ch = torch.as_tensor(cache_lens, dtype=torch.int32).cpu().contiguous()
+    nh = None if new_lens is None else torch.as_tensor(new_lens, dtype=torch.int32).cpu().contiguous()
+    return library().ws_step_workspace_bytes_window(batch, num_q_heads, num_kv_heads, new_len, ch.data_ptr(), _ptr(nh),
+                                                    sinks, window)
+
+
+def step_workspace_bytes_4bit(batch, num_q_heads, num_kv_heads, new_len, cache_lens, new_lens=None):
+    """Workspace bytes of a step over a 4-bit cache (arrays as above)."""
+    ch = torch.as_tensor(cache_lens, dtype=torch.int32).cpu().contiguous()
+    nh = None if new_lens is None else torch.as_tensor(new_lens, dtype=torch.int32).cpu().contiguous()
+    return library().ws_step_workspace_bytes_4bit(batch, num_q_heads, num_kv_heads, new_len, ch.data_ptr(), _ptr(nh))
+
+
+def prefill_window_bwd_workspace_bytes(batch, num_q_heads, num_kv_heads, seq_len, sinks, window):
+    """Workspace bytes of the gradients through a window."""
+    window, sinks = _window(window, sinks)
+    return library().ws_prefill_window_bwd_workspace_bytes(batch, num_q_heads, num_kv_heads, seq_len, sinks, window)
 
 
 def step_plan(batch, num_q_heads, num_kv_heads, new_len, cache_lens, new_lens=None, num_cus=0):
