@@ -108,10 +108,16 @@ const at::Tensor *tensor(PyObject *o) {
     return t.defined() && t.layout() == at::kStrided && t.has_storage() ? &t : nullptr;
 }
 
-// The current device, whose stream the library launches on: asked once a call
-thread_local c10::DeviceIndex device_now;
-void ask_device() { device_now = c10::hip::current_device(); }
-bool here(const at::Tensor &t) { return t.is_cuda() && t.device().index() == device_now; }
+// Whether a tensor is on the current device, whose stream the library launches
+// on.  The device is asked for once a call, by its first device tensor (where
+// there is none the question is an error).
+thread_local c10::DeviceIndex device_now = -1;
+void new_call() { device_now = -1; }
+bool here(const at::Tensor &t) {
+    if (!t.is_cuda()) return false;
+    if (device_now < 0) device_now = c10::hip::current_device();
+    return t.device().index() == device_now;
+}
 
 bool shaped(const at::Tensor &t, std::initializer_list<int64_t> shape) { return t.sizes() == at::IntArrayRef(shape); }
 
@@ -295,7 +301,7 @@ PyObject *result(int rc, std::initializer_list<at::Tensor> out) {
 // append(cache, lens, k_new, v_new, new_lens) -> status, or None
 PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    ask_device();
+    new_call();
     if (n != 5) Py_RETURN_NONE;
     const at::Tensor *k = tensor(a[2]);
     if (!k || k->dim() != 4) Py_RETURN_NONE;
@@ -320,7 +326,7 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // append4(cache, lens, k_new, v_new, new_lens) -> status, or None
 PyObject *append4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    ask_device();
+    new_call();
     if (n != 5) Py_RETURN_NONE;
     const at::Tensor *k = tensor(a[2]);
     if (!k || k->dim() != 4) Py_RETURN_NONE;
@@ -344,7 +350,7 @@ PyObject *append4(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // read4(cache, starts, length, k, v) -> (status, k, v), or None
 PyObject *read4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    ask_device();
+    new_call();
     if (n != 5 || !PyTuple_CheckExact(a[1]) || PyTuple_GET_SIZE(a[1]) != 2 || !PyLong_CheckExact(a[2])) Py_RETURN_NONE;
     const at::Tensor *h = tensor(PyTuple_GET_ITEM(a[1], 0));
     if (!h || h->dim() != 1) Py_RETURN_NONE;
@@ -377,7 +383,7 @@ PyObject *read4(PyObject *, PyObject *const *a, Py_ssize_t n) {
 //   -> (status, out, lse), or None
 // (step_window: and window, sinks; step4: a PagedCache4)
 PyObject *step_of(PyObject *const *a, const Window &win, bool four = false) {
-    ask_device();
+    new_call();
     const at::Tensor *q = tensor(a[0]);
     if (!q || q->dim() != 4) Py_RETURN_NONE;
     const int64_t B = q->size(0), L = q->size(1), H = q->size(2), D = q->size(3);
@@ -478,7 +484,7 @@ PyObject *step4(PyObject *, PyObject *const *a, Py_ssize_t n) {
 //         want_lse, lse, text_starts) -> (status, out, lse), or None
 // (prefill_window: and window, sinks)
 PyObject *prefill_of(PyObject *const *a, const Window &win) {
-    ask_device();
+    new_call();
     const at::Tensor *q = tensor(a[0]);
     if (!q || q->dim() != 4) Py_RETURN_NONE;
     const int64_t B = q->size(0), L = q->size(1), H = q->size(2), D = q->size(3);
@@ -557,7 +563,7 @@ PyObject *prefill_window(PyObject *, PyObject *const *a, Py_ssize_t n) {
 //             workspace) -> (status, dq, dk, dv), or None
 // (prefill_window_bwd: and window, sinks, grad_dtype)
 PyObject *prefill_bwd_of(PyObject *const *a, const Window &win, at::ScalarType grads) {
-    ask_device();
+    new_call();
     const at::Tensor *q = tensor(a[0]), *k = tensor(a[1]), *lse = tensor(a[5]);
     if (!q || q->dim() != 4 || !k || k->dim() != 4 || !lse) Py_RETURN_NONE;
     const int64_t B = q->size(0), L = q->size(1), H = q->size(2), D = q->size(3), hkv = k->size(2);
