@@ -339,6 +339,8 @@ def _check_table(cache, B):
     if cache.page_table_host.shape[0] < B or cache.page_table.shape != cache.page_table_host.shape:
         raise ValueError("page table has fewer rows than the batch")
     _check_pair("page table", cache.page_table_host, cache.page_table)
+    if getattr(type(cache), "desc", PagedCache.desc) not in (PagedCache.desc, PagedCache4.desc):
+        return   # (a descriptor of its own says which pools are read)
     pools, size = ((cache.pool,), 1) if isinstance(cache, PagedCache4) else ((cache.k_pool, cache.v_pool), 2)
     if not all(_here(p) and p.is_contiguous() and p.element_size() == size for p in pools):
         raise ValueError("cache pools must be contiguous tensors of their type on the current device")

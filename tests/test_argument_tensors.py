@@ -31,3 +31,20 @@ def test_workspace():
     ws._check_workspace(None)
     with pytest.raises(ValueError, match="workspace"):
         ws._check_workspace(torch.zeros(16, dtype=torch.uint8))
+
+
+def test_a_cache_with_its_own_descriptor(monkeypatch):
+    """What its attributes hold is its own matter: desc() says what is read."""
+    class Placed(ws.PagedCache):
+        def desc(self):
+            return super().desc()
+
+    class Duck:
+        page_table_host = page_table = torch.zeros(1, 2, dtype=torch.int32)
+
+        def desc(self):
+            raise AssertionError("not asked here")
+    monkeypatch.setattr(ws, "_check_pair", lambda *_: None)   # (no device copy of the table here)
+    pool = torch.zeros(3, 2, 64, 64, dtype=torch.bfloat16)
+    ws._check_table(Placed(pool, pool, torch.zeros(1, 2, dtype=torch.int32)), 1)
+    ws._check_table(Duck(), 1)
