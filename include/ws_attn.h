@@ -587,6 +587,108 @@ size_t ws_step_workspace_bytes_4bit(int32_t batch, int32_t num_q_heads, int32_t 
                                     const int32_t *new_lens_host);
 
 /*
+ * Linear attention with a decay for each head: a layer whose memory of a session
+ * is one head_dim x head_dim state per KV head, whatever the session's length.
+ * With g = exp(log_decay[h]) of KV head h, token i of a sequence has
+ *   S_i = g S_(i-1) + k_i v_i^T,    o_i = scale * q_i S_i
+ * from the state S_-1 that the sequence brings (or zero).  Query head h reads KV
+ * head h / (Hq / Hkv).
+ * log_decay: device f32 [num_kv_heads], 0 or less (-INFINITY: nothing is kept;
+ * a positive one grows its state); a constant, without a gradient.
+ * States are f32 [slot][num_kv_heads][head_dim (k)][head_dim (v)] in a pool of
+ * num_slots; sequence (or stream) b lives in slot slots[b] (device and host
+ * copy, int32, the same values).  A call that writes states refuses slots that
+ * repeat (WS_ERR_PAGE, as a slot outside the pool).
+ * Outputs bf16 or f32.  States hold f32 accuracy over any number of tokens, f32
+ * outputs too; in a bf16 output of several tokens' chunk two operands (the
+ * scores and the state that a chunk of 32 tokens meets) are rounded to bf16.
+ * A query, key or value that is not finite may reach other tokens of its own
+ * chunk of the sequence, and never another sequence.
+ */
+typedef struct {
+    float *pool;                /* 16-byte aligned */
+    const int32_t *slots_dev;
+    const int32_t *slots_host;
+    int32_t num_slots;
+    int32_t num_kv_heads;
+    int32_t head_dim;
+} ws_linear_state;
+
+/* flags of the linear entry points: sequences begin with zero, whatever their
+ * slots hold; states are read and not written */
+enum { WS_STATE_RESET = 1, WS_STATE_KEEP = 2 };
+
+/*
+ * ws_linear_attn_prefill -- linear attention over packed sequences of different
+ * lengths, in chunks.
+ *   q:    bf16 [total_tokens][num_q_heads][head_dim] (stride_b is not used)
+ *   k, v: bf16 [total_tokens][num_kv_heads][head_dim]
+ *   seq_offsets_host / _dev: int32 [num_seqs + 1], same values: sequence s is the
+ *         tokens [seq_offsets[s], seq_offsets[s + 1]); first 0, non-decreasing,
+ *         last at most total_tokens.  A sequence may have no token: its state
+ *         stays as it is (WS_STATE_RESET: becomes zero).
+ *   state_or_null: sequences begin with their slots' states and leave theirs
+ *         there; NULL: they begin with zero and leave none
+ *   flags: WS_STATE_RESET, WS_STATE_KEEP
+ *   out:  bf16 or f32 [total_tokens][num_q_heads][head_dim]; rows behind the last
+ *         sequence are left as they were
+ *   workspace: ws_linear_workspace_bytes(...) bytes, 16-byte aligned
+ * Errors: WS_ERR_NULL, WS_ERR_SHAPE, WS_ERR_UNSUPPORTED, WS_ERR_ALIGN,
+ * WS_ERR_HEADS, WS_ERR_OFFSETS, WS_ERR_PAGE, WS_ERR_WORKSPACE, WS_ERR_HIP.
+ */
+int ws_linear_attn_prefill(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const float *log_decay,
+                           const int32_t *seq_offsets_host, const int32_t *seq_offsets_dev,
+                           int32_t num_seqs, int32_t total_tokens, int32_t num_q_heads,
+                           int32_t num_kv_heads, int32_t head_dim, float scale,
+                           const ws_linear_state *state_or_null, int32_t flags, ws_tensor4 out,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * ws_linear_attn_step -- the recurrent form: a few new tokens of each stream
+ * against its state (any number; from some tens on the chunked form is faster).
+ *   q: bf16 [batch][new_len][num_q_heads][head_dim]; k, v: [..][num_kv_heads][..]
+ *   new_lens_host / _dev: int32 [batch], 0 <= new_lens[b] <= new_len, or both NULL
+ *         (every stream has new_len tokens); rows past them are left as they were
+ *   flags: WS_STATE_KEEP tries the tokens and leaves the states (a block that is
+ *         not committed); else they are advanced in place
+ * Errors: as above, without offsets and workspace.
+ */
+int ws_linear_attn_step(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const float *log_decay,
+                        const ws_linear_state *state, const int32_t *new_lens_host,
+                        const int32_t *new_lens_dev, int32_t batch, int32_t new_len,
+                        int32_t num_q_heads, float scale, int32_t flags, ws_tensor4 out, void *stream);
+
+/*
+ * ws_linear_attn_prefill_bwd -- gradients of ws_linear_attn_prefill for an
+ * upstream gradient dO of the output and, where the final states were used, dS of
+ * them.  Arguments as the forward's, and
+ *   dout:    bf16, as q
+ *   state_or_null: the states the sequences began with (read only); NULL: zero
+ *   dstate:  NULL (zero) or f32 [num_seqs][num_kv_heads][head_dim][head_dim], the
+ *            gradient of the final states
+ *   dstate0: NULL or the same shape, written: the gradient of the first states
+ *   dq: bf16 [total_tokens][num_q_heads][head_dim], dk, dv: bf16
+ *            [..][num_kv_heads][..], written; rows behind the last sequence are not
+ *   workspace: ws_linear_workspace_bytes(...) bytes, 16-byte aligned
+ * Deterministic.  dstate and dstate0 must not overlap.
+ */
+int ws_linear_attn_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 dout,
+                               const float *log_decay, const int32_t *seq_offsets_host,
+                               const int32_t *seq_offsets_dev, int32_t num_seqs, int32_t total_tokens,
+                               int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float scale,
+                               const ws_linear_state *state_or_null, const float *dstate, float *dstate0,
+                               ws_tensor4 dq, ws_tensor4 dk, ws_tensor4 dv, void *workspace,
+                               size_t workspace_bytes, void *stream);
+
+/*
+ * Workspace bytes of ws_linear_attn_prefill and ws_linear_attn_prefill_bwd for
+ * these sizes, whatever the sequences' lengths (host arithmetic: no device is
+ * asked).  0 for invalid arguments.
+ */
+size_t ws_linear_workspace_bytes(int32_t num_seqs, int32_t total_tokens, int32_t num_q_heads,
+                                 int32_t num_kv_heads, int32_t head_dim);
+
+/*
  * Workspace bytes ws_block_causal_attn_fwd (and its _text variant) needs
  * for this shape (op =
  * WS_OP_STEP; num_kv_heads = the cache's; max_k = largest cache_lens[b] +

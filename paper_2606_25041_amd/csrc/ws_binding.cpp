@@ -55,8 +55,16 @@ struct Cache4Abi {
     decltype(&ws_step_workspace_bytes_4bit) step_bytes;
 } abi4;
 
+struct LinearAbi {
+    decltype(&ws_linear_attn_prefill) prefill;
+    decltype(&ws_linear_attn_step) step;
+    decltype(&ws_linear_attn_prefill_bwd) bwd;
+    decltype(&ws_linear_workspace_bytes) bytes;
+} labi;
+
 PyObject *cache_class;    // PagedCache
 PyObject *cache4_class;   // PagedCache4
+PyObject *state_class;    // LinearState
 
 bool take_addresses(void **to, size_t count, PyObject *const *args, Py_ssize_t n) {
     if (n != (Py_ssize_t)count) {
@@ -83,6 +91,16 @@ PyObject *bind_cache4(PyObject *, PyObject *const *args, Py_ssize_t n) {
     }
     Py_INCREF(args[0]);
     Py_XSETREF(cache4_class, args[0]);
+    Py_RETURN_NONE;
+}
+
+PyObject *bind_linear(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n < 1 || !take_addresses((void **)&labi, sizeof labi / sizeof(void *), args + 1, n - 1)) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "the state class first");
+        return nullptr;
+    }
+    Py_INCREF(args[0]);
+    Py_XSETREF(state_class, args[0]);
     Py_RETURN_NONE;
 }
 
@@ -131,6 +149,15 @@ bool token_tensor(const at::Tensor *t, std::initializer_list<int64_t> shape, ws_
     return true;
 }
 
+// descriptor of a packed [T][H][d] tensor
+bool packed_tokens(const at::Tensor *t, std::initializer_list<int64_t> shape, ws_tensor4 &d) {
+    if (!t || !here(*t) || !shaped(*t, shape) || t->stride(2) != 1) return false;
+    const auto dt = t->scalar_type();
+    if (dt != at::kBFloat16 && dt != at::kFloat) return false;
+    d = ws_tensor4{t->data_ptr(), dt == at::kBFloat16 ? WS_DTYPE_BF16 : WS_DTYPE_F32, 0, t->stride(0), t->stride(1)};
+    return true;
+}
+
 struct Ints {
     const int32_t *host = nullptr, *dev = nullptr;
 };
@@ -163,6 +190,7 @@ struct NoGil {
 
 PyObject *names[7];   // attribute names of PagedCache, in the order below
 PyObject *pool_name;  // PagedCache4: "pool" in place of the first two
+PyObject *state_names[3];   // LinearState's: pool, slots_host, slots
 
 // a contiguous tensor of the current device (of elements of `size` bytes; 0: any)
 bool packed(const at::Tensor *t, int64_t size) {
@@ -632,10 +660,198 @@ PyObject *prefill_window_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// A LinearState's descriptor for `count` sequences; its tensors are held.
+struct States : ws_linear_state {
+    at::Tensor hold[3];
+};
+bool states(PyObject *o, int64_t count, States &d) {
+    if ((PyObject *)Py_TYPE(o) != state_class) return false;
+    PyObject *v[3] = {};
+    bool ok = true;
+    for (int i = 0; i < 3 && ok; ++i) ok = (v[i] = PyObject_GetAttr(o, state_names[i])) != nullptr;
+    if (!ok) PyErr_Clear();
+    if (ok) {
+        const at::Tensor *p = tensor(v[0]), *h = tensor(v[1]), *s = tensor(v[2]);
+        ok = packed(p, 4) && p->scalar_type() == at::kFloat && p->dim() == 4 && p->size(2) == p->size(3) &&
+             p->size(0) <= INT32_MAX && h && s && shaped(*h, {count}) && shaped(*s, {count}) && h->scalar_type() == at::kInt &&
+             s->scalar_type() == at::kInt && h->is_contiguous() && s->is_contiguous() && h->is_cpu() && here(*s);
+        if (ok) {
+            static_cast<ws_linear_state &>(d) =
+                ws_linear_state{(float *)p->data_ptr(), (const int32_t *)s->data_ptr(), (const int32_t *)h->data_ptr(),
+                                (int32_t)p->size(0), (int32_t)p->size(1), (int32_t)p->size(2)};
+            d.hold[0] = *p, d.hold[1] = *h, d.hold[2] = *s;
+        }
+    }
+    for (PyObject *x : v) Py_XDECREF(x);
+    return ok;
+}
+
+// f32 [Hkv] on the current device
+bool decays(PyObject *o, int64_t hkv, const float *&p) {
+    const at::Tensor *t = tensor(o);
+    if (!t || !here(*t) || !shaped(*t, {hkv}) || !packed_f32(*t)) return false;
+    p = (const float *)t->data_ptr();
+    return true;
+}
+
+// a (host, device) pair of sequence offsets; num: its sequences
+bool offsets_of(PyObject *o, Ints &x, int64_t &num) {
+    if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 2) return false;
+    const at::Tensor *h = tensor(PyTuple_GET_ITEM(o, 0));
+    if (!h || h->dim() != 1 || h->size(0) < 2 || h->size(0) > INT32_MAX) return false;
+    num = h->size(0) - 1;
+    return int_pair(o, {num + 1}, false, x);
+}
+
+// linear_prefill(q, k, v, log_decay, seq_offsets, scale, state, reset, commit, out,
+//                out_dtype, workspace) -> (status, out), or None
+PyObject *linear_prefill(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    new_call();
+    if (n != 12) Py_RETURN_NONE;
+    const at::Tensor *q = tensor(a[0]), *k = tensor(a[1]);
+    if (!q || q->dim() != 3 || !k || k->dim() != 3) Py_RETURN_NONE;
+    const int64_t T = q->size(0), H = q->size(1), D = q->size(2), hkv = k->size(1);
+    if (T == 0 || T > INT32_MAX) Py_RETURN_NONE;
+    ws_tensor4 qd, kd, vd, od;
+    Ints off;
+    States st{};
+    int64_t S;
+    float scale;
+    bool reset, commit;
+    const float *ld;
+    if (!packed_tokens(q, {T, H, D}, qd) || !packed_tokens(k, {T, hkv, D}, kd) ||
+        !packed_tokens(tensor(a[2]), {T, hkv, D}, vd) || !decays(a[3], hkv, ld) || !offsets_of(a[4], off, S) ||
+        !scale_of(a[5], D, scale) || (a[6] != Py_None && !states(a[6], S, st)) || !flag(a[7], reset) || !flag(a[8], commit))
+        Py_RETURN_NONE;
+    const at::ScalarType type = a[9] == Py_None ? dtype_of(a[10]) : at::kBFloat16;
+    if (type != at::kBFloat16 && type != at::kFloat) Py_RETURN_NONE;
+    const at::Tensor *wsp = a[11] == Py_None ? nullptr : tensor(a[11]);
+    if (a[11] != Py_None && !packed(wsp, 1)) Py_RETURN_NONE;
+    at::Tensor out, own;
+    if (!given(a[9], {T, H, D}, out) || (out.defined() && !packed_tokens(&out, {T, H, D}, od))) Py_RETURN_NONE;
+    int rc = -1;
+    {
+        NoGil free;
+        const size_t need = wsp ? 0 : labi.bytes(S, T, H, hkv, D);
+        if (wsp || need) {
+            allocate(out, {T, H, D}, type, *q);
+            packed_tokens(&out, {T, H, D}, od);
+            if (!wsp) {
+                own = at::empty({(int64_t)need}, q->options().dtype(at::kByte));
+                wsp = &own;
+            }
+            rc = labi.prefill(qd, kd, vd, ld, off.host, off.dev, S, T, H, hkv, D, scale, a[6] != Py_None ? &st : nullptr,
+                              (reset ? WS_STATE_RESET : 0) | (commit ? 0 : WS_STATE_KEEP), od, wsp->data_ptr(), wsp->numel(),
+                              stream());
+        }
+    }
+    if (rc < 0) Py_RETURN_NONE;   // (the Python code names the mistake)
+    return result(rc, {out});
+    END_HANDLE_TH_ERRORS
+}
+
+// linear_step(q, k, v, log_decay, state, scale, commit, new_lens, out, out_dtype)
+//   -> (status, out), or None
+PyObject *linear_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    new_call();
+    if (n != 10) Py_RETURN_NONE;
+    const at::Tensor *q = tensor(a[0]);
+    if (!q || q->dim() != 4) Py_RETURN_NONE;
+    const int64_t B = q->size(0), L = q->size(1), H = q->size(2), D = q->size(3);
+    if (B == 0 || L == 0 || B > INT32_MAX || L > INT32_MAX) Py_RETURN_NONE;
+    ws_tensor4 qd, kd, vd, od;
+    Ints nl;
+    States st{};
+    float scale;
+    bool commit;
+    const float *ld;
+    if (!states(a[4], B, st) || st.head_dim != D) Py_RETURN_NONE;
+    const int64_t hkv = st.num_kv_heads;
+    if (!token_tensor(q, {B, L, H, D}, qd) || !token_tensor(tensor(a[1]), {B, L, hkv, D}, kd) ||
+        !token_tensor(tensor(a[2]), {B, L, hkv, D}, vd) || !decays(a[3], hkv, ld) || !scale_of(a[5], D, scale) ||
+        !flag(a[6], commit) || !int_pair(a[7], {B}, true, nl))
+        Py_RETURN_NONE;
+    const at::ScalarType type = a[8] == Py_None ? dtype_of(a[9]) : at::kBFloat16;
+    if (type != at::kBFloat16 && type != at::kFloat) Py_RETURN_NONE;
+    at::Tensor out;
+    if (!given(a[8], {B, L, H, D}, out) || (out.defined() && !token_tensor(&out, {B, L, H, D}, od))) Py_RETURN_NONE;
+    int rc;
+    {
+        NoGil free;
+        allocate(out, {B, L, H, D}, type, *q);
+        token_tensor(&out, {B, L, H, D}, od);
+        rc = labi.step(qd, kd, vd, ld, &st, nl.host, nl.dev, B, L, H, scale, commit ? 0 : WS_STATE_KEEP, od, stream());
+    }
+    return result(rc, {out});
+    END_HANDLE_TH_ERRORS
+}
+
+// linear_bwd(q, k, v, dout, log_decay, seq_offsets, scale, state, dstate, want_dstate0,
+//            dq, dk, dv, dstate0, workspace) -> (status, dq, dk, dv, dstate0), or None
+PyObject *linear_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    new_call();
+    if (n != 15) Py_RETURN_NONE;
+    const at::Tensor *q = tensor(a[0]), *k = tensor(a[1]);
+    if (!q || q->dim() != 3 || !k || k->dim() != 3) Py_RETURN_NONE;
+    const int64_t T = q->size(0), H = q->size(1), D = q->size(2), hkv = k->size(1);
+    if (T == 0 || T > INT32_MAX) Py_RETURN_NONE;
+    ws_tensor4 qd, kd, vd, dd, dqd, dkd, dvd;
+    Ints off;
+    States st{};
+    int64_t S;
+    float scale;
+    bool want;
+    const float *ld;
+    if (!packed_tokens(q, {T, H, D}, qd) || !packed_tokens(k, {T, hkv, D}, kd) ||
+        !packed_tokens(tensor(a[2]), {T, hkv, D}, vd) || !packed_tokens(tensor(a[3]), {T, H, D}, dd) || !decays(a[4], hkv, ld) ||
+        !offsets_of(a[5], off, S) || !scale_of(a[6], D, scale) || (a[7] != Py_None && !states(a[7], S, st)) || !flag(a[9], want))
+        Py_RETURN_NONE;
+    at::Tensor dq, dk, dv, ds, ds0, own;
+    if (!given(a[8], {S, hkv, D, D}, ds) || (ds.defined() && !packed_f32(ds)) || !given(a[13], {S, hkv, D, D}, ds0) ||
+        (ds0.defined() && !packed_f32(ds0)) || !given(a[10], {T, H, D}, dq) ||
+        (dq.defined() && !packed_tokens(&dq, {T, H, D}, dqd)) || !given(a[11], {T, hkv, D}, dk) ||
+        (dk.defined() && !packed_tokens(&dk, {T, hkv, D}, dkd)) || !given(a[12], {T, hkv, D}, dv) ||
+        (dv.defined() && !packed_tokens(&dv, {T, hkv, D}, dvd)))
+        Py_RETURN_NONE;
+    const at::Tensor *wsp = a[14] == Py_None ? nullptr : tensor(a[14]);
+    if (a[14] != Py_None && !packed(wsp, 1)) Py_RETURN_NONE;
+    int rc = -1;
+    {
+        NoGil free;
+        const size_t need = wsp ? 0 : labi.bytes(S, T, H, hkv, D);
+        if (wsp || need) {
+            allocate(dq, {T, H, D}, at::kBFloat16, *q);
+            allocate(dk, {T, hkv, D}, at::kBFloat16, *q);
+            allocate(dv, {T, hkv, D}, at::kBFloat16, *q);
+            packed_tokens(&dq, {T, H, D}, dqd);
+            packed_tokens(&dk, {T, hkv, D}, dkd);
+            packed_tokens(&dv, {T, hkv, D}, dvd);
+            if (want) allocate(ds0, {S, hkv, D, D}, at::kFloat, *q);
+            if (!wsp) {
+                own = at::empty({(int64_t)need}, q->options().dtype(at::kByte));
+                wsp = &own;
+            }
+            rc = labi.bwd(qd, kd, vd, dd, ld, off.host, off.dev, S, T, H, hkv, D, scale, a[7] != Py_None ? &st : nullptr,
+                          ds.defined() ? (const float *)ds.data_ptr() : nullptr, ds0.defined() ? (float *)ds0.data_ptr() : nullptr,
+                          dqd, dkd, dvd, wsp->data_ptr(), wsp->numel(), stream());
+        }
+    }
+    if (rc < 0) Py_RETURN_NONE;   // (the Python code names the mistake)
+    return result(rc, {dq, dk, dv, ds0});
+    END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)())bind, METH_FASTCALL, "the cache class, then the C ABI's addresses in Abi's order"},
     {"bind_window", (PyCFunction)(void (*)())bind_window, METH_FASTCALL, "the windowed ABI's addresses in WindowAbi's order"},
     {"bind_cache4", (PyCFunction)(void (*)())bind_cache4, METH_FASTCALL, "PagedCache4, then the 4-bit ABI's addresses"},
+    {"bind_linear", (PyCFunction)(void (*)())bind_linear, METH_FASTCALL, "LinearState, then the linear ABI's addresses"},
+    {"linear_prefill", (PyCFunction)(void (*)())linear_prefill, METH_FASTCALL, nullptr},
+    {"linear_step", (PyCFunction)(void (*)())linear_step, METH_FASTCALL, nullptr},
+    {"linear_bwd", (PyCFunction)(void (*)())linear_bwd, METH_FASTCALL, nullptr},
     {"append4", (PyCFunction)(void (*)())append4, METH_FASTCALL, nullptr},
     {"read4", (PyCFunction)(void (*)())read4, METH_FASTCALL, nullptr},
     {"step4", (PyCFunction)(void (*)())step4, METH_FASTCALL, nullptr},
@@ -656,5 +872,8 @@ PyMODINIT_FUNC PyInit__wsbinding() {
     for (int i = 0; i < 7; ++i)
         if (!(names[i] = PyUnicode_InternFromString(n[i]))) return nullptr;
     if (!(pool_name = PyUnicode_InternFromString("pool"))) return nullptr;
+    const char *s[3] = {"pool", "slots_host", "slots"};
+    for (int i = 0; i < 3; ++i)
+        if (!(state_names[i] = PyUnicode_InternFromString(s[i]))) return nullptr;
     return PyModule_Create(&module);
 }

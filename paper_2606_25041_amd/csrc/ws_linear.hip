@@ -1,0 +1,772 @@
+// Linear attention with a decay for each head (gfx950): packed sequences in
+// chunks, backwards in time for the gradients, and a few new tokens against
+// states that stay in memory.
+//
+// One operator serves the forward and all gradients.  Over the tokens of a
+// sequence, with g the decay of a KV head and w the time between two tokens,
+//   out_i = scale * ( sum_t g^w(i,t) (x_i . y_t) z_t  +  g^(..) x_i S )
+// where t runs over i and the tokens before it, S [y dim][z dim] is the state
+// the sequence brings, and S' = g^n S + sum_t g^(..) y_t z_t^T the one it
+// leaves.  Forward: (x, y, z) = (q, k, v).  dQ: (dO, v, k) with S^T.  dV and dK
+// are the same backwards in time, (k, q, dO) and (v, dO, q), the query heads of
+// a KV head being key sets that are summed; there a token sees those after it.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "ws_device_util.h"
+#include "ws_linear.h"
+
+namespace ws {
+namespace {
+
+constexpr int C = LIN_CHUNK;
+enum { ONE = 0, KEYS = 1, ROWS = 2 };
+constexpr float LOG2E = 1.4426950408889634f;
+
+// A state times g^n: S + (g^n - 1) S where g^n is at least 1/2, so that no rounding
+// of g^n itself adds up over many chunks or tokens (a head that holds for 8192
+// tokens would be off by 2^-24 x 8192); g^n S below, where g^n - 1 would lose its
+// last bits.
+struct Decay {
+    float by;
+    bool slow;
+};
+__device__ __forceinline__ Decay decay_of(float x) {   // g^n = e^x (wave-uniform)
+    const bool slow = x >= -0.6931472f;
+    const float by = slow ? expm1f(x) : expf(x);
+    return Decay{__uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(by))),
+                 __builtin_amdgcn_readfirstlane((int)slow) != 0};
+}
+
+// (log_decay of -inf: g = 0 and g^0 = 1, without inf * 0)
+__device__ __forceinline__ float log_decay_of(const float *p, int kvh) {
+    const float ld = __uint_as_float((uint32_t)ld_uniform((const int32_t *)p, kvh));
+    return ld < -1e30f ? -1e30f : ld;
+}
+
+// Eight values as an operand of NP bf16 parts, whose sum holds 8, 16 or f32's 24
+// bits of each.
+template <int NP>
+__device__ __forceinline__ void parts_of(const float (&v)[8], bf16x8 (&out)[NP]) {
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = v[e];
+#pragma unroll
+    for (int c = 0; c < NP; ++c) {
+        u32x4 r;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            r[h] = pack_bf16x2(x[2 * h], x[2 * h + 1]);
+            if (c + 1 < NP) {
+                x[2 * h] -= __uint_as_float(r[h] << 16);
+                x[2 * h + 1] -= __uint_as_float(r[h] & 0xFFFF0000u);
+            }
+        }
+        out[c] = __builtin_bit_cast(bf16x8, r);
+    }
+}
+
+// A chunk of a sequence's tokens, and one of its key sets.
+struct Step {
+    int t, n;       // first token and tokens
+    int seq, set;
+    bool first;     // the state is to be read: from the sequence's own (own) or the cell's
+    bool last;      // no more of this sequence in the cell: its end (own) or the cell's
+    bool own_first, own_last;
+    bool live;
+};
+
+// The steps of a cell's tokens [t0, t1), in their order.
+template <bool REV>
+struct Walk {
+    const int32_t *off;
+    int t0, t1, sets;
+    int seq, ps, pe, pos, set;   // the piece of sequence seq: tokens [ps, pe)
+
+    __device__ __forceinline__ void piece() {
+        ps = max(ld_uniform(off, seq), t0);
+        pe = min(ld_uniform(off, seq + 1), t1);
+        pos = REV ? pe : ps;
+    }
+    __device__ __forceinline__ Step next() {
+        Step r;
+        r.live = REV ? pe > t0 : ps < t1;
+        r.seq = seq;
+        r.set = set;
+        r.n = REV ? ((pos - ps - 1) & (C - 1)) + 1 : min(C, pe - pos);
+        r.t = REV ? pos - r.n : pos;
+        r.first = set == 0 && pos == (REV ? pe : ps);
+        r.last = false;
+        r.own_first = r.own_last = false;
+        if (!r.live) return r;
+        const int begin = ld_uniform(off, seq), end = ld_uniform(off, seq + 1);
+        r.own_first = REV ? pe == end : ps == begin;
+        if (++set < sets) return r;
+        set = 0;
+        pos = REV ? r.t : pos + r.n;
+        if (pos != (REV ? ps : pe)) return r;
+        r.last = true;
+        r.own_last = REV ? ps == begin : pe == end;
+        // (sequences without tokens are passed over)
+        if constexpr (REV) {
+            if (ps > t0) {
+                do --seq; while (ld_uniform(off, seq) == ps);
+                piece();
+            } else {
+                pe = t0;
+            }
+        } else {
+            if (pe < t1) {
+                do ++seq; while (ld_uniform(off, seq + 1) == pe);
+                piece();
+            } else {
+                ps = t1;
+            }
+        }
+        return r;
+    }
+};
+
+// The sequence that holds token t (the last whose first token is not past it),
+// by 64 probes at a time; every lane active.
+__device__ __forceinline__ int sequence_of(const int32_t *off, int S, int t, int lane) {
+    int base = 0, len = S;
+    while (len > 64) {
+        const int part = (len + 63) / 64;
+        const int64_t k = base + (int64_t)lane * part;
+        base += part * (__builtin_popcountll(__builtin_amdgcn_ballot_w64(k < S && off[k] <= t)) - 1);
+        len = min(part, S - base);
+    }
+    return base + __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < len && off[base + lane] <= t)) - 1;
+}
+
+// A work-group is D / 32 waves; wave w holds 32 columns (z dims) of the state,
+// D x 32 in f32 accumulators, over all of a cell's tokens, so the state never
+// leaves the registers.  A chunk of 32 tokens x i:
+//   P^T = Y X^T       keys in rows, tokens in columns: its accumulators are the
+//   O^T = S^T X^T       B operand of Z^T P^T under a fixed permutation of the
+//   O^T = g^(i+1) O^T + Z^T (P^T . W)   keys, and the state's those of S^T X^T
+//   S   = g^n S + Y^T (Z . w)             under one of the dims
+// Rounded to bf16 are the operands P . W and S (f32 output: three bf16 parts
+// each, 24 bits); the state's own sum takes Z . w in three parts, so that it
+// holds f32 accuracy over any number of tokens.
+// Per token and head 42 MFMAs a wave and chunk (24 of them the state's) against
+// 4 D bf16 of memory traffic: bound by HBM where the chip is full.
+// Tiles go global -> LDS, three stages, one barrier a chunk.
+// OUT = false: the state alone, of the sequence that goes on past the cell's
+// edge, written to `cells`.
+// SETS: KEYS, the key sets of a KV head's query heads are summed, a chunk of each
+// after the other; ROWS, its query heads are taken after each other against the
+// same keys, whose products with the state (24 of the 44 MFMAs) are then formed
+// once.
+template <int D, bool REV, bool F32, bool OUT, int SETS>
+__global__ __launch_bounds__(2 * D, 2) void linear_kernel(const LinearArgs a) {
+    constexpr int NW = D / 32, MT = D / 32, KS = D / 16;
+    constexpr int PP = F32 ? 3 : 2, PS = F32 ? 3 : 1;   // bf16 parts of P . W and of S as operands
+    // A tile's rows lie in groups of 1 KiB, what one wave-wide load brings, 16
+    // bytes apart; in a group 16-byte chunk c of row r is in slot c ^ turn(r), so
+    // that of chunk indices only the upper bits are in an XOR and the rest of a
+    // read's address is a constant.
+    constexpr int ROWB = 2 * D, GROUPB = 1024 + 16, TILEB = C * ROWB / 1024 * GROUPB;
+    // rings of the keys and values and, behind them, of the rows, three stages each
+    // (two of keys where several steps share them)
+    constexpr int NYZ = SETS == ROWS ? 2 : 3, NX = OUT ? 3 : 0, XRING = NYZ * 2 * TILEB;
+    constexpr int LPR = ROWB / 16, RPW = 64 / LPR;   // lanes per row, rows per wave-wide load
+    constexpr int NI = C / (NW * RPW);               // loads per wave and tile
+    static_assert(NI == 2, "two loads a tile");
+    __shared__ __attribute__((aligned(1024))) char smem[XRING + NX * TILEB];
+
+    const int lane = threadIdx.x & 63, hf = lane >> 5, l32 = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+    // ---- work item: (cell, KV head, job) ---------------------------------------
+    const uint32_t w = (blockIdx.x % NUM_XCD) * (uint32_t)a.per_xcd + blockIdx.x / NUM_XCD;
+    if (w >= (uint32_t)a.n_work) return;
+    uint32_t item = w;
+    int jn = 0;
+    if (OUT && a.njobs == 2) {
+        jn = item & 1;
+        item >>= 1;
+    }
+    const uint32_t cell_u = fastdiv(item, a.fd_hkv);
+    const int kvh = (int)(item - cell_u * (uint32_t)a.Hkv);
+    // (cells from the end on in a pass backwards)
+    const int cell = REV ? a.ncells - 1 - (int)cell_u : (int)cell_u;
+    const LinearJob &job = a.job[jn];
+
+    Walk<REV> walk;
+    walk.off = a.seqs;
+    walk.t0 = cell * a.cell_len;
+    walk.t1 = min(walk.t0 + a.cell_len, a.T);
+    walk.sets = SETS == ONE || (SETS == ROWS && !OUT) ? 1 : a.sets;
+    walk.set = 0;
+    if constexpr (OUT) {
+        walk.seq = sequence_of(a.seqs, a.S, REV ? walk.t1 - 1 : walk.t0, lane);
+    } else {
+        // the sequence that goes on past the edge, if one does
+        walk.seq = sequence_of(a.seqs, a.S, REV ? walk.t0 : walk.t1 - 1, lane);
+        if (REV ? ld_uniform(a.seqs, walk.seq) >= walk.t0 : ld_uniform(a.seqs, walk.seq + 1) <= walk.t1) return;
+    }
+    walk.seq = __builtin_amdgcn_readfirstlane(walk.seq);
+    walk.piece();
+    if constexpr (!OUT) {   // only this piece
+        if (REV) walk.t1 = walk.pe;
+        else walk.t0 = walk.ps;
+    }
+
+    const float ld = log_decay_of(a.log_decay, kvh);
+    const float l2 = ld * LOG2E;
+
+    // ---- tile loads -------------------------------------------------------------
+    const int lrow = wave * RPW + lane / LPR;        // this lane's row of load 0
+    auto turn = [](int r) -> int { return D == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); };
+    const uint32_t lch = 16 * ((lane % LPR) ^ turn(lane / LPR));
+    // byte strides of tokens (below 2^25, checked on the host: 32 rows' offsets fit 32 bits)
+    const uint32_t xs = 2 * (uint32_t)job.x_st, ys = 2 * (uint32_t)job.y_st, zs = 2 * (uint32_t)job.z_st;
+    const uint32_t ofs_x = lrow * xs + lch, ofs_y = lrow * ys + lch, ofs_z = lrow * zs + lch;
+    const char *xb = (const char *)job.x, *yb = (const char *)job.y, *zb = (const char *)job.z;
+    // head of the rows and of the keys in a step
+    auto row_head = [&](const Step &r) -> int64_t { return SETS == ROWS ? (int64_t)kvh * a.sets + r.set : kvh; };
+    auto key_head = [&](const Step &r) -> int64_t { return SETS == KEYS ? (int64_t)kvh * a.sets + r.set : kvh; };
+    auto loads_keys = [&](const Step &r) -> bool { return SETS != ROWS || r.set == 0; };
+    // A chunk of fewer tokens stands at the end of its tiles (backwards: at their
+    // beginning), where the weights of a whole one hold; the other rows repeat a
+    // token and their z counts as 0.
+    auto tail_row = [](int row, int n) -> int { return REV ? min(row, n - 1) : max(row - (C - n), 0); };
+    auto is_token = [](int row, int n) -> bool { return REV ? row < n : row >= C - n; };
+    auto issue = [&](const Step &r, int xstage, int kstage) {
+        const uint32_t to = lds_addr(smem) + wave * GROUPB, tx = to + XRING + xstage * TILEB, ty = to + kstage * 2 * TILEB;
+        const char *x = OUT ? xb + 2 * row_head(r) * job.x_sh + (uint64_t)r.t * xs : nullptr;
+        const char *y = yb + 2 * key_head(r) * job.y_sh + (uint64_t)r.t * ys;
+        const char *z = zb + 2 * key_head(r) * job.z_sh + (uint64_t)r.t * zs;
+        const bool keys = loads_keys(r);
+        if (r.n == C) {
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const uint32_t row = i * NW * RPW, at = i * NW * GROUPB;
+                if constexpr (OUT) dma16s(x + (uint64_t)row * xs, ofs_x, tx + at);
+                if (keys) {
+                    dma16s(y + (uint64_t)row * ys, ofs_y, ty + at);
+                    dma16s(z + (uint64_t)row * zs, ofs_z, ty + TILEB + at);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const uint32_t row = tail_row(lrow + i * NW * RPW, r.n), at = i * NW * GROUPB;
+                if constexpr (OUT) dma16s(x, row * xs + lch, tx + at);
+                if (keys) {
+                    dma16s(y, row * ys + lch, ty + at);
+                    dma16s(z, row * zs + lch, ty + TILEB + at);
+                }
+            }
+        }
+        asm volatile("" ::: "memory");
+    };
+
+    // ---- weights of a whole chunk --------------------------------------------------
+    // key j(v) of accumulator register v of this lane; its row is token l32
+    auto key = [&](int v) -> int { return 8 * (v >> 2) + 4 * hf + (v & 3); };
+    float pw[16], kw[16];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        const int far = REV ? key(v) - l32 : l32 - key(v);
+        pw[v] = far >= 0 ? fast_exp2(far * l2) * a.scale : 0.f;   // (the output's scale goes with them)
+    }
+#pragma unroll
+    for (int v = 0; v < 16; ++v) kw[v] = fast_exp2((REV ? key(v) + 1 : C - 1 - key(v)) * l2);
+    const Decay whole = decay_of(C * ld);
+    const float head = fast_exp2((REV ? C - 1 - l32 : l32 + 1) * l2) * a.scale;
+
+    f32x16 S[MT];
+    u32x4 held[F32 ? 4 : 2];   // a chunk's output rows, stored behind the next barrier
+    int held_n = 0;            // its tokens (0: nothing is held)
+    char *held_to = nullptr;
+    auto store_held = [&]() {
+        if (is_token(l32, held_n)) {
+            if constexpr (F32) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) *(u32x4 *)(held_to + 32 * g) = held[g];
+            } else {
+#pragma unroll
+                for (int g = 0; g < 2; ++g) *(u32x4 *)(held_to + 32 * g) = held[g];
+            }
+        }
+    };
+
+    // ---- states --------------------------------------------------------------------
+    // (the lane is hidden from the optimiser there, so that no addresses are
+    // computed ahead of the loop and held in registers)
+    auto read_state = [&](const Step &r) {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const int col = 32 * wave + (ln & 31), half = ln >> 5;
+        const float *p = nullptr;
+        float scale = 1.f;
+        const bool turned = r.own_first ? job.own_turned : job.cells_turned;
+        if (r.own_first) {
+            if (a.state_in) {
+                p = a.state_in + ((int64_t)(a.slots ? ld_uniform(a.slots, r.seq) : r.seq) * a.Hkv + kvh) * (D * D);
+                scale = a.in_scale;
+            }
+        } else if constexpr (OUT) {
+            p = a.cells + ((int64_t)cell * a.Hkv + kvh) * (D * D);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int row = 32 * m + 8 * g + 4 * half;
+                f32x4 x = {0.f, 0.f, 0.f, 0.f};
+                if (p) {
+                    if (turned) {
+                        x = *(const f32x4 *)(p + col * D + row);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = p[(row + e) * D + col];
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) S[m][4 * g + e] = x[e] * scale;
+            }
+    };
+    auto write_state = [&](float *p, float scale) {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        p += 4 * (ln >> 5) * D + 32 * wave + (ln & 31);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) p[(32 * m + 8 * (v >> 2) + (v & 3)) * D] = S[m][v] * scale;
+    };
+
+    // ---- LDS reads -------------------------------------------------------------------
+    // row_frag: dims 16 s + 8 (e / 4) + 4 hf + e % 4 of row l32, in the accumulators'
+    // order: chunks 2 s and 2 s + 1, of which s / 2 is in the XOR
+    constexpr int RG = 1024 / ROWB;   // rows of a group
+    const int j16 = lane & 15, tr = 4 * hf + (j16 >> 2);
+    uint32_t rbase[MT], cbase[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        rbase[m] = (l32 / RG) * GROUPB + (l32 % RG) * ROWB + 8 * hf + (16 * turn(l32 % RG) ^ 64 * m);
+        cbase[m] = (tr / RG) * GROUPB + (tr % RG) * ROWB + 8 * (j16 & 1) +
+                   16 * ((4 * m + 2 * ((lane >> 4) & 1) + ((j16 & 3) >> 1)) ^ turn(tr % RG));
+    }
+    auto row_frag = [&](const char *tile, int s) -> bf16x8 {
+        const char *p = tile + rbase[s >> 1] + 32 * (s & 1);
+        const u32x2 lo = *(const u32x2 *)p, hi = *(const u32x2 *)(p + 16);
+        return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+    };
+    // dims 32 m + l32 of keys 16 s + 8 (e / 4) + 4 hf + e % 4, by transpose reads
+    // (col_of: of a base, the wave's own columns or cbase[m])
+    auto col_of = [&](const char *tile, int s, uint32_t base) -> bf16x8 {
+        const char *p = tile + base + 16 / RG * s * GROUPB;
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)p);
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(p + 8 / RG * GROUPB));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto col_frag = [&](const char *tile, int s, int m) -> bf16x8 { return col_of(tile, s, cbase[m]); };
+    uint32_t zbase = cbase[0];
+#pragma unroll
+    for (int m = 1; m < MT; ++m) zbase = wave == m ? cbase[m] : zbase;
+
+    f32x16 o;
+    auto compute = [&](const Step &r, int xstage, int kstage) {
+        const char *tx = smem + XRING + xstage * TILEB, *ty = smem + kstage * 2 * TILEB, *tz = ty + TILEB;
+        const bool part = r.n < C;
+        if (r.first) read_state(r);
+        // (steps are fenced, so that the reads stay a step or two ahead of their
+        // MFMAs and the registers hold no more than that)
+        bf16x8 zf[2] = {col_of(tz, 0, zbase), col_of(tz, 1, zbase)};
+        if (part) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                u32x4 zr = __builtin_bit_cast(u32x4, zf[s]);
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    zr[h] &= (is_token(key(8 * s + 2 * h), r.n) ? 0xFFFFu : 0u) | (is_token(key(8 * s + 2 * h + 1), r.n) ? 0xFFFF0000u : 0u);
+                zf[s] = __builtin_bit_cast(bf16x8, zr);
+            }
+        }
+        if constexpr (OUT) {
+            const f32x16 zero = {};
+            f32x16 p = zero;
+            constexpr int RA = 3;   // fragments in flight
+            bf16x8 xf[RA], yf[RA];
+#pragma unroll
+            for (int s = 0; s + 1 < RA; ++s) xf[s] = row_frag(tx, s), yf[s] = row_frag(ty, s);
+            // P^T (and, once a chunk, S^T X^T)
+            auto products = [&](auto inter) {
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    const int nx = s + RA - 1;
+                    if (nx < KS) xf[nx % RA] = row_frag(tx, nx), yf[nx % RA] = row_frag(ty, nx);
+                    p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yf[s % RA], xf[s % RA], s ? p : zero, 0, 0, 0);
+                    if constexpr (decltype(inter)::value) {
+                        float x[8];
+                        bf16x8 sf[PS];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = S[s / 2][8 * (s & 1) + e];
+                        parts_of<PS>(x, sf);
+#pragma unroll
+                        for (int c = 0; c < PS; ++c)
+                            o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(sf[c], xf[s % RA], s + c ? o : zero, 0, 0, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            if (SETS != KEYS || r.set == 0) {
+                products(std::true_type{});
+                float hd = head;
+                if (part) {
+                    int n = r.n;
+                    asm volatile("" : "+s"(n));
+                    hd = fast_exp2(max(REV ? n - 1 - l32 : l32 + 1 - (C - n), 0) * l2) * a.scale;
+                }
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[v] *= hd;
+            } else {
+                products(std::false_type{});
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                float x[8];
+                bf16x8 pf[PP];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int v = 8 * s + e;
+                    x[e] = p[v] * pw[v];
+                }
+                parts_of<PP>(x, pf);
+#pragma unroll
+                for (int c = 0; c < PP; ++c) o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(zf[s], pf[c], o, 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // the state behind the chunk
+        auto advance = [&](const Decay &dec) {
+            if (SETS != KEYS || r.set == 0) {
+                if (dec.slow) {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) S[m][v] = __builtin_fmaf(S[m][v], dec.by, S[m][v]);
+                } else {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) S[m][v] *= dec.by;
+                }
+            }
+            // pairs of row blocks, the next pair's fragments read one pair ahead
+            bf16x8 yt[2][2], zw[3];
+            yt[0][0] = col_frag(ty, 0, 0), yt[0][1] = col_frag(ty, 0, 1);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {   // k-step i / (MT / 2), row blocks 2 (i % (MT / 2)) and the next
+                const int s = i / (MT / 2), m = 2 * (i % (MT / 2)), nx = i + 1;
+                if (i % (MT / 2) == 0) {
+                    float x[8];
+                    const u32x4 zr = __builtin_bit_cast(u32x4, zf[s]);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        x[2 * h] = __uint_as_float(zr[h] << 16) * kw[8 * s + 2 * h];
+                        x[2 * h + 1] = __uint_as_float(zr[h] & 0xFFFF0000u) * kw[8 * s + 2 * h + 1];
+                    }
+                    parts_of<3>(x, zw);
+                }
+                if (nx < MT) {
+                    const int s1 = nx / (MT / 2), m1 = 2 * (nx % (MT / 2));
+                    yt[nx & 1][0] = col_frag(ty, s1, m1), yt[nx & 1][1] = col_frag(ty, s1, m1 + 1);
+                }
+#pragma unroll
+                for (int c = 0; c < 3; ++c) {
+                    S[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yt[i & 1][0], zw[c], S[m], 0, 0, 0);
+                    S[m + 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yt[i & 1][1], zw[c], S[m + 1], 0, 0, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        // (of several query heads the last one brings the state on)
+        if (SETS != ROWS || !OUT || r.set == a.sets - 1) {
+            Decay dec = whole;
+            if (part) {
+                int n = r.n;
+                asm volatile("" : "+s"(n));   // (a real branch)
+                dec = decay_of(n * ld);
+            }
+            advance(dec);
+        }
+        if constexpr (OUT) {
+            if (SETS != KEYS || r.set == a.sets - 1) {
+                const int64_t at = (int64_t)(r.t + l32 - (REV ? 0 : C - r.n)) * job.o_st + row_head(r) * job.o_sh + 32 * wave;
+                held_n = r.n;
+                if constexpr (F32) {
+                    held_to = (char *)((float *)job.out + at + 4 * hf);
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) held[g][e] = __float_as_uint(o[4 * g + e]);
+                } else {
+                    // (after the swap a lane holds 8 neighbouring dims)
+                    held_to = (char *)((uint16_t *)job.out + at + 8 * hf);
+#pragma unroll
+                    for (int g = 0; g < 2; ++g)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const u32x2 x = __builtin_amdgcn_permlane32_swap(
+                                pack_bf16x2(o[8 * g + 2 * h], o[8 * g + 2 * h + 1]),
+                                pack_bf16x2(o[8 * g + 4 + 2 * h], o[8 * g + 5 + 2 * h]), false, false);
+                            held[g][h] = x[0];
+                            held[g][2 + h] = x[1];
+                        }
+                }
+            }
+            if (r.last && r.own_last && a.state_out && jn == 0)
+                write_state(a.state_out + ((int64_t)(a.out_by_slot ? ld_uniform(a.slots, r.seq) : r.seq) * a.Hkv + kvh) * (D * D),
+                            a.out_scale);
+        } else if (r.last) {
+            write_state(a.cells + ((int64_t)(REV ? cell - 1 : cell + 1) * a.Hkv + kvh) * (D * D), 1.f);
+        }
+    };
+
+    // ---- pipeline ------------------------------------------------------------------
+    // At the barrier of step c its tiles have landed and every wave is done with
+    // step c - 1, whose row stage the loads of step c + 2 take.  (Two key stages: the
+    // loads of the next chunk's keys stand at least one step behind this chunk's
+    // first, after every wave's last read of the chunk before.)
+    auto inc = [](int i, int n) -> int { return i + 1 == n ? 0 : i + 1; };
+    Step r0 = walk.next(), r1 = walk.next();
+    int x0 = 0, k0 = 0, k1 = loads_keys(r1) ? inc(0, NYZ) : 0;   // stages of r0 and r1
+    issue(r0, 0, 0);
+    if (r1.live) issue(r1, 1, k1);
+    while (r0.live) {
+        if (!r1.live) wait_vm_lgkm<0>();
+        else if (loads_keys(r1)) wait_vm_lgkm<(OUT ? 3 : 2) * NI>();
+        else wait_vm_lgkm<NI>();
+        wg_barrier();
+        if constexpr (OUT) {
+            store_held();
+            held_n = 0;
+        }
+        const Step r2 = walk.next();   // (not live past the end)
+        const int k2 = loads_keys(r2) ? inc(k1, NYZ) : k1;
+        if (r2.live) issue(r2, x0 == 0 ? 2 : x0 - 1, k2);
+        compute(r0, x0, k0);
+        r0 = r1;
+        r1 = r2;
+        k0 = k1;
+        k1 = k2;
+        x0 = inc(x0, 3);
+    }
+    if constexpr (OUT) store_held();
+}
+
+// Joins the cells' states: where the sequence at a cell's edge began before the
+// whole cell, the state there is the cell's own plus g^cell_len times the one at
+// its other edge.  A work-group takes 256 elements of a KV head's states, edge
+// by edge.
+template <bool REV>
+__global__ __launch_bounds__(64) void linear_scan_kernel(const LinearArgs a, int elems) {
+    __shared__ uint8_t kind[LIN_MAX_CELLS];   // of each cell's state: 0 none, 1 the neighbour cell's alone, 2 joined
+    const int kvh = blockIdx.y;
+    for (int c = threadIdx.x; c < a.ncells; c += 64) {
+        int k = 0;
+        // the edge this cell's state stands at, and the far edge of the neighbour it came over
+        const int64_t edge = REV ? (int64_t)(c + 1) * a.cell_len : (int64_t)c * a.cell_len;
+        const int64_t far = REV ? edge + a.cell_len : edge - a.cell_len;
+        if (edge > 0 && edge < a.T) {
+            int lo = 0, hi = a.S;   // the sequence of token edge
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (a.seqs[mid] <= edge) lo = mid;
+                else hi = mid;
+            }
+            const int begin = a.seqs[lo], end = a.seqs[lo + 1];
+            if (begin < edge) k = (REV ? end > far : begin < far) ? 2 : 1;
+        }
+        kind[c] = (uint8_t)k;
+    }
+    __syncthreads();
+    const float full = expf(a.cell_len * log_decay_of(a.log_decay, kvh));
+    float *p = a.cells + (int64_t)kvh * elems + (int64_t)blockIdx.x * 256 + 4 * threadIdx.x;
+    const int64_t stride = (int64_t)a.Hkv * elems;
+    constexpr int AHEAD = 16;
+    f32x4 run = {0.f, 0.f, 0.f, 0.f};
+    for (int c0 = 0; c0 < a.ncells; c0 += AHEAD) {
+        f32x4 x[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int c = REV ? a.ncells - 1 - c0 - i : c0 + i;
+            if (c0 + i < a.ncells && kind[c]) x[i] = *(const f32x4 *)(p + c * stride);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int c = REV ? a.ncells - 1 - c0 - i : c0 + i;
+            if (c0 + i >= a.ncells || !kind[c]) continue;
+            if (kind[c] == 2) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[i][e] = __builtin_fmaf(run[e], full, x[i][e]);
+                *(f32x4 *)(p + c * stride) = x[i];
+            }
+            run = x[i];
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void linear_empty_kernel(const LinearArgs a, int elems) {
+    const int s = blockIdx.x, kvh = blockIdx.y;
+    if (a.seqs[s] != a.seqs[s + 1]) return;
+    const int64_t in = (int64_t)(a.slots ? a.slots[s] : s) * a.Hkv + kvh, out = a.out_by_slot ? in : (int64_t)s * a.Hkv + kvh;
+    for (int i = threadIdx.x; i < elems; i += 256)
+        a.state_out[out * elems + i] = a.state_in ? a.state_in[in * elems + i] * a.in_scale * a.out_scale : 0.f;
+}
+
+__global__ __launch_bounds__(256) void linear_commit_kernel(const float *from, float *pool, const int32_t *slots, int hkv, int elems) {
+    const int per = elems / 1024, s = blockIdx.x / per, kvh = blockIdx.y;
+    const f32x4 *f = (const f32x4 *)(from + ((int64_t)s * hkv + kvh) * elems);
+    f32x4 *t = (f32x4 *)(pool + ((int64_t)slots[s] * hkv + kvh) * elems);
+    const int i = blockIdx.x % per * 256 + threadIdx.x;
+    t[i] = f[i];
+}
+
+// A few new tokens against the states in memory, one after the other: with S
+// the state's D x 32 columns of a wave in registers,
+//   S = g S + k v^T,   o = scale q S   for each query head.
+// Bound by reading and writing the states, 4 D^2 bytes each, while a token
+// takes (2 + G) D^2 FMAs per KV head.  A lane holds 4 neighbouring columns of
+// every eighth row, so a load instruction covers eight 128-byte pieces, and the
+// rows' sums meet in three lane exchanges; no barrier, no LDS.
+template <int D, bool F32>
+__global__ __launch_bounds__(64) void linear_step_kernel(const LinearStepArgs a) {
+    constexpr int NR = D / 8;
+    const int lane = threadIdx.x, cg = lane & 7, rg = lane >> 3;
+    const int part = blockIdx.x % (D / 32);
+    const uint32_t bh = blockIdx.x / (D / 32);
+    const int b = (int)fastdiv(bh, a.fd_hkv), kvh = (int)(bh - (uint32_t)b * (uint32_t)a.Hkv);
+    const int n = a.new_lens ? ld_uniform(a.new_lens, b) : a.Ln;
+    if (n == 0) return;
+    const int col = 32 * part + 4 * cg;
+    float *p = a.pool + ((int64_t)ld_uniform(a.slots, b) * a.Hkv + kvh) * (D * D) + rg * D + col;
+    f32x4 S[NR];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) S[i] = *(const f32x4 *)(p + 8 * i * D);
+    const Decay dec = decay_of(log_decay_of(a.log_decay, kvh));
+    const uint32_t keep = dec.slow ? ~0u : 0u;
+    const uint16_t *q = a.q + b * a.q_sb + (int64_t)kvh * a.G * a.q_sh + rg;
+    const uint16_t *k = a.k + b * a.k_sb + kvh * a.k_sh + rg;
+    const uint16_t *v = a.v + b * a.v_sb + kvh * a.v_sh + col;
+    for (int t = 0; t < n; ++t) {
+        const u32x2 vr = *(const u32x2 *)(v + t * a.v_st);
+        const f32x4 vv = {__uint_as_float(vr[0] << 16), __uint_as_float(vr[0] & 0xFFFF0000u), __uint_as_float(vr[1] << 16),
+                          __uint_as_float(vr[1] & 0xFFFF0000u)};
+        float kf[NR];
+#pragma unroll
+        for (int i = 0; i < NR; ++i) kf[i] = __uint_as_float((uint32_t)k[t * a.k_st + 8 * i] << 16);
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float kept = __uint_as_float(__float_as_uint(S[i][e]) & keep);   // S of a slow head, else 0
+                S[i][e] = __builtin_fmaf(kf[i], vv[e], __builtin_fmaf(S[i][e], dec.by, kept));
+            }
+        for (int g = 0; g < a.G; ++g) {
+            f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                const float x = __uint_as_float((uint32_t)q[t * a.q_st + g * a.q_sh + 8 * i] << 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(x, S[i][e], o[e]);
+            }
+#pragma unroll
+            for (int m = 8; m < 64; m *= 2)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], m);
+            if (rg == 0) {
+                const int64_t at = b * a.o_sb + t * a.o_st + (int64_t)(kvh * a.G + g) * a.o_sh + col;
+                if constexpr (F32) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] *= a.scale;
+                    *(f32x4 *)((float *)a.out + at) = o;
+                } else {
+                    *(u32x2 *)((uint16_t *)a.out + at) = u32x2{pack_bf16x2(o[0] * a.scale, o[1] * a.scale),
+                                                              pack_bf16x2(o[2] * a.scale, o[3] * a.scale)};
+                }
+            }
+        }
+    }
+    if (a.commit)
+#pragma unroll
+        for (int i = 0; i < NR; ++i) *(f32x4 *)(p + 8 * i * D) = S[i];
+}
+
+template <int D, bool REV>
+int linear_t(const LinearArgs &a, hipStream_t st) {
+    const dim3 grid(a.per_xcd * NUM_XCD), block(2 * D);
+    // (gradients are bf16; backwards the sets are of keys, forwards of rows)
+    constexpr int MANY = REV ? KEYS : ROWS;
+    if (a.out_f32 && !REV) {
+        if (a.sets > 1) hipLaunchKernelGGL((linear_kernel<D, REV, !REV, true, MANY>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((linear_kernel<D, REV, !REV, true, ONE>), grid, block, 0, st, a);
+    } else {
+        if (a.sets > 1) hipLaunchKernelGGL((linear_kernel<D, REV, false, true, MANY>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((linear_kernel<D, REV, false, true, ONE>), grid, block, 0, st, a);
+    }
+    return (int)hipGetLastError();
+}
+
+template <int D, bool REV>
+int cells_t(LinearArgs a, hipStream_t st) {
+    a.n_work = a.ncells * a.Hkv;
+    a.per_xcd = (a.n_work + NUM_XCD - 1) / NUM_XCD;
+    const dim3 grid(a.per_xcd * NUM_XCD), block(2 * D);
+    // (forwards the states do not depend on the row heads)
+    if (REV && a.sets > 1) hipLaunchKernelGGL((linear_kernel<D, REV, false, false, REV ? KEYS : ONE>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((linear_kernel<D, REV, false, false, ONE>), grid, block, 0, st, a);
+    if (int e = (int)hipGetLastError()) return e;
+    hipLaunchKernelGGL((linear_scan_kernel<REV>), dim3(D * D / 256, a.Hkv), dim3(64), 0, st, a, D * D);
+    return (int)hipGetLastError();
+}
+
+}  // namespace
+
+int launch_linear(const LinearArgs &a, bool backwards, int head_dim, void *stream) {
+    hipStream_t st = (hipStream_t)stream;
+    if (head_dim == 128) return backwards ? linear_t<128, true>(a, st) : linear_t<128, false>(a, st);
+    if (head_dim == 64) return backwards ? linear_t<64, true>(a, st) : linear_t<64, false>(a, st);
+    return (int)hipErrorInvalidValue;
+}
+
+int launch_linear_cells(const LinearArgs &a, bool backwards, int head_dim, void *stream) {
+    hipStream_t st = (hipStream_t)stream;
+    if (a.ncells > LIN_MAX_CELLS) return (int)hipErrorInvalidValue;
+    if (head_dim == 128) return backwards ? cells_t<128, true>(a, st) : cells_t<128, false>(a, st);
+    if (head_dim == 64) return backwards ? cells_t<64, true>(a, st) : cells_t<64, false>(a, st);
+    return (int)hipErrorInvalidValue;
+}
+
+int launch_linear_empty(const LinearArgs &a, int head_dim, void *stream) {
+    hipLaunchKernelGGL(linear_empty_kernel, dim3(a.S, a.Hkv), dim3(256), 0, (hipStream_t)stream, a, head_dim * head_dim);
+    return (int)hipGetLastError();
+}
+
+int launch_linear_commit(const float *from, float *pool, const int32_t *slots, int32_t S, int32_t hkv, int head_dim, void *stream) {
+    const int elems = head_dim * head_dim;
+    hipLaunchKernelGGL(linear_commit_kernel, dim3((unsigned)(elems / 1024) * S, hkv), dim3(256), 0, (hipStream_t)stream, from, pool, slots, hkv, elems);
+    return (int)hipGetLastError();
+}
+
+int launch_linear_step(const LinearStepArgs &a, int head_dim, void *stream) {
+    hipStream_t st = (hipStream_t)stream;
+    const dim3 grid((unsigned)a.B * a.Hkv * (head_dim / 32)), block(64);
+    if (head_dim == 128) {
+        if (a.out_f32) hipLaunchKernelGGL((linear_step_kernel<128, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((linear_step_kernel<128, false>), grid, block, 0, st, a);
+    } else {
+        if (a.out_f32) hipLaunchKernelGGL((linear_step_kernel<64, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((linear_step_kernel<64, false>), grid, block, 0, st, a);
+    }
+    return (int)hipGetLastError();
+}
+
+}  // namespace ws
