@@ -587,6 +587,73 @@ size_t ws_step_workspace_bytes_4bit(int32_t batch, int32_t num_q_heads, int32_t 
                                     const int32_t *new_lens_host);
 
 /*
+ * ws_block_causal_prefill_packed -- attention over whole sequences of different
+ * lengths that stand one behind the other in one token axis, without padding
+ * (prompts of a serving batch, documents of a training step).  A token sees its
+ * own sequence only.
+ *   q:    bf16 [total_tokens][num_q_heads][head_dim] (stride_b is not used)
+ *   k, v: bf16 [total_tokens][num_kv_heads][head_dim]
+ *   seq_offsets_host / _dev: int32 [num_seqs + 1], same values: sequence s is the
+ *         tokens [seq_offsets[s], seq_offsets[s + 1]); first 0, non-decreasing,
+ *         last at most total_tokens.  Sequences may have no token.
+ *   block_offsets_host / _dev: NULL and num_blocks 0: causal, token i of a
+ *         sequence that begins at a sees a <= j <= i.  Or int32 [num_blocks + 1],
+ *         same values, in the packed axis: first 0, non-decreasing, last the end of
+ *         the last sequence, and every sequence begins at a block's beginning;
+ *         token i then sees the j >= a of ws_block_causal_prefill.
+ *   text_starts_host / _dev: NULL, or (with blocks) int32 [num_blocks] in the packed
+ *         axis, as ws_block_causal_prefill_text
+ *   out:  bf16 or f32 [total_tokens][num_q_heads][head_dim]; lse: NULL or device
+ *         f32 [num_q_heads][total_tokens]; rows behind the last sequence are left as
+ *         they were
+ * f32 outputs hold f32 accuracy (as ws_block_causal_attn_fwd_window's).
+ * A key or value that is not finite reaches no sequence of more than 256 tokens but
+ * its own; sequences of up to 256 tokens that are neighbours may share a tile.
+ * (Past 512 tiles of 256 tokens, or 2^24 tokens, tiles may be shared by any
+ * neighbours.)
+ * total_tokens must not exceed 2^31 - 257 (WS_ERR_SHAPE).
+ * Errors: WS_ERR_NULL, WS_ERR_SHAPE, WS_ERR_UNSUPPORTED, WS_ERR_ALIGN,
+ * WS_ERR_HEADS, WS_ERR_OFFSETS, WS_ERR_HIP.
+ */
+int ws_block_causal_prefill_packed(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v,
+                                   const int32_t *seq_offsets_host, const int32_t *seq_offsets_dev,
+                                   const int32_t *block_offsets_host, const int32_t *block_offsets_dev,
+                                   const int32_t *text_starts_host, const int32_t *text_starts_dev,
+                                   int32_t num_seqs, int32_t total_tokens, int32_t num_blocks,
+                                   int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                   float scale, ws_tensor4 out, float *lse, void *stream);
+
+/*
+ * ws_block_causal_prefill_packed_bwd -- gradients of
+ * ws_block_causal_prefill_packed.  Arguments and errors as the forward's, and as
+ * ws_block_causal_prefill_bwd
+ *   o, dout:    bf16, as q; o is the forward's output, lse its lse
+ *   dq, dk, dv: all f32, or all bf16; rows behind the last sequence are left as
+ *               they were
+ *   workspace:  ws_prefill_packed_bwd_workspace_bytes(...) bytes, 16-byte aligned;
+ *               8 * num_q_heads * total_tokens bytes (rounded up to 256) + 8 *
+ *               total_tokens are enough to run, unsplit
+ * total_tokens must be below 2^30.  Deterministic, and as exact, as
+ * ws_block_causal_prefill_bwd.
+ */
+int ws_block_causal_prefill_packed_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 o,
+                                       ws_tensor4 dout, const float *lse,
+                                       const int32_t *seq_offsets_host, const int32_t *seq_offsets_dev,
+                                       const int32_t *block_offsets_host, const int32_t *block_offsets_dev,
+                                       const int32_t *text_starts_host, const int32_t *text_starts_dev,
+                                       int32_t num_seqs, int32_t total_tokens, int32_t num_blocks,
+                                       int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                       float scale, ws_tensor4 dq, ws_tensor4 dk, ws_tensor4 dv,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Workspace bytes of ws_block_causal_prefill_packed_bwd, with room for the sums it
+ * would split on a whole chip, whatever the sequences' lengths (host arithmetic).
+ * 0 for invalid arguments.
+ */
+size_t ws_prefill_packed_bwd_workspace_bytes(int32_t total_tokens, int32_t num_q_heads, int32_t num_kv_heads);
+
+/*
  * Linear attention with a decay for each head: a layer whose memory of a session
  * is one head_dim x head_dim state per KV head, whatever the session's length.
  * With g = exp(log_decay[h]) of KV head h, token i of a sequence has

@@ -21,6 +21,8 @@ lengths padded to a common one)
 and a sliding window of the latest)
   PagedCache4: a cache held in 4 bits; kv_append and block_causal_attn_fwd take it,
   kv_read(cache, starts, length) returns what it holds
+  block_causal_prefill_packed, block_causal_prefill_packed_bwd,
+  prefill_packed_bwd_workspace_bytes: sequences of different lengths without padding (packed.py)
   LinearState, linear_attn_prefill, linear_attn_step, linear_attn_prefill_bwd,
   linear_workspace_bytes: linear attention with a decay for each head (linear.py)
   workspace_bytes(op, batch, num_q_heads, num_kv_heads, max_q, max_k)
@@ -41,7 +43,8 @@ from . import build as _build
 __all__ = ["WsError", "PagedCache", "PagedCache4", "kv_append", "kv_read", "block_causal_attn_fwd", "block_causal_attn_fwd_noalloc",
            "block_causal_prefill", "block_causal_prefill_bwd", "workspace_bytes",
            "step_workspace_bytes_varlen", "step_workspace_bytes_window", "step_workspace_bytes_4bit",
-           "prefill_window_bwd_workspace_bytes", "step_plan", "LinearState", "linear_attn_prefill", "linear_attn_step",
+           "prefill_window_bwd_workspace_bytes", "step_plan", "block_causal_prefill_packed",
+           "block_causal_prefill_packed_bwd", "prefill_packed_bwd_workspace_bytes", "LinearState", "linear_attn_prefill", "linear_attn_step",
            "linear_attn_prefill_bwd", "linear_workspace_bytes", "library",
            "abi_version", "WS_OP_STEP", "WS_OP_PREFILL", "WS_OP_PREFILL_BWD", "PAGE_SIZE"]
 
@@ -164,6 +167,7 @@ def library():
             Tensor4, Tensor4, Tensor4, KV4, P, P, P, P, P, P, I32, I32, I32, F, I32, Tensor4, P, P, ctypes.c_size_t, P]
         lib.ws_step_workspace_bytes_4bit.restype = ctypes.c_size_t
         lib.ws_step_workspace_bytes_4bit.argtypes = [I32, I32, I32, I32, P, P]
+        packed.declare(lib)
         linear.declare(lib)
         if lib.ws_abi_version() != 5:
             raise RuntimeError("libwsattn.so ABI version mismatch")
@@ -190,6 +194,8 @@ def _bind_native(lib):
         "ws_block_causal_prefill_window_bwd", "ws_prefill_window_bwd_workspace_bytes")))
     _NATIVE.bind_cache4(PagedCache4, *(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
         "ws_kv_append_4bit", "ws_kv_read_4bit", "ws_block_causal_attn_fwd_4bit", "ws_step_workspace_bytes_4bit")))
+    _NATIVE.bind_packed(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
+        "ws_block_causal_prefill_packed", "ws_block_causal_prefill_packed_bwd", "ws_prefill_packed_bwd_workspace_bytes")))
     _NATIVE.bind_linear(LinearState, *(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in (
         "ws_linear_attn_prefill", "ws_linear_attn_step", "ws_linear_attn_prefill_bwd", "ws_linear_workspace_bytes")))
 
@@ -774,6 +780,8 @@ def block_causal_prefill_bwd(q, k, v, o, dout, lse, block_offsets, scale=None, t
 
 
 # (the helpers above are theirs too)
-from . import linear  # noqa: E402
+from . import linear, packed  # noqa: E402
 from .linear import (LinearState, linear_attn_prefill, linear_attn_prefill_bwd, linear_attn_step,  # noqa: E402
                      linear_workspace_bytes)
+from .packed import (block_causal_prefill_packed, block_causal_prefill_packed_bwd,  # noqa: E402
+                     prefill_packed_bwd_workspace_bytes)

@@ -13,7 +13,8 @@ LIB = os.path.join(HERE, "libwsattn.so")
 DEVICE_SOURCES = [os.path.join(CSRC, "ws_kernels.hip"), os.path.join(CSRC, "ws_bwd.hip"),
                   os.path.join(CSRC, "ws_cache4.hip"), os.path.join(CSRC, "ws_linear.hip"),
                   os.path.join(CSRC, "ws_device.hip")]
-HOST_SOURCES = [os.path.join(CSRC, "ws_api.cpp"), os.path.join(CSRC, "ws_api4.cpp"), os.path.join(CSRC, "ws_api_linear.cpp")]
+HOST_SOURCES = [os.path.join(CSRC, "ws_api.cpp"), os.path.join(CSRC, "ws_api4.cpp"), os.path.join(CSRC, "ws_api_linear.cpp"),
+                os.path.join(CSRC, "ws_api_pack.cpp")]
 SOURCES = DEVICE_SOURCES + HOST_SOURCES + [os.path.join(CSRC, "ws_binding.cpp")]
 HEADERS = [os.path.join(CSRC, "ws_kernels.h"), os.path.join(CSRC, "ws_host.h"), os.path.join(CSRC, "ws_device_util.h"),
            os.path.join(CSRC, "ws_cache4.h"), os.path.join(CSRC, "ws_linear.h"), os.path.join(os.path.dirname(HERE), "include", "ws_attn.h")]

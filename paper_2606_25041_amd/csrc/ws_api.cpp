@@ -233,7 +233,6 @@ bool parts_only(const StepPlan &p, int64_t max_k, bool out_f32) {
 // Time, in tiles, of work-groups taken longest first by `cus` compute units:
 // groups of n equal items of `size` tiles, sizes not increasing.  Units with
 // the same load are kept together, so a round costs one entry.
-struct ItemGroup { int size, n; };
 int dispatch_time(int cus, const ItemGroup *groups, int ngroups) {
     int total = 0;
     for (int g = 0; g < ngroups; ++g) total += groups[g].n;
@@ -264,8 +263,6 @@ int dispatch_time(int cus, const ItemGroup *groups, int ngroups) {
     return q[len - 1].at;
 }
 
-// rounds of work-groups up to which their order is the launch's time
-constexpr int64_t FEW_ROUNDS = 6;
 
 // Query tile of a prefill: 256 rows, or 128 rows whose keys the work-group's
 // two halves share (items half as long, twice as many), where few items leave

@@ -55,6 +55,12 @@ struct Cache4Abi {
     decltype(&ws_step_workspace_bytes_4bit) step_bytes;
 } abi4;
 
+struct PackedAbi {
+    decltype(&ws_block_causal_prefill_packed) prefill;
+    decltype(&ws_block_causal_prefill_packed_bwd) bwd;
+    decltype(&ws_prefill_packed_bwd_workspace_bytes) bwd_bytes;
+} pabi;
+
 struct LinearAbi {
     decltype(&ws_linear_attn_prefill) prefill;
     decltype(&ws_linear_attn_step) step;
@@ -91,6 +97,11 @@ PyObject *bind_cache4(PyObject *, PyObject *const *args, Py_ssize_t n) {
     }
     Py_INCREF(args[0]);
     Py_XSETREF(cache4_class, args[0]);
+    Py_RETURN_NONE;
+}
+
+PyObject *bind_packed(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (!take_addresses((void **)&pabi, sizeof pabi / sizeof(void *), args, n)) return nullptr;
     Py_RETURN_NONE;
 }
 
@@ -703,6 +714,103 @@ bool offsets_of(PyObject *o, Ints &x, int64_t &num) {
     return int_pair(o, {num + 1}, false, x);
 }
 
+// Block offsets [nb + 1] and segment starts [nb] of a packed call; None: causal
+bool blocks_of(PyObject *o, PyObject *t, Ints &blocks, Ints &text, int64_t &nb) {
+    nb = 0;
+    if (o == Py_None) return t == Py_None;
+    return offsets_of(o, blocks, nb) && int_pair(t, {nb}, true, text);
+}
+
+// packed_prefill(q, k, v, seq_offsets, block_offsets, scale, out, out_dtype, want_lse,
+//                lse, text_starts) -> (status, out, lse), or None
+PyObject *packed_prefill(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    new_call();
+    if (n != 11) Py_RETURN_NONE;
+    const at::Tensor *q = tensor(a[0]), *k = tensor(a[1]);
+    if (!q || q->dim() != 3 || !k || k->dim() != 3) Py_RETURN_NONE;
+    const int64_t T = q->size(0), H = q->size(1), D = q->size(2), hkv = k->size(1);
+    if (T == 0 || T > INT32_MAX) Py_RETURN_NONE;
+    ws_tensor4 qd, kd, vd, od;
+    Ints off, blocks, text;
+    int64_t S, nb;
+    float scale;
+    bool want_lse;
+    if (!packed_tokens(q, {T, H, D}, qd) || !packed_tokens(k, {T, hkv, D}, kd) ||
+        !packed_tokens(tensor(a[2]), {T, hkv, D}, vd) || !offsets_of(a[3], off, S) ||
+        !blocks_of(a[4], a[10], blocks, text, nb) || !scale_of(a[5], D, scale) || !flag(a[8], want_lse))
+        Py_RETURN_NONE;
+    const at::ScalarType type = a[6] == Py_None ? dtype_of(a[7]) : at::kBFloat16;
+    if (type != at::kBFloat16 && type != at::kFloat) Py_RETURN_NONE;
+    at::Tensor out, lse;
+    const bool with_lse = want_lse || a[9] != Py_None;
+    if (!given(a[6], {T, H, D}, out) || (out.defined() && !packed_tokens(&out, {T, H, D}, od)) ||
+        !given(a[9], {H, T}, lse) || (lse.defined() && !packed_f32(lse)))
+        Py_RETURN_NONE;
+    int rc;
+    {
+        NoGil free;
+        allocate(out, {T, H, D}, type, *q);
+        packed_tokens(&out, {T, H, D}, od);
+        if (with_lse) allocate(lse, {H, T}, at::kFloat, *q);
+        rc = pabi.prefill(qd, kd, vd, off.host, off.dev, blocks.host, blocks.dev, text.host, text.dev, S, T, nb, H, hkv, D, scale,
+                          od, lse.defined() ? (float *)lse.data_ptr() : nullptr, stream());
+    }
+    return result(rc, {out, lse});
+    END_HANDLE_TH_ERRORS
+}
+
+// packed_bwd(q, k, v, o, dout, lse, seq_offsets, block_offsets, scale, text_starts, dq,
+//            dk, dv, workspace, grad_dtype) -> (status, dq, dk, dv), or None
+PyObject *packed_bwd(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    new_call();
+    if (n != 15) Py_RETURN_NONE;
+    const at::Tensor *q = tensor(a[0]), *k = tensor(a[1]), *lse = tensor(a[5]);
+    if (!q || q->dim() != 3 || !k || k->dim() != 3 || !lse) Py_RETURN_NONE;
+    const int64_t T = q->size(0), H = q->size(1), D = q->size(2), hkv = k->size(1);
+    if (T == 0 || T > INT32_MAX) Py_RETURN_NONE;
+    ws_tensor4 qd, kd, vd, od, dd, dqd, dkd, dvd;
+    Ints off, blocks, text;
+    int64_t S, nb;
+    float scale;
+    if (!packed_tokens(q, {T, H, D}, qd) || !packed_tokens(k, {T, hkv, D}, kd) ||
+        !packed_tokens(tensor(a[2]), {T, hkv, D}, vd) || !packed_tokens(tensor(a[3]), {T, H, D}, od) ||
+        !packed_tokens(tensor(a[4]), {T, H, D}, dd) || !here(*lse) || !shaped(*lse, {H, T}) || !packed_f32(*lse) ||
+        !offsets_of(a[6], off, S) || !blocks_of(a[7], a[9], blocks, text, nb) || !scale_of(a[8], D, scale))
+        Py_RETURN_NONE;
+    const at::ScalarType grads = dtype_of(a[14]);
+    const at::Tensor *wsp = a[13] == Py_None ? nullptr : tensor(a[13]);
+    if (a[13] != Py_None && !packed(wsp, 1)) Py_RETURN_NONE;
+    at::Tensor dq, dk, dv, own;
+    if (!given(a[10], {T, H, D}, dq) || (dq.defined() && !packed_tokens(&dq, {T, H, D}, dqd)) ||
+        !given(a[11], {T, hkv, D}, dk) || (dk.defined() && !packed_tokens(&dk, {T, hkv, D}, dkd)) ||
+        !given(a[12], {T, hkv, D}, dv) || (dv.defined() && !packed_tokens(&dv, {T, hkv, D}, dvd)))
+        Py_RETURN_NONE;
+    int rc = -1;
+    {
+        NoGil free;
+        const size_t need = wsp ? 0 : pabi.bwd_bytes(T, H, hkv);
+        if (wsp || need) {
+            allocate(dq, {T, H, D}, grads, *q);
+            allocate(dk, {T, hkv, D}, grads, *q);
+            allocate(dv, {T, hkv, D}, grads, *q);
+            packed_tokens(&dq, {T, H, D}, dqd);
+            packed_tokens(&dk, {T, hkv, D}, dkd);
+            packed_tokens(&dv, {T, hkv, D}, dvd);
+            if (!wsp) {
+                own = at::empty({(int64_t)need}, q->options().dtype(at::kByte));
+                wsp = &own;
+            }
+            rc = pabi.bwd(qd, kd, vd, od, dd, (const float *)lse->data_ptr(), off.host, off.dev, blocks.host, blocks.dev, text.host,
+                          text.dev, S, T, nb, H, hkv, D, scale, dqd, dkd, dvd, wsp->data_ptr(), wsp->numel(), stream());
+        }
+    }
+    if (rc < 0) Py_RETURN_NONE;   // (the Python code names the mistake)
+    return result(rc, {dq, dk, dv});
+    END_HANDLE_TH_ERRORS
+}
+
 // linear_prefill(q, k, v, log_decay, seq_offsets, scale, state, reset, commit, out,
 //                out_dtype, workspace) -> (status, out), or None
 PyObject *linear_prefill(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -848,6 +956,9 @@ PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)())bind, METH_FASTCALL, "the cache class, then the C ABI's addresses in Abi's order"},
     {"bind_window", (PyCFunction)(void (*)())bind_window, METH_FASTCALL, "the windowed ABI's addresses in WindowAbi's order"},
     {"bind_cache4", (PyCFunction)(void (*)())bind_cache4, METH_FASTCALL, "PagedCache4, then the 4-bit ABI's addresses"},
+    {"bind_packed", (PyCFunction)(void (*)())bind_packed, METH_FASTCALL, "the packed ABI's addresses in PackedAbi's order"},
+    {"packed_prefill", (PyCFunction)(void (*)())packed_prefill, METH_FASTCALL, nullptr},
+    {"packed_bwd", (PyCFunction)(void (*)())packed_bwd, METH_FASTCALL, nullptr},
     {"bind_linear", (PyCFunction)(void (*)())bind_linear, METH_FASTCALL, "LinearState, then the linear ABI's addresses"},
     {"linear_prefill", (PyCFunction)(void (*)())linear_prefill, METH_FASTCALL, nullptr},
     {"linear_step", (PyCFunction)(void (*)())linear_step, METH_FASTCALL, nullptr},

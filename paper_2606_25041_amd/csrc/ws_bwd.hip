@@ -6,11 +6,21 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "ws_kernels.h"
 #include "ws_device_util.h"
 
 namespace ws {
 namespace {
+
+// the launch's plan beside its arguments (packed sequences)
+struct NoPlan {};
+template <int WIN>
+using RowPlan = std::conditional_t<WIN == 2, PackPlan, NoPlan>;
+template <int WIN>
+using KeyPlan = std::conditional_t<WIN == 2, PackBwdPlan, NoPlan>;
+
 
 constexpr int KB_DKDV = 16;   // key tiles of one group taken together on an XCD (dK/dV)
 constexpr int AH = 2;         // LDS operand reads issued this many MFMAs ahead
@@ -75,14 +85,14 @@ __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w 
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
 // Loads rows [r0, r0 + nrows) of a [rows][D] bf16 tile (row r of the tile
-// = global row min(r0 + r, rmax), at least 0) straight into LDS at `lds` in the
+// = global row min(r0 + r, rmax), at least rmin) straight into LDS at `lds` in the
 // swizzled layout, spread over NWV waves: wave-wide load i of wave w fills
 // tile bytes [(i * NWV + w) * 1024, +1024), lane l the 16 bytes at +16 l,
 // so it fetches the chunk that belongs there.  The caller waits for them
 // (s_waitcnt vmcnt) before the barrier that publishes the tile.
 template <int D, int NWV, int ROWS>
 __device__ __forceinline__ void dma_rows(const char *g, int64_t st_bytes, int r0, int rmax, uint32_t lds,
-                                         int wave, int lane) {
+                                         int wave, int lane, int rmin = 0) {
     constexpr int ROWB = 2 * D, RPW = 1024 / ROWB, LPR = ROWB / 16;
     constexpr int NI = ROWS * ROWB / (NWV * 1024);
     static_assert(NI >= 1 && ROWS * ROWB % (NWV * 1024) == 0, "the tile splits into wave-wide loads");
@@ -90,7 +100,7 @@ __device__ __forceinline__ void dma_rows(const char *g, int64_t st_bytes, int r0
     for (int i = 0; i < NI; ++i) {
         const int r = (i * NWV + wave) * RPW + lane / LPR;
         const int ch = (lane % LPR) ^ swz<D>(r);
-        const int gr = max(min(r0 + r, rmax), 0);
+        const int gr = max(min(r0 + r, rmax), rmin);
         dma16(g + (int64_t)gr * st_bytes + 16 * ch, lds + (i * NWV + wave) * 1024);
     }
 }
@@ -107,12 +117,15 @@ __device__ __forceinline__ void dma_rows(const char *g, int64_t st_bytes, int r0
 // WIN (sliding window with sinks): the tiles between the sinks and the first
 // row's window are never loaded, as in the forward; the first key of each
 // token's window goes to the dK/dV launch beside its key end.
-template <int D, bool WIN, bool BF16>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void bwd_dq_kernel(const BwdArgs a) {
+// WIN = 2: packed sequences; the rows' items come from a table, the key tiles are
+// counted from the first key of the first row's sequence, as in the forward.
+template <int D, int WIN, bool BF16>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void bwd_dq_kernel(const BwdArgs a, const RowPlan<WIN> rp) {
     constexpr int ROWB = 2 * D, KK = D / 16, MD = D / 32;
     constexpr int TILEB = 64 * ROWB;
     __shared__ __attribute__((aligned(1024))) char smem[2 * 2 * TILEB];   // [stage][K, V]
-    const int nqt = (a.L + 127) / 128;
+    int nqt = (a.L + 127) / 128;
+    if constexpr (WIN == 2) nqt = rp.n;
     const int wid = blockIdx.x;
     // query tiles heaviest first over all (stream, head) pairs, so the
     // dispatch order is longest-first across the whole launch and the last
@@ -128,23 +141,36 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int g = h / a.G;
     const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int q0 = qt * 128;
+    int q0 = qt * 128, rows = a.L;   // the item's first row, and the end of its rows
+    if constexpr (WIN == 2) {
+        rows = a.rows;
+        if (rp.table) {
+            const uint32_t e = (uint32_t)ld_uniform((const int32_t *)rp.item, wid / (a.B * a.Hq));
+            q0 = (int)(e & 0xFFFFFFu);
+            rows = q0 + (int)(e >> 24) + 1;
+        }
+    }
     const int row = q0 + 32 * wave + l32;
-    const int rc = min(row, a.L - 1);
+    const int rc = min(row, rows - 1);
     const int32_t *offs = a.offsets + (int64_t)b * (a.nb + 1);
     const int32_t *text = a.text_starts ? a.text_starts + (int64_t)b * a.nb : nullptr;
     const BlockWindow win = block_window(offs, text, a.nb, q0, lane);
-    const int k_hi = token_key_end(win, min(q0 + 127, a.L - 1), lane);
+    const int k_hi = token_key_end(win, min(q0 + 127, rows - 1), lane);
     const int kfull = token_key_end(win, q0, lane);
-    const int my_kend = lane_key_end(win, min(q0 + 32 * wave, a.L - 1), rc, lane);
-    int my_klo = 0, nst = 0, gap = 0;
-    if constexpr (WIN) {
+    const int my_kend = lane_key_end(win, min(q0 + 32 * wave, rows - 1), rc, lane);
+    int my_klo = 0, nst = 0, gap = 0, base = 0;   // (base: packed, the first row's first key)
+    if constexpr (WIN == 2) {
+        const BlockWindow swin = block_window(a.seqs, nullptr, a.nseqs, q0, lane);
+        base = __builtin_amdgcn_readfirstlane(token_anchor(swin, q0, lane));
+        my_klo = lane_anchor(swin, min(q0 + 32 * wave, rows - 1), rc, lane);
+    } else if constexpr (WIN) {
         const int first = max(token_anchor(win, q0, lane) - a.window, 0) / 64;
         my_klo = lane_anchor(win, min(q0 + 32 * wave, a.L - 1), rc, lane) - a.window;
         nst = min((int)(((uint32_t)a.sinks + 63) / 64), first);
         gap = first - nst;
     }
-    auto tile_of = [&](int u) -> int { return WIN && u >= nst ? u + gap : u; };
+    // first key of live tile u
+    auto key_of = [&](int u) -> int { return WIN == 2 ? base + 64 * u : 64 * (WIN && u >= nst ? u + gap : u); };
     // this wave's first key end and last window start: masks where they cut
     int w_full = kfull, w_last = 0;
     if constexpr (WIN) {
@@ -186,7 +212,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
     // the row data of the dK/dV launch: lse2 and -D of this head's row and,
     // once per token, its key end
-    if (row < a.L && hf == 0) {
+    if (row < rows && hf == 0) {
         float *dl = a.dl + 2 * ((int64_t)b * a.Hq + h) * a.L + row;
         dl[0] = lse2;
         dl[a.L] = nD;
@@ -211,19 +237,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const bool wide = a.wide_strides != 0;
     auto issue_part = [&](int u, int i) {
         const uint32_t kl = lds_addr(smem) + (u & 1) * 2 * TILEB;
-        const int t = tile_of(u);
-        if ((t + 1) * 64 > k_hi || wide) {
-            if (i || t * 64 >= k_hi) return;
+        const int t0 = key_of(u);
+        if (t0 + 64 > k_hi || wide) {
+            if (i || t0 >= k_hi) return;
             // (the lane is hidden from the optimiser, so that what this rare
             // path derives from it is not hoisted and held in registers)
             int ln = lane;
             asm volatile("" : "+v"(ln));
-            dma_rows<D, 4, 64>(kg, kst, t * 64, k_hi - 1, kl, wave, ln);
-            dma_rows<D, 4, 64>(vg, vst, t * 64, k_hi - 1, kl + TILEB, wave, ln);
+            dma_rows<D, 4, 64>(kg, kst, t0, k_hi - 1, kl, wave, ln);
+            dma_rows<D, 4, 64>(vg, vst, t0, k_hi - 1, kl + TILEB, wave, ln);
         } else if (i < NI) {
-            dma16s(kg + (t * 64 + i * 4 * RPW) * kst, kofs, kl + i * 4096 + wave * 1024);
+            dma16s(kg + (t0 + i * 4 * RPW) * kst, kofs, kl + i * 4096 + wave * 1024);
         } else {
-            dma16s(vg + (t * 64 + (i - NI) * 4 * RPW) * vst, vofs, kl + TILEB + (i - NI) * 4096 + wave * 1024);
+            dma16s(vg + (t0 + (i - NI) * 4 * RPW) * vst, vofs, kl + TILEB + (i - NI) * 4096 + wave * 1024);
         }
     };
     uint32_t kbase = (uint32_t)(l32 * ROWB + 16 * (hf ^ swz<D>(l32)));
@@ -235,13 +261,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     for (int md = 0; md < MD; ++md)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[md][v] = 0.f;
-    const int ntile = (k_hi + 63) / 64 - gap;
+    const int ntile = WIN == 2 ? (k_hi - base + 63) / 64 : (k_hi + 63) / 64 - gap;
 #pragma unroll
     for (int i = 0; i < 2 * NI; ++i) issue_part(0, i);
     wait_vm_lgkm<0>();
     wg_barrier();
     for (int u = 0; u < ntile; ++u) {
-        const int t = tile_of(u);
+        const int t0 = key_of(u);
         const char *kt = smem + (u & 1) * 2 * TILEB, *vt = kt + TILEB;
         // One MFMA stream over the tile's two halves of 32 keys, every vector
         // instruction beside a matrix instruction that does not need it:
@@ -264,12 +290,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         // some row's end only (a real branch: the compiler would otherwise
         // turn this rare path into selects executed on every tile)
         auto mask = [&](int h) {
-            if ((t + 1) * 64 > w_full || (WIN && t * 64 < w_last && (t + 1) * 64 > a.sinks)) {
+            if (t0 + 64 > w_full || (WIN && t0 < w_last && (WIN == 2 || t0 + 64 > a.sinks))) {
                 asm volatile("" ::: "memory");
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
-                    const int key = t * 64 + h * 32 + 8 * (v >> 2) + 4 * hf + (v & 3);
-                    if ((key >= my_kend) | (WIN && ((key < my_klo) & (key >= a.sinks)))) S[h][v] = 0.f;
+                    const int key = t0 + h * 32 + 8 * (v >> 2) + 4 * hf + (v & 3);
+                    if ((key >= my_kend) | (WIN && ((key < my_klo) & (WIN == 2 || key >= a.sinks)))) S[h][v] = 0.f;
                 }
             }
         };
@@ -313,7 +339,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         wait_vm_lgkm<0>();   // tile t + 1 landed (and this tile's LDS reads are done)
         wg_barrier();
     }
-    if (row < a.L) {
+    if (row < rows) {
         const int64_t ofs = b * a.dq_sb + (int64_t)row * a.dq_st + h * a.dq_sh;
 #pragma unroll
         for (int md = 0; md < MD; ++md)
@@ -351,8 +377,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // the sequence end; a key tile with sinks is seen to the end, and its parts
 // are separate work-groups (BwdArgs), the heaviest, dispatched first.  It spills 7
 // scalars at D = 128 (none without) and 87 at 64 (26 without).
-template <int D, bool WIN, bool BF16>
-__global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
+// WIN = 2: packed sequences; the key tiles and the shares of their rows come from a
+// table, longest first.
+template <int D, int WIN, bool BF16>
+__global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a, const KeyPlan<WIN> rp) {
     constexpr int ROWB = 2 * D, KK = D / 16, MD = D / 32;
     constexpr int TILEK = 128 * ROWB, TILEC = 32 * ROWB;
     constexpr int CPR = ROWB / 16, RPP = 512 / CPR, NPK = 128 / RPP;
@@ -374,7 +402,21 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     // and work-groups past the last key tile exit at once.
     const int ngrp = a.B * a.Hkv;
     int kt, grpi, split = 0, nsplit = 1, slot = 0;
-    if constexpr (WIN) {
+    int kw0 = 0, keys = a.L;   // the tile's first key, and the end of its keys
+    if constexpr (WIN == 2) {
+        kt = wid / ngrp;
+        grpi = wid - kt * ngrp;
+        kw0 = 128 * kt;
+        keys = a.rows;
+        if (rp.table) {
+            const uint32_t e = (uint32_t)ld_uniform((const int32_t *)rp.item, kt), s = (uint32_t)ld_uniform((const int32_t *)rp.share, kt);
+            kw0 = (int)(e & 0xFFFFFFu);
+            keys = kw0 + (int)(e >> 24) + 1;
+            slot = (int)(s & 0xFFFFu);
+            split = (int)((s >> 16) & 255u);
+            nsplit = (int)(s >> 24);
+        }
+    } else if constexpr (WIN) {
         const int nsink = a.sink_tiles * a.sink_parts * ngrp, w = wid - (nsink + NUM_XCD - 1) / NUM_XCD * NUM_XCD;
         if (w < 0) {
             slot = wid / ngrp;
@@ -431,7 +473,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int grp = wave >> 2, sub = wave & 3;
-    const int kw0 = kt * 128;
+    if constexpr (WIN != 2) kw0 = kt * 128;
     const int key = kw0 + 32 * sub + l32;
     const float c2 = a.scale_log2;
     // the work-group's K and V (rows past the end repeat the last key)
@@ -442,7 +484,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
 #pragma unroll
         for (int p = 0; p < NPK; ++p) {
             const int r = lr + p * RPP;
-            const int kr = min(kw0 + r, a.L - 1);
+            const int kr = min(kw0 + r, keys - 1);
             *(u32x4 *)(smem + tile_off<D>(r, lc)) = *(const u32x4 *)(kg + (int64_t)kr * a.k_st);
             *(u32x4 *)(smem + TILEK + tile_off<D>(r, lc)) = *(const u32x4 *)(vg + (int64_t)kr * a.v_st);
         }
@@ -452,11 +494,12 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     // window: the first row at or past r0 whose entry of a non-decreasing array
     // is past k (L: none), by 64 probes at a time (two loads up to 4096 rows; the
     // four binary searches of a work-group took 50 of them one after the other)
+    const int end = WIN == 2 ? a.rows : a.L;   // of all rows
     auto first_past = [&](const int32_t *x, int r0, int k) -> int {
-        int lo = r0, hi = a.L;
+        int lo = r0, hi = end;
         while (lo < hi) {
             const int step = (hi - lo + 63) / 64, i = lo + (lane + 1) * step - 1;
-            const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < hi && x[min(i, a.L - 1)] <= k));
+            const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < hi && x[min(i, end - 1)] <= k));
             hi = min(hi, lo + (n + 1) * step - 1);
             lo = min(lo + n * step, hi);
         }
@@ -472,6 +515,9 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
         }
     }
     const int i0 = lo;
+    // rows before these are no rows (packed: another sequence's, which may hold
+    // anything)
+    const int low = WIN == 2 ? i0 : 0;
     // Chunks of 32 query rows counted from the sequence end, down to row i0,
     // with the query heads innermost: chunk it holds rows L - 32 (c + 1) ..
     // L - 32 c - 1 (c = it / G) of head it % G.  The work-groups of a KV head
@@ -480,7 +526,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     // none of these keys, so the masking zeroes their terms.
     // A split takes a contiguous share [first, total) of the chunks; group grp
     // takes chunks first + grp, first + grp + 2, ...
-    const int last = WIN && kw0 >= a.sinks ? first_past(kend_b + a.L, i0, min(kw0 + 127, a.L - 1)) : a.L;   // end of those rows
+    const int last = WIN && (WIN == 2 || kw0 >= a.sinks) ? first_past(kend_b + a.L, i0, min(kw0 + 127, keys - 1)) : a.L;   // end of those rows
     const int nch = (last - i0 + 31) / 32;
     const int first = (int)((int64_t)a.G * nch * split / nsplit);
     const int total = (int)((int64_t)a.G * nch * (split + 1) / nsplit);
@@ -490,7 +536,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     // is at or past im needs no element masks (key ends do not decrease).
     int im;
     {
-        const int kl = min(kw0 + 32 * sub + 31, a.L - 1);
+        const int kl = min(kw0 + 32 * sub + 31, keys - 1);
         int mlo = i0, mhi = a.L;
         if constexpr (WIN) mlo = mhi = first_past(kend_b, i0, kl);
         while (mlo < mhi) {
@@ -502,7 +548,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
     // ... and, with a window, before row il
     int il = a.L;
     if constexpr (WIN) {
-        const int k0 = max(kw0 + 32 * sub, a.sinks);
+        const int k0 = WIN == 2 ? kw0 + 32 * sub : max(kw0 + 32 * sub, a.sinks);
         if (k0 < kw0 + 32 * sub + 32) il = first_past(kend_b + a.L, i0, k0);
     }
     // Q and dO rows of one chunk go straight to LDS: wave-wide load i of wave
@@ -551,15 +597,15 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
         if (ni >= total) return;
         const uint32_t base = lds_addr(smem) + (uint32_t)(2 * TILEK + (grp * 2 + st) * 2 * TILEC);
         const uint32_t rl = lds_addr((const char *)&srow[grp][st][0]);
-        if (nr0 < 0 || wide) {
+        if (nr0 < low || wide) {
             if (i) return;
             // (the lane is hidden from the optimiser, so that what this rare
             // path derives from it is not hoisted and held in registers)
             int ln = lane;
             asm volatile("" : "+v"(ln));
-            dma_rows<D, 4, 32>(nq - nr0 * qst, qst, nr0, a.L - 1, base, sub, ln);
-            dma_rows<D, 4, 32>(nd - nr0 * dst, dst, nr0, a.L - 1, base + TILEC, sub, ln);
-            const int64_t r = max(nr0 + (ln & 31), 0);
+            dma_rows<D, 4, 32>(nq - nr0 * qst, qst, nr0, a.L - 1, base, sub, ln, low);
+            dma_rows<D, 4, 32>(nd - nr0 * dst, dst, nr0, a.L - 1, base + TILEC, sub, ln, low);
+            const int64_t r = max(nr0 + (ln & 31), low);
             if (sub == 0) dma4(nr + 4 * (r - nr0 + (ln >> 5) * (int64_t)a.L), rl);
             if (sub == 1) dma4(kend_b + r + (WIN ? (ln >> 5) * (int64_t)a.L : 0), rl + 256);
         } else if (i < NI) {
@@ -646,8 +692,8 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
                 if constexpr (WIN) kl = *(const i32x4 *)&srow[grp][st][96 + r];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const bool in = !WIN || (ky >= kl[e]) | (ky < a.sinks);
-                    S[4 * gq + e] = ((r0 + r + e >= 0) & (ky < ke[e]) & in) ? S[4 * gq + e] : 0.f;
+                    const bool in = !WIN || (ky >= kl[e]) | (WIN != 2 && ky < a.sinks);
+                    S[4 * gq + e] = ((r0 + r + e >= low) & (ky < ke[e]) & in) ? S[4 * gq + e] : 0.f;
                 }
             }
         }
@@ -727,7 +773,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a) {
             }
         return;
     }
-    if (grp == 0 && key < a.L) {
+    if (grp == 0 && key < keys) {
         const int64_t kofs = b * a.dk_sb + (int64_t)key * a.dk_st + kvh * a.dk_sh;
         const int64_t vofs = b * a.dv_sb + (int64_t)key * a.dv_st + kvh * a.dv_sh;
 #pragma unroll
@@ -822,15 +868,63 @@ __global__ __launch_bounds__(256) void bwd_sum_window_kernel(const BwdArgs a) {
     else store_grad<BF16>(a.dk, b * a.dk_sb + (int64_t)key * a.dk_st + kvh * a.dk_sh + d0, sum);
 }
 
+// The same for the parts of a packed launch (tile i of the plan: `parts` parts from
+// slot `slot` on).
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void bwd_sum_packed_kernel(const BwdArgs a, const PackBwdPlan rp) {
+    constexpr int PER = 128 * D / 4 / 256;   // blocks per (tile, group, dK or dV)
+    const int ngrp = a.Hkv;
+    const int blk = blockIdx.x % PER, wh = blockIdx.x / PER % 2, tg = blockIdx.x / (2 * PER);
+    const int i = tg / ngrp, kvh = tg - i * ngrp;
+    const uint32_t e = (uint32_t)ld_uniform((const int32_t *)rp.item, i), s = (uint32_t)ld_uniform((const int32_t *)rp.share, i);
+    const int kw0 = (int)(e & 0xFFFFFFu), keys = kw0 + (int)(e >> 24) + 1, s0 = (int)(s & 0xFFFFu), ns = (int)(s >> 24);
+    const int u = blk * 256 + threadIdx.x;   // ((sub * MD + md) * 4 + gq) * 64 + lane
+    const int64_t stride = (int64_t)ngrp * 2 * 128 * D;
+    const float *pp = a.part + (((int64_t)s0 * ngrp + kvh) * 2 + wh) * 128 * D + 4 * u;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < ns; p += 4) {
+        f32x4 x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = *(const f32x4 *)(pp + min(p + j, ns - 1) * stride);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (p + j < ns)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) sum[c] += x[j][c];
+    }
+    const int lane = u & 63, gq = (u >> 6) & 3, md = (u >> 8) % (D / 32), sub = (u >> 8) / (D / 32);
+    const int key = kw0 + 32 * sub + (lane & 31);
+    if (key >= keys) return;
+    const int d0 = 32 * md + 8 * gq + 4 * (lane >> 5);
+    if (!wh)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sum[c] *= a.scale;
+    if (wh) store_grad<BF16>(a.dv, (int64_t)key * a.dv_st + kvh * a.dv_sh + d0, sum);
+    else store_grad<BF16>(a.dk, (int64_t)key * a.dk_st + kvh * a.dk_sh + d0, sum);
+}
+
+template <int D, bool BF16>
+int launch_bwd_packed_t(const BwdArgs &a, const PackPlan &rows, const PackBwdPlan &keys, const PackBwdPlan &sums, hipStream_t st) {
+    hipLaunchKernelGGL((bwd_dq_kernel<D, 2, BF16>), dim3((unsigned)a.Hq * rows.n), dim3(256), 0, st, a, rows);
+    if (int e = (int)hipGetLastError()) return e;
+    hipLaunchKernelGGL((bwd_dkdv_kernel<D, 2, BF16>), dim3((unsigned)a.Hkv * keys.n), dim3(512), 0, st, a, keys);
+    if (int e = (int)hipGetLastError()) return e;
+    if (sums.n) {
+        constexpr int PER = 128 * D / 4 / 256;
+        hipLaunchKernelGGL((bwd_sum_packed_kernel<D, BF16>), dim3((unsigned)(sums.n * a.Hkv * 2 * PER)), dim3(256), 0, st, a, sums);
+    }
+    return (int)hipGetLastError();
+}
+
 template <int D, bool BF16>
 int launch_bwd_window_t(const BwdArgs &a, hipStream_t st) {
     const int64_t nqt = (a.L + 127) / 128, ngrp = (int64_t)a.B * a.Hkv;
-    hipLaunchKernelGGL((bwd_dq_kernel<D, true, BF16>), dim3((unsigned)(a.B * a.Hq * nqt)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((bwd_dq_kernel<D, 1, BF16>), dim3((unsigned)(a.B * a.Hq * nqt)), dim3(256), 0, st, a, NoPlan{});
     if (int e = (int)hipGetLastError()) return e;
     const int64_t sinks = (a.sink_tiles * a.sink_parts * ngrp + NUM_XCD - 1) / NUM_XCD * NUM_XCD;
     const int64_t rest = (nqt - a.sink_tiles) * a.tile_parts;
     const int64_t grid = sinks + (ngrp % NUM_XCD == 0 ? ngrp * ((rest + KB_DKDV - 1) / KB_DKDV) * KB_DKDV : ngrp * rest);
-    hipLaunchKernelGGL((bwd_dkdv_kernel<D, true, BF16>), dim3((unsigned)grid), dim3(512), 0, st, a);
+    hipLaunchKernelGGL((bwd_dkdv_kernel<D, 1, BF16>), dim3((unsigned)grid), dim3(512), 0, st, a, NoPlan{});
     if (int e = (int)hipGetLastError()) return e;
     const int64_t summed = (a.sink_parts > 1 ? a.sink_tiles : 0) + (a.tile_parts > 1 ? nqt - a.sink_tiles : 0);
     if (summed) {
@@ -844,22 +938,32 @@ template <int D>
 int launch_bwd_t(const BwdArgs &a, hipStream_t st) {
     if (a.has_window) return a.grads_bf16 ? launch_bwd_window_t<D, true>(a, st) : launch_bwd_window_t<D, false>(a, st);
     const int64_t nqt = (a.L + 127) / 128;
-    hipLaunchKernelGGL((bwd_dq_kernel<D, false, false>), dim3((unsigned)(a.B * a.Hq * nqt)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((bwd_dq_kernel<D, 0, false>), dim3((unsigned)(a.B * a.Hq * nqt)), dim3(256), 0, st, a, NoPlan{});
     if (int e = (int)hipGetLastError()) return e;
     const int64_t ngrp = (int64_t)a.B * a.Hkv;
     if (a.split_tiles) {
-        hipLaunchKernelGGL((bwd_dkdv_kernel<D, false, false>), dim3((unsigned)(ngrp * a.tile_start[nqt])), dim3(512), 0, st, a);
+        hipLaunchKernelGGL((bwd_dkdv_kernel<D, 0, false>), dim3((unsigned)(ngrp * a.tile_start[nqt])), dim3(512), 0, st, a, NoPlan{});
         if (int e = (int)hipGetLastError()) return e;
         constexpr int64_t PER = 128 * D / 4 / 256;
         hipLaunchKernelGGL(bwd_sum_kernel<D>, dim3((unsigned)(a.split_tiles * ngrp * 2 * PER)), dim3(256), 0, st, a);
         return (int)hipGetLastError();
     }
     const int64_t grid = ngrp % NUM_XCD == 0 ? ngrp * ((nqt + KB_DKDV - 1) / KB_DKDV) * KB_DKDV : ngrp * nqt;
-    hipLaunchKernelGGL((bwd_dkdv_kernel<D, false, false>), dim3((unsigned)grid), dim3(512), 0, st, a);
+    hipLaunchKernelGGL((bwd_dkdv_kernel<D, 0, false>), dim3((unsigned)grid), dim3(512), 0, st, a, NoPlan{});
     return (int)hipGetLastError();
 }
 
 }  // namespace
+
+int launch_packed_bwd(const BwdArgs &a, const PackPlan &rows, const PackBwdPlan &keys, const PackBwdPlan &sums, int head_dim,
+                      void *stream) {
+    hipStream_t st = (hipStream_t)stream;
+    if (head_dim == 128)
+        return a.grads_bf16 ? launch_bwd_packed_t<128, true>(a, rows, keys, sums, st) : launch_bwd_packed_t<128, false>(a, rows, keys, sums, st);
+    if (head_dim == 64)
+        return a.grads_bf16 ? launch_bwd_packed_t<64, true>(a, rows, keys, sums, st) : launch_bwd_packed_t<64, false>(a, rows, keys, sums, st);
+    return (int)hipErrorInvalidValue;
+}
 
 int launch_prefill_bwd(const BwdArgs &a, int head_dim, void *stream) {
     hipStream_t st = (hipStream_t)stream;

@@ -63,5 +63,14 @@ StepPlan plan_room(const StepPlan &uni, int batch, const int64_t *tiles);
 void ragged_work(AttnArgs &a, const RaggedPlan &r);
 // Work items and dividers of a launch; false when it would not fit.
 bool finish_work(AttnArgs &a);
+// Time of groups of n equal items each (sizes not increasing), longest first.
+struct ItemGroup { int size, n; };
+int dispatch_time(int cus, const ItemGroup *groups, int ngroups);
+// rounds of work-groups up to which their order is the launch's time
+constexpr int64_t FEW_ROUNDS = 6;
+// 256 query rows a work-group; whether a prefill's items may be dealt to 2^deal
+// classes per group.
+TileShape default_shape();
+bool deal_pays(int cus, const AttnArgs &a, int64_t groups, int deal, TileShape shape);
 
 }  // namespace ws

@@ -125,6 +125,25 @@ struct AttnArgs {
     // step over a cache held in 4 bits: its pool (else nullptr; kpool and vpool
     // are unused then)
     uint8_t *pool4;
+    // packed sequences (else nullptr): their first tokens and the end [nseqs + 1],
+    // on the device; a token sees no key before its sequence's first
+    const int32_t *seqs;
+    int32_t nseqs;
+};
+
+// Rows (or keys) that a work-group of a packed call takes: up to 256 neighbouring
+// tokens of one sequence, or of several that lie whole in them.  Beside the
+// arguments of a launch, longest first; without a table (too many for it) item i
+// is tokens [size i, size (i + 1)) whatever they belong to, from the last on.
+struct PackItem {
+    uint32_t first : 24, more : 8;   // first token, and how many follow it
+};
+constexpr int PACK_ITEMS = 512;      // of a table
+constexpr int32_t PACK_TOKENS = 1 << 24;
+struct PackPlan {
+    int32_t table;                   // items of the table, 0: none
+    int32_t n, size, tokens;         // items; without a table their size and the end of the last
+    PackItem item[PACK_ITEMS];
 };
 
 constexpr int LENS_IN_ARGS = 32;
@@ -251,8 +270,31 @@ struct BwdArgs {
     // sink_tiles * sink_parts + (kt - sink_tiles) * tile_parts) + part.
     int32_t has_window, sinks, window;
     int32_t sink_tiles, sink_parts, tile_parts;
-    int32_t grads_bf16;   // dq, dk, dv are bf16 (windowed only)
+    int32_t grads_bf16;   // dq, dk, dv are bf16 (windowed or packed only)
+    // packed sequences (else nullptr): as in AttnArgs; `rows` tokens are of some
+    // sequence.  kend as for a window.
+    const int32_t *seqs;
+    int32_t nseqs, rows;
 };
+
+// Key tiles of a packed dK/dV launch (at most 128 keys each) and the shares of
+// their rows: share `part` of `parts`, which writes partial sums at `slot` where
+// parts > 1.
+struct PackPart {
+    uint16_t slot;
+    uint8_t part, parts;
+};
+constexpr int PACK_PARTS = 320;      // of a table
+struct PackBwdPlan {
+    int32_t table;                   // shares of the table, 0: none (whole tiles of 128 keys, from the first)
+    int32_t n;                       // shares
+    PackItem item[PACK_PARTS];
+    PackPart share[PACK_PARTS];
+};
+
+// (kernel arguments hold 4 KiB)
+static_assert(sizeof(AttnArgs) + sizeof(PackPlan) <= 4000 && sizeof(BwdArgs) + sizeof(PackBwdPlan) <= 4000 &&
+              sizeof(BwdArgs) + sizeof(PackPlan) <= 4000 && sizeof(PackItem) == 4 && sizeof(PackPart) == 4, "launch arguments");
 
 // Launch shapes compiled into the library.
 struct TileShape {
@@ -268,6 +310,9 @@ struct TileShape {
 // Each returns 0 or a HIP error code (hipError_t as int).
 // (rag: per-stream splits, or nullptr for one split count)
 int launch_attention(const AttnArgs &a, const RaggedPlan *rag, int head_dim, TileShape shape, void *stream);
+// whole packed sequences
+__attribute__((visibility("hidden"))) int launch_packed(const AttnArgs &a, const PackPlan &p, int head_dim, TileShape shape,
+                                                        void *stream);
 int launch_combine(const AttnArgs &a, const RaggedPlan *rag, int head_dim, void *stream);
 int launch_append(const AppendArgs &a, void *stream);
 int launch_append4(const Cache4Args &a, void *stream);
@@ -276,6 +321,10 @@ int launch_read4(const Cache4Args &a, void *stream);
 int launch_few4(const AttnArgs &a, const Few4Plan &p, int head_dim, void *stream);
 // dQ (with the row data), then dK/dV and the sum of its parts; 0 or a HIP error code
 int launch_prefill_bwd(const BwdArgs &a, int head_dim, void *stream);
+// gradients of packed sequences: the rows' items, the keys', and the tiles whose
+// parts are summed (n of them, share: first slot and parts)
+__attribute__((visibility("hidden"))) int launch_packed_bwd(const BwdArgs &a, const PackPlan &rows, const PackBwdPlan &keys,
+                                                            const PackBwdPlan &sums, int head_dim, void *stream);
 // Compute units of the current HIP device (queried once per device, then
 // cached): 0 and *cus set, or a HIP error code (e.g. no device).
 int current_device_cus(int *cus);

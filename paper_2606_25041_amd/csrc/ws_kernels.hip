@@ -131,8 +131,8 @@ enum Kind { PREFILL_CONTIGUOUS, PREFILL_PAGED, STEP, STEP_SPLIT, STEP_RAGGED, ST
 constexpr bool is_ragged(int kind) { return kind == STEP_RAGGED || kind == STEP_CACHE4_RAGGED; }
 constexpr bool is_cache4(int kind) { return kind == STEP_CACHE4 || kind == STEP_CACHE4_RAGGED; }
 struct NoPlan {};
-template <bool RAGGED>
-using Plan = std::conditional_t<RAGGED, RaggedPlan, NoPlan>;
+template <bool RAGGED, int WIN = 0>
+using Plan = std::conditional_t<WIN == 2, PackPlan, std::conditional_t<RAGGED, RaggedPlan, NoPlan>>;
 
 //
 // KG = 2 (prefill): the work-group takes 128 query rows, and its two halves of
@@ -154,12 +154,19 @@ using Plan = std::conditional_t<RAGGED, RaggedPlan, NoPlan>;
 // are f16 values under a power of two per row, not a second bf16
 // rounding (output off by 2.3e-3 of its norm instead of 2.9e-3; the last
 // rounding alone makes 1.7e-3).
-template <int D, int NW, int NB, int KIND, bool F32, int KG, bool WIN = false>
-__global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const Plan<is_ragged(KIND)> rp) {
+// WIN = 2: packed sequences.  The same with klo(i) the first token of i's sequence
+// and no sinks.  An item's rows come from a table (PackPlan), so that one of a
+// sequence of more than a tile holds rows of that sequence alone; its key tiles are
+// counted from its first row's klo, so that it loads no key of another sequence
+// and masks none.  Only the rows of short sequences that share an item have
+// different klo; a wave skips the tiles before its first row's.
+template <int D, int NW, int NB, int KIND, bool F32, int KG, int WIN = 0>
+__global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const Plan<is_ragged(KIND), WIN> rp) {
     constexpr bool C4 = is_cache4(KIND);
     constexpr bool step = KIND == STEP || KIND == STEP_SPLIT || KIND == STEP_RAGGED || C4;
     constexpr bool RAGGED = is_ragged(KIND);
     static_assert(!WIN || (KIND != STEP_SPLIT && !C4), "windows: STEP and STEP_RAGGED");
+    static_assert(WIN != 2 || KIND == PREFILL_CONTIGUOUS, "packed sequences: contiguous keys");
     constexpr bool P3 = (WIN || C4) && F32;
     constexpr bool HALF = (WIN || C4) && !F32;
     constexpr int NT = NW * 64;
@@ -259,7 +266,16 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     auto row_token = [&](int p) -> int { return step ? (int)fastdiv((uint32_t)p, fd_gq) : p; };
     auto row_head = [&](int p, int t) -> int { return step ? kvh * (int)G + (p - t * (int)G) : hq; };
     const int qt = step ? (int)qi : (int)(nqt - 1 - qi);  // prefill: heaviest tiles first
-    const int q0 = qt * QT;
+    int q0 = qt * QT;
+    if constexpr (WIN == 2) {   // (nrows: the end of this item's rows)
+        if (rp.table) {
+            const uint32_t e = (uint32_t)ld_uniform((const int32_t *)rp.item, (int)qi);
+            q0 = (int)(e & 0xFFFFFFu);
+            nrows = (uint32_t)q0 + (e >> 24) + 1;
+        } else {
+            nrows = (uint32_t)min(q0 + QT, rp.tokens);
+        }
+    }
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
@@ -342,7 +358,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         kfull = n_new + min(nl, max(ts, (int)fastdiv((uint32_t)q0, fd_gq) + 1));
     } else {
         n_pool = KIND == PREFILL_PAGED ? a.Lq : 0;
-        const int q_last = min(q0 + QT, a.Lq) - 1;
+        const int q_last = min(q0 + QT, WIN == 2 ? (int)nrows : a.Lq) - 1;
         win = block_window(offs, text, a.nb, q0, lane);
         k_hi = token_key_end(win, q_last, lane);
         kfull = token_key_end(win, q0, lane);
@@ -350,7 +366,11 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     // window: the first row's klo, at least 0 (it is not past the row's own key),
     // the live tiles and their mapping
     int lo_min = 0, nst = 0, gap = 0;
-    if constexpr (WIN) {
+    BlockWindow swin;   // (packed: the sequences around the rows)
+    if constexpr (WIN == 2) {
+        swin = block_window(a.seqs, nullptr, a.nseqs, q0, lane);
+        lo_min = __builtin_amdgcn_readfirstlane(token_anchor(swin, q0, lane));
+    } else if constexpr (WIN) {
         if (step) {
             const int t0 = (int)fastdiv((uint32_t)q0, fd_gq);
             lo_min = n_pool + (t0 >= ts ? t0 : 0);
@@ -363,11 +383,13 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         gap = first - nst;
     }
     auto tile_of = [&](int u) -> int { return WIN && u >= nst ? u + gap : u; };
+    // first key of live tile u
+    auto key_of = [&](int u) -> int { return WIN == 2 ? lo_min + u * KT : tile_of(u) * KT; };
     // whether a step's tile holds keys between the sinks and the window: no row
     // sees them, so their slots may hold anything (a prefill's keys are all
     // seen by their own row)
     auto holed = [&](int kt) -> bool { return WIN && step && kt < lo_min && kt + KT > a.sinks; };
-    const int ntile = (k_hi + KT - 1) / KT - gap;
+    const int ntile = WIN == 2 ? (k_hi - lo_min + KT - 1) / KT : (k_hi + KT - 1) / KT - gap;
     // (split * ntile < 2^31: ntile < 2^25 and split < MAX_SPLITS = 32)
     const int t_begin = (int)fastdiv(split * (uint32_t)ntile, fd_split);
     const int t_end = (int)fastdiv((split + 1) * (uint32_t)ntile, fd_split);
@@ -404,6 +426,8 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         else kend[n] = lane_key_end(win, min(q0 + rblk * 32 * NB + 32 * n, (int)nrows - 1), tok[n], lane);
         klo[n] = 0;
         if constexpr (WIN && step) klo[n] = n_pool + (tok[n] >= ts ? tok[n] : 0) - a.window;
+        else if constexpr (WIN == 2)
+            klo[n] = lane_anchor(swin, min(q0 + rblk * 32 * NB + 32 * n, (int)nrows - 1), tok[n], lane);
         else if constexpr (WIN)
             klo[n] = lane_anchor(win, min(q0 + rblk * 32 * NB + 32 * n, (int)nrows - 1), tok[n], lane) - a.window;
     }
@@ -415,8 +439,12 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     // row, as live tiles u: [cut_lo, cut_hi), where the sinks end or a window starts,
     // and those from cut_end on.  (Skipping the tiles that none of a wave's rows see
     // too: 87 us there, but 2 % more where an item runs many tiles.)
-    int cut_lo = 0, cut_hi = 0, cut_end = 0;
-    if constexpr (WIN) {
+    int cut_lo = 0, cut_hi = 0, cut_end = 0, skip = 0;   // (skip: packed, tiles before the first)
+    if constexpr (WIN == 2) {
+        skip = (__builtin_amdgcn_readlane(klo[0], 0) - lo_min) / KT;
+        cut_hi = (__builtin_amdgcn_readlane(klo[0], 31) - lo_min + KT - 1) / KT;
+        cut_end = (__builtin_amdgcn_readlane(kend[0], 0) - lo_min) / KT;
+    } else if constexpr (WIN) {
         cut_lo = a.sinks / KT;
         cut_hi = (max(__builtin_amdgcn_readlane(klo[0], 31), 0) + KT - 1) / KT - gap;
         cut_end = __builtin_amdgcn_readlane(kend[0], 0) / KT - gap;
@@ -458,7 +486,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         bool straddle;
     };
     auto plan_tile = [&](int u, int s, int page) -> TileLoad {
-        const int kt = tile_of(u) * KT;
+        const int kt = key_of(u);
         TileLoad t;
         t.kd = lds_addr(smem) + s * TILEB + lwave * 1024;
         t.vd = t.kd + VRING;
@@ -492,7 +520,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     };
     // rows past the end repeat the last key (their scores are masked)
     auto issue_straddle = [&](int u, int s, int page) {
-        const int kt = tile_of(u) * KT;
+        const int kt = key_of(u);
         const uint32_t kd = lds_addr(smem) + s * TILEB + lwave * 1024;
         const uint32_t vd = kd + VRING;
         const int64_t tb = ((int64_t)page * a.Hkv + kvh) * TILEB;
@@ -690,7 +718,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     };
     // element masks only where the tile is not visible to every row
     auto mask = [&](int t, Tile &sc) {
-        const int kt = tile_of(t) * KT;
+        const int kt = key_of(t);
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -700,7 +728,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
                     const int key = kt + mb * 32 + (v >> 2) * 8 + 4 * hf + (v & 3);
                     const int end = C4 && kt < n_new ? n_pool : kend[n];
                     // (| and &: no branch per element)
-                    if ((key >= end) | (WIN && ((key < klo[n]) & (key >= a.sinks)))) sc[n][mb][v] = -INFINITY;
+                    if ((key >= end) | (WIN && ((key < klo[n]) & (WIN == 2 || key >= a.sinks)))) sc[n][mb][v] = -INFINITY;
                 }
     };
     // Running max (log2 domain) from a tile's in-lane max, with lazy rescale:
@@ -948,14 +976,14 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
             if (busy) {
                 // S^T of tile j first: its accumulators are complete long
                 // before the softmax reads them after the barrier
-                if (j < t_end) qk(stage_off(j), S);
-                if (j > t_begin) pv(stage_off(j - 1), pf);
+                if (j < t_end && (WIN != 2 || j >= skip)) qk(stage_off(j), S);
+                if (j > t_begin && (WIN != 2 || j > skip)) pv(stage_off(j - 1), pf);
             }
             wg_barrier();
             // the leading waves issue the loads of tile j+3 here, ahead of
             // their softmax, rather than ahead of their MFMA block
             if (lead && j + 3 < t_end) issue_tile(j + 3, (j + 3 - t_begin) % NSTAGE, pg_next);
-            if (busy && j < t_end) softmax(j, S, pf);
+            if (busy && j < t_end && (WIN != 2 || j >= skip)) softmax(j, S, pf);
             // (read here, under the wait below: a scalar read left in flight
             // across the MFMA block would force full LDS drains there)
             if (lead && j + 4 < t_end) pg_next = page_glb(j + 4);
@@ -997,13 +1025,13 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
                 asm volatile("" : "+v"(kbase), "+v"(vbase[0]), "+v"(vbase[1]), "+v"(lofs_p), "+v"(lofs_k), "+v"(lofs_v));
                 const int t = t_begin + 2 * j + kg;
                 if (busy) {
-                    if (t < t_end) qk(stage_off(t), S);
-                    if (j > 0 && t - 2 < t_end) pv(stage_off(t - 2), pf);
+                    if (t < t_end && (WIN != 2 || t >= skip)) qk(stage_off(t), S);
+                    if (j > 0 && t - 2 < t_end && (WIN != 2 || t - 2 >= skip)) pv(stage_off(t - 2), pf);
                 }
                 wait_vm_lgkm<0>();   // the tile issued in the last softmax phase landed
                 wg_barrier();
                 if (t + 3 < t_end) issue_tile(t + 3, (t + 3 - t_begin) % NSTAGE, pg_next);
-                if (busy && t < t_end) softmax(t, S, pf);
+                if (busy && t < t_end && (WIN != 2 || t >= skip)) softmax(t, S, pf);
                 if (t + 5 < t_end) pg_next = page_glb(t + 5);
                 wait_vm_lgkm<63>();
                 wg_barrier();
@@ -1429,8 +1457,8 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {
     }
 }
 
-template <int D, int KIND, int KG, bool WIN = false>
-int launch_attn_t(const AttnArgs &a, const Plan<is_ragged(KIND)> &rp, hipStream_t st) {
+template <int D, int KIND, int KG, int WIN = 0>
+int launch_attn_t(const AttnArgs &a, const Plan<is_ragged(KIND), WIN> &rp, hipStream_t st) {
     const dim3 grid(a.per_xcd * NUM_XCD), block(8 * 64);
     if (a.out_f32)
         hipLaunchKernelGGL((attn_kernel<D, 8, 1, KIND, true, KG, WIN>), grid, block, 0, st, a, rp);
@@ -1439,7 +1467,7 @@ int launch_attn_t(const AttnArgs &a, const Plan<is_ragged(KIND)> &rp, hipStream_
     return (int)hipGetLastError();
 }
 
-template <int D, int KIND, bool WIN = false>
+template <int D, int KIND, int WIN = 0>
 int launch_prefill_t(const AttnArgs &a, int key_groups, hipStream_t st) {
     return key_groups == 2 ? launch_attn_t<D, KIND, 2, WIN>(a, NoPlan{}, st)
                            : launch_attn_t<D, KIND, 1, WIN>(a, NoPlan{}, st);
@@ -1448,10 +1476,10 @@ int launch_prefill_t(const AttnArgs &a, int key_groups, hipStream_t st) {
 template <int D>
 int launch_attn_d(const AttnArgs &a, const RaggedPlan *rag, TileShape shape, hipStream_t st) {
     if (a.has_window)
-        return rag ? launch_attn_t<D, STEP_RAGGED, 1, true>(a, *rag, st)
-             : a.mode == MODE_STEP ? launch_attn_t<D, STEP, 1, true>(a, NoPlan{}, st)
-             : a.paged ? launch_prefill_t<D, PREFILL_PAGED, true>(a, shape.kg, st)
-                       : launch_prefill_t<D, PREFILL_CONTIGUOUS, true>(a, shape.kg, st);
+        return rag ? launch_attn_t<D, STEP_RAGGED, 1, 1>(a, *rag, st)
+             : a.mode == MODE_STEP ? launch_attn_t<D, STEP, 1, 1>(a, NoPlan{}, st)
+             : a.paged ? launch_prefill_t<D, PREFILL_PAGED, 1>(a, shape.kg, st)
+                       : launch_prefill_t<D, PREFILL_CONTIGUOUS, 1>(a, shape.kg, st);
     if (a.pool4)
         return rag ? launch_attn_t<D, STEP_CACHE4_RAGGED, 1>(a, *rag, st) : launch_attn_t<D, STEP_CACHE4, 1>(a, NoPlan{}, st);
     return rag ? launch_attn_t<D, STEP_RAGGED, 1>(a, *rag, st)
@@ -1510,6 +1538,16 @@ int launch_attention(const AttnArgs &a, const RaggedPlan *rag, int head_dim, Til
     if (shape.nw != 8 || shape.nb != 1) return (int)hipErrorInvalidValue;
     if (head_dim == 128) return launch_attn_d<128>(a, rag, shape, st);
     if (head_dim == 64) return launch_attn_d<64>(a, rag, shape, st);
+    return (int)hipErrorInvalidValue;
+}
+
+int launch_packed(const AttnArgs &a, const PackPlan &p, int head_dim, TileShape shape, void *stream) {
+    hipStream_t st = (hipStream_t)stream;
+    if (shape.nw != 8 || shape.nb != 1) return (int)hipErrorInvalidValue;
+    if (head_dim == 128)
+        return shape.kg == 2 ? launch_attn_t<128, PREFILL_CONTIGUOUS, 2, 2>(a, p, st) : launch_attn_t<128, PREFILL_CONTIGUOUS, 1, 2>(a, p, st);
+    if (head_dim == 64)
+        return shape.kg == 2 ? launch_attn_t<64, PREFILL_CONTIGUOUS, 2, 2>(a, p, st) : launch_attn_t<64, PREFILL_CONTIGUOUS, 1, 2>(a, p, st);
     return (int)hipErrorInvalidValue;
 }
 

@@ -16,8 +16,8 @@ import math
 
 import torch
 
-from . import (WS_DTYPE_BF16, WS_DTYPE_F32, Tensor4, _check, _check_pair, _check_workspace, _here, _int32_pair, _native, _ptr,
-               _shape, _stream, _t4, library)
+from . import (Tensor4, _check, _check_pair, _here, _int32_pair, _native, _ptr, _shape, _stream, _t4, library)
+from .packed import _seq_offsets, _t3, _workspace
 
 WS_STATE_RESET, WS_STATE_KEEP = 1, 2
 
@@ -74,28 +74,6 @@ def linear_workspace_bytes(num_seqs, total_tokens, num_q_heads, num_kv_heads, he
     return library().ws_linear_workspace_bytes(num_seqs, total_tokens, num_q_heads, num_kv_heads, head_dim)
 
 
-def _t3(t):
-    """Descriptor of a packed [T][H][d] tensor."""
-    if t.dim() != 3 or t.stride(2) != 1:
-        raise ValueError("packed tensors must be 3-d [T][H][d] with a contiguous last dim")
-    if t.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError(f"unsupported dtype {t.dtype}")
-    return Tensor4(t.data_ptr(), WS_DTYPE_BF16 if t.dtype == torch.bfloat16 else WS_DTYPE_F32, 0, t.stride(0), t.stride(1))
-
-
-def _seq_offsets(seq_offsets, device):
-    """(host, device) int32 sequence offsets and the number of sequences."""
-    if isinstance(seq_offsets, tuple):
-        host, dev = seq_offsets
-    else:
-        host = torch.as_tensor(seq_offsets, dtype=torch.int32).cpu().contiguous()
-        dev = host.to(device)
-    if host.dim() != 1 or len(host) < 1 or dev.shape != host.shape:
-        raise ValueError("seq_offsets must be [num_seqs + 1]")
-    _check_pair("seq_offsets", host, dev)
-    return host, dev, len(host) - 1
-
-
 def _check_decay(log_decay, hkv):
     _shape("log_decay", log_decay, (hkv,))
     if log_decay.dtype != torch.float32 or not log_decay.is_contiguous():
@@ -117,13 +95,6 @@ def _check_states(name, t, shape):
     _shape(name, t, shape)
     if t is not None and (t.dtype != torch.float32 or not t.is_contiguous()):
         raise ValueError(f"{name} must be contiguous f32")
-
-
-def _workspace(workspace, need, device):
-    _check_workspace(workspace)
-    if workspace is None:
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
-    return workspace, workspace.numel() * workspace.element_size()
 
 
 def linear_attn_prefill(q, k, v, log_decay, seq_offsets, scale=None, state=None, reset=False, commit=True, out=None,

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2606_25041_amd as ws
-from paper_2606_25041_amd import linear
+from paper_2606_25041_amd import linear, packed
 
 if torch.cuda.device_count() > 0:
     pytest.skip("uses fake device pointers; CPU-only module", allow_module_level=True)
@@ -147,8 +147,8 @@ def test_python_arguments():
     with pytest.raises(ValueError):
         linear._check_state(object(), 1)
     with pytest.raises(ValueError):
-        linear._t3(torch.zeros(2, 3, 4, 5, dtype=torch.bfloat16))
+        packed._t3(torch.zeros(2, 3, 4, 5, dtype=torch.bfloat16))
     with pytest.raises(ValueError):
-        linear._t3(torch.zeros(3, 4, 5, dtype=torch.float16))
+        packed._t3(torch.zeros(3, 4, 5, dtype=torch.float16))
     with pytest.raises(ValueError):
-        linear._seq_offsets(torch.zeros(2, 2), "cpu")
+        packed._seq_offsets(torch.zeros(2, 2), "cpu")
