@@ -117,16 +117,25 @@ LinearJob job_of(const ws_tensor4 &x, const ws_tensor4 &y, const ws_tensor4 &z, 
 }
 
 // Cells and work items of a pass whose jobs, heads and sequences are set;
-// false: too many.
-bool plan_pass(LinearArgs &a, int head_dim) {
+// false: too many.  Where even all query heads' work-groups run at once, each
+// row head is one of its own (that repeats the state's products, but nobody
+// waits for a CU).
+bool plan_pass(LinearArgs &a, bool backwards, int head_dim) {
     const int64_t rows = (int64_t)a.Hkv * a.njobs;
     a.cell_len = plan_cell_len(a.T, rows, head_dim);
     a.ncells = cells_of(a.T, a.cell_len);
-    const int64_t n = a.ncells * rows;
+    int64_t n = a.ncells * rows;
     if (n > (1 << 30)) return false;
+    a.head_rows = 1;
+    if (!backwards && n * a.sets <= resident(head_dim)) {
+        a.head_rows = a.sets;
+        n *= a.sets;
+        a.sets = 1;
+    }
     a.n_work = (int32_t)n;
     a.per_xcd = (a.n_work + NUM_XCD - 1) / NUM_XCD;
-    a.fd_hkv = fastdiv_make((uint32_t)a.Hkv);
+    a.fd_heads = fastdiv_make((uint32_t)(a.Hkv * a.head_rows));
+    a.fd_rows = fastdiv_make((uint32_t)a.head_rows);
     return true;
 }
 
@@ -186,11 +195,11 @@ int ws_linear_attn_prefill(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const float
     a.out_f32 = out.dtype == WS_DTYPE_F32;
     a.slots = state ? state->slots_dev : nullptr;
     a.state_in = reads ? state->pool : nullptr;
-    if (tokens > 0 && !plan_pass(a, head_dim)) return fail(WS_ERR_SHAPE, "too many work items");
+    if (tokens > 0 && !plan_pass(a, false, head_dim)) return fail(WS_ERR_SHAPE, "too many work items");
     const bool edges = tokens > 0 && crosses(off_host, num_seqs, a.cell_len);
-    // the state of a sequence's first cell may be read after the last cell's
-    // work-group has written it: it goes through the workspace
-    const bool late = writes && reads && edges;
+    // a sequence's state may be read (by its first cell, by the work-groups of other
+    // query heads) after the work-group that writes it: it goes through the workspace
+    const bool late = writes && reads && tokens > 0 && (edges || a.head_rows > 1);
     a.cells = (float *)workspace;
     float *after = (float *)((char *)workspace + cells_bytes(tokens, num_kv_heads, head_dim));
     a.state_out = !writes ? nullptr : late ? after : state->pool;
@@ -265,7 +274,7 @@ int ws_linear_attn_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tens
     r.state_out = dstate0;
     r.out_scale = scale;
     if (tokens > 0) {
-        if (!plan_pass(a, head_dim) || !plan_pass(r, head_dim)) return fail(WS_ERR_SHAPE, "too many work items");
+        if (!plan_pass(a, false, head_dim) || !plan_pass(r, true, head_dim)) return fail(WS_ERR_SHAPE, "too many work items");
         for (LinearArgs *p : {&a, &r}) {
             if (crosses(off_host, num_seqs, p->cell_len))
                 if (int e = launch_linear_cells(*p, p == &r, head_dim, stream)) return fail(WS_ERR_HIP, "launch failed (hip error %d)", e);

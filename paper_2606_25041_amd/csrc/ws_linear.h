@@ -45,7 +45,8 @@ struct LinearArgs {
     float *cells;
     float scale;
     int32_t out_f32;
-    FastDiv fd_hkv;             // divider by Hkv
+    int32_t head_rows;          // query heads that are work-groups of their own, per KV head (1: none are)
+    FastDiv fd_heads, fd_rows;  // dividers by Hkv * head_rows and by head_rows
     int32_t n_work, per_xcd;
 };
 

@@ -20,6 +20,8 @@
 namespace ws {
 namespace {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
 constexpr int C = LIN_CHUNK;
 enum { ONE = 0, KEYS = 1, ROWS = 2 };
 constexpr float LOG2E = 1.4426950408889634f;
@@ -27,17 +29,8 @@ constexpr float LOG2E = 1.4426950408889634f;
 // A state times g^n: S + (g^n - 1) S where g^n is at least 1/2, so that no rounding
 // of g^n itself adds up over many chunks or tokens (a head that holds for 8192
 // tokens would be off by 2^-24 x 8192); g^n S below, where g^n - 1 would lose its
-// last bits.
-struct Decay {
-    float by;
-    bool slow;
-};
-__device__ __forceinline__ Decay decay_of(float x) {   // g^n = e^x (wave-uniform)
-    const bool slow = x >= -0.6931472f;
-    const float by = slow ? expm1f(x) : expf(x);
-    return Decay{__uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(by))),
-                 __builtin_amdgcn_readfirstlane((int)slow) != 0};
-}
+// last bits.  x: the logarithm of g^n (wave-uniform).
+__device__ __forceinline__ bool is_slow(float x) { return __builtin_amdgcn_readfirstlane((int)(x >= -0.6931472f)) != 0; }
 
 // (log_decay of -inf: g = 0 and g^0 = 1, without inf * 0)
 __device__ __forceinline__ float log_decay_of(const float *p, int kvh) {
@@ -45,25 +38,17 @@ __device__ __forceinline__ float log_decay_of(const float *p, int kvh) {
     return ld < -1e30f ? -1e30f : ld;
 }
 
-// Eight values as an operand of NP bf16 parts, whose sum holds 8, 16 or f32's 24
-// bits of each.
+// Two values as NP bf16 parts each (a word of every part), whose sums hold 8, 16 or
+// f32's 24 bits.
 template <int NP>
-__device__ __forceinline__ void parts_of(const float (&v)[8], bf16x8 (&out)[NP]) {
-    float x[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = v[e];
+__device__ __forceinline__ void parts_of(float x, float y, uint32_t (&out)[NP]) {
 #pragma unroll
     for (int c = 0; c < NP; ++c) {
-        u32x4 r;
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            r[h] = pack_bf16x2(x[2 * h], x[2 * h + 1]);
-            if (c + 1 < NP) {
-                x[2 * h] -= __uint_as_float(r[h] << 16);
-                x[2 * h + 1] -= __uint_as_float(r[h] & 0xFFFF0000u);
-            }
+        out[c] = pack_bf16x2(x, y);
+        if (c + 1 < NP) {
+            x -= __uint_as_float(out[c] << 16);
+            y -= __uint_as_float(out[c] & 0xFFFF0000u);
         }
-        out[c] = __builtin_bit_cast(bf16x8, r);
     }
 }
 
@@ -180,7 +165,8 @@ __global__ __launch_bounds__(2 * D, 2) void linear_kernel(const LinearArgs a) {
     const int lane = threadIdx.x & 63, hf = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-    // ---- work item: (cell, KV head, job) ---------------------------------------
+    // ---- work item: (cell, head, job), the heads being KV heads or, with
+    // head_rows of them to a KV head, query heads ---------------------------------
     const uint32_t w = (blockIdx.x % NUM_XCD) * (uint32_t)a.per_xcd + blockIdx.x / NUM_XCD;
     if (w >= (uint32_t)a.n_work) return;
     uint32_t item = w;
@@ -189,8 +175,9 @@ __global__ __launch_bounds__(2 * D, 2) void linear_kernel(const LinearArgs a) {
         jn = item & 1;
         item >>= 1;
     }
-    const uint32_t cell_u = fastdiv(item, a.fd_hkv);
-    const int kvh = (int)(item - cell_u * (uint32_t)a.Hkv);
+    const uint32_t cell_u = fastdiv(item, a.fd_heads);
+    const int head_no = (int)(item - cell_u * (uint32_t)(a.Hkv * a.head_rows)), kvh = (int)fastdiv((uint32_t)head_no, a.fd_rows);
+    const bool leads = jn == 0 && head_no == kvh * a.head_rows;   // this work-group writes the sequences' states
     // (cells from the end on in a pass backwards)
     const int cell = REV ? a.ncells - 1 - (int)cell_u : (int)cell_u;
     const LinearJob &job = a.job[jn];
@@ -227,7 +214,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_kernel(const LinearArgs a) {
     const uint32_t ofs_x = lrow * xs + lch, ofs_y = lrow * ys + lch, ofs_z = lrow * zs + lch;
     const char *xb = (const char *)job.x, *yb = (const char *)job.y, *zb = (const char *)job.z;
     // head of the rows and of the keys in a step
-    auto row_head = [&](const Step &r) -> int64_t { return SETS == ROWS ? (int64_t)kvh * a.sets + r.set : kvh; };
+    auto row_head = [&](const Step &r) -> int64_t { return SETS == ROWS ? (int64_t)kvh * a.sets + r.set : head_no; };
     auto key_head = [&](const Step &r) -> int64_t { return SETS == KEYS ? (int64_t)kvh * a.sets + r.set : kvh; };
     auto loads_keys = [&](const Step &r) -> bool { return SETS != ROWS || r.set == 0; };
     // A chunk of fewer tokens stands at the end of its tiles (backwards: at their
@@ -276,7 +263,10 @@ __global__ __launch_bounds__(2 * D, 2) void linear_kernel(const LinearArgs a) {
     }
 #pragma unroll
     for (int v = 0; v < 16; ++v) kw[v] = fast_exp2((REV ? key(v) + 1 : C - 1 - key(v)) * l2);
-    const Decay whole = decay_of(C * ld);
+    // (in scalar registers)
+    const bool head_slow = is_slow(C * ld);
+    auto uniform = [](float x) -> float { return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(x))); };
+    const float whole = uniform(head_slow ? expm1f(C * ld) : expf(C * ld));
     const float head = fast_exp2((REV ? C - 1 - l32 : l32 + 1) * l2) * a.scale;
 
     f32x16 S[MT];
@@ -372,12 +362,10 @@ __global__ __launch_bounds__(2 * D, 2) void linear_kernel(const LinearArgs a) {
     for (int m = 1; m < MT; ++m) zbase = wave == m ? cbase[m] : zbase;
 
     f32x16 o;
-    auto compute = [&](const Step &r, int xstage, int kstage) {
+    auto compute = [&](const Step &r, int xstage, int kstage, auto slow) {
         const char *tx = smem + XRING + xstage * TILEB, *ty = smem + kstage * 2 * TILEB, *tz = ty + TILEB;
         const bool part = r.n < C;
         if (r.first) read_state(r);
-        // (steps are fenced, so that the reads stay a step or two ahead of their
-        // MFMAs and the registers hold no more than that)
         bf16x8 zf[2] = {col_of(tz, 0, zbase), col_of(tz, 1, zbase)};
         if (part) {
 #pragma unroll
@@ -389,113 +377,137 @@ __global__ __launch_bounds__(2 * D, 2) void linear_kernel(const LinearArgs a) {
                 zf[s] = __builtin_bit_cast(bf16x8, zr);
             }
         }
-        if constexpr (OUT) {
-            const f32x16 zero = {};
-            f32x16 p = zero;
-            constexpr int RA = 3;   // fragments in flight
-            bf16x8 xf[RA], yf[RA];
-#pragma unroll
-            for (int s = 0; s + 1 < RA; ++s) xf[s] = row_frag(tx, s), yf[s] = row_frag(ty, s);
-            // P^T (and, once a chunk, S^T X^T)
-            auto products = [&](auto inter) {
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    const int nx = s + RA - 1;
-                    if (nx < KS) xf[nx % RA] = row_frag(tx, nx), yf[nx % RA] = row_frag(ty, nx);
-                    p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yf[s % RA], xf[s % RA], s ? p : zero, 0, 0, 0);
-                    if constexpr (decltype(inter)::value) {
-                        float x[8];
-                        bf16x8 sf[PS];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = S[s / 2][8 * (s & 1) + e];
-                        parts_of<PS>(x, sf);
-#pragma unroll
-                        for (int c = 0; c < PS; ++c)
-                            o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(sf[c], xf[s % RA], s + c ? o : zero, 0, 0, 0);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            };
-            if (SETS != KEYS || r.set == 0) {
-                products(std::true_type{});
-                float hd = head;
-                if (part) {
-                    int n = r.n;
-                    asm volatile("" : "+s"(n));
-                    hd = fast_exp2(max(REV ? n - 1 - l32 : l32 + 1 - (C - n), 0) * l2) * a.scale;
-                }
-#pragma unroll
-                for (int v = 0; v < 16; ++v) o[v] *= hd;
-            } else {
-                products(std::false_type{});
-            }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                float x[8];
-                bf16x8 pf[PP];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int v = 8 * s + e;
-                    x[e] = p[v] * pw[v];
-                }
-                parts_of<PP>(x, pf);
-#pragma unroll
-                for (int c = 0; c < PP; ++c) o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(zf[s], pf[c], o, 0, 0, 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
+        const bool adv = SETS != ROWS || !OUT || r.set == a.sets - 1;   // (of several query heads the last brings the state on)
+        float hd = head, by = whole;
+        if (part) {
+            int n = r.n;
+            asm volatile("" : "+s"(n));   // (a real branch)
+            if constexpr (OUT) hd = fast_exp2(max(REV ? n - 1 - l32 : l32 + 1 - (C - n), 0) * l2) * a.scale;
+            by = uniform(slow ? expm1f(n * ld) : expf(n * ld));
         }
-        // the state behind the chunk
-        auto advance = [&](const Decay &dec) {
-            if (SETS != KEYS || r.set == 0) {
-                if (dec.slow) {
+        // One stream of MFMAs in which the vector work stands beside those that do
+        // not need it: P^T = Y X^T beside the weights of z's first half; S^T X^T
+        // beside P . W; Z^T (P . W) beside the state's decay; the state's products
+        // beside the weights of z's second half.  The steps are fenced, so that
+        // this order stays and no more operands are read ahead than these.
+        // (Of several row heads, whose state's part is not always there, it stands
+        // behind the others' whole.)
+        constexpr bool ADV = OUT && SETS == ONE;
+        {
+            u32x4 zw[2][3];   // parts of Z . w, of either half of the keys
+            auto weigh = [&](int s, int h) {
+                const uint32_t zr = __builtin_bit_cast(u32x4, zf[s])[h];
+                uint32_t w[3];
+                parts_of<3>(__uint_as_float(zr << 16) * kw[8 * s + 2 * h], __uint_as_float(zr & 0xFFFF0000u) * kw[8 * s + 2 * h + 1], w);
 #pragma unroll
-                    for (int m = 0; m < MT; ++m)
+                for (int c = 0; c < 3; ++c) zw[s][c][h] = w[c];
+            };
+            auto decay = [&](int m) {
 #pragma unroll
-                        for (int v = 0; v < 16; ++v) S[m][v] = __builtin_fmaf(S[m][v], dec.by, S[m][v]);
-                } else {
+                for (int v = 0; v < 16; ++v) S[m][v] = slow ? __builtin_fmaf(S[m][v], by, S[m][v]) : S[m][v] * by;
+            };
+            bf16x8 yt[2][2];   // pairs of row blocks of Y^T, one pair ahead
+            auto read_yt = [&](int i) {
+                const int s = i / (MT / 2), m = 2 * (i % (MT / 2));
+                yt[i & 1][0] = col_frag(ty, s, m), yt[i & 1][1] = col_frag(ty, s, m + 1);
+            };
+            if constexpr (OUT) {
+                const f32x16 zero = {};
+                f32x16 p = zero;
+                constexpr int RA = 3;   // fragments in flight
+                bf16x8 xf[RA], yf[RA];
+                u32x4 pf[2][PP];   // P . W
+                auto weigh_p = [&](int i) {   // registers 2 i, 2 i + 1
+                    uint32_t w[PP];
+                    parts_of<PP>(p[2 * i] * pw[2 * i], p[2 * i + 1] * pw[2 * i + 1], w);
 #pragma unroll
-                    for (int m = 0; m < MT; ++m)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) S[m][v] *= dec.by;
-                }
-            }
-            // pairs of row blocks, the next pair's fragments read one pair ahead
-            bf16x8 yt[2][2], zw[3];
-            yt[0][0] = col_frag(ty, 0, 0), yt[0][1] = col_frag(ty, 0, 1);
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {   // k-step i / (MT / 2), row blocks 2 (i % (MT / 2)) and the next
-                const int s = i / (MT / 2), m = 2 * (i % (MT / 2)), nx = i + 1;
-                if (i % (MT / 2) == 0) {
-                    float x[8];
-                    const u32x4 zr = __builtin_bit_cast(u32x4, zf[s]);
+                    for (int c = 0; c < PP; ++c) pf[i / 4][c][i % 4] = w[c];
+                };
+                auto state_part = [&](int s) {   // k-step s of S^T X^T
+                    u32x4 sf[PS];
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
-                        x[2 * h] = __uint_as_float(zr[h] << 16) * kw[8 * s + 2 * h];
-                        x[2 * h + 1] = __uint_as_float(zr[h] & 0xFFFF0000u) * kw[8 * s + 2 * h + 1];
+                        uint32_t w[PS];
+                        parts_of<PS>(S[s / 2][8 * (s & 1) + 2 * h], S[s / 2][8 * (s & 1) + 2 * h + 1], w);
+#pragma unroll
+                        for (int c = 0; c < PS; ++c) sf[c][h] = w[c];
                     }
-                    parts_of<3>(x, zw);
+#pragma unroll
+                    for (int c = 0; c < PS; ++c)
+                        o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, sf[c]), xf[s % RA], s + c ? o : zero, 0, 0, 0);
+                };
+                auto products = [&](auto with_state) {
+#pragma unroll
+                    for (int s = 0; s + 1 < RA; ++s) xf[s] = row_frag(tx, s), yf[s] = row_frag(ty, s);
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) {
+                        const int nx = s + RA - 1;
+                        if (nx < KS) xf[nx % RA] = row_frag(tx, nx), yf[nx % RA] = row_frag(ty, nx);
+                        p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yf[s % RA], xf[s % RA], s ? p : zero, 0, 0, 0);
+                        if constexpr (decltype(with_state)::value) state_part(s);
+                        if (ADV && s % (KS / 4) == KS / 4 - 1) weigh(0, s / (KS / 4));
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                };
+                if (SETS != KEYS || r.set == 0) {
+                    products(std::true_type{});
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) o[v] *= hd;
+                } else {
+                    products(std::false_type{});
                 }
-                if (nx < MT) {
-                    const int s1 = nx / (MT / 2), m1 = 2 * (nx % (MT / 2));
-                    yt[nx & 1][0] = col_frag(ty, s1, m1), yt[nx & 1][1] = col_frag(ty, s1, m1 + 1);
+                if constexpr (ADV) read_yt(0);
+#pragma unroll
+                for (int i = 0; i < 2 * PP; ++i) {
+                    if (i == 0 || (!ADV && i == PP)) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) weigh_p(4 * (i / PP) + e);
+                    }
+                    o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(zf[i / PP], __builtin_bit_cast(bf16x8, pf[i / PP][i % PP]), o, 0, 0, 0);
+                    if constexpr (ADV) {
+                        if (i < PP) {
+#pragma unroll
+                            for (int e = 4 + 4 * i / PP; e < 4 + 4 * (i + 1) / PP; ++e) weigh_p(e);
+                        }
+                        if (i < MT) decay(i);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                if constexpr (!ADV) __builtin_amdgcn_sched_barrier(0);
+            }
+            if (ADV || adv) {
+                if constexpr (!ADV) {
+                    read_yt(0);
+                    if (SETS != KEYS || r.set == 0) {
+                        if (slow) {
+#pragma unroll
+                            for (int m = 0; m < MT; ++m) decay(m);
+                        } else {
+#pragma unroll
+                            for (int m = 0; m < MT; ++m) decay(m);
+                        }
+                    }
                 }
 #pragma unroll
-                for (int c = 0; c < 3; ++c) {
-                    S[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yt[i & 1][0], zw[c], S[m], 0, 0, 0);
-                    S[m + 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yt[i & 1][1], zw[c], S[m + 1], 0, 0, 0);
+                for (int i = 0; i < MT; ++i) {   // half i / (MT / 2) of the keys, row blocks 2 (i % (MT / 2)) and the next
+                    const int s = i / (MT / 2), m = 2 * (i % (MT / 2));
+                    if (!ADV && i % (MT / 2) == 0) {
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) weigh(s, h);
+                    }
+                    if (i + 1 < MT) read_yt(i + 1);
+#pragma unroll
+                    for (int c = 0; c < 3; ++c) {
+                        S[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yt[i & 1][0], __builtin_bit_cast(bf16x8, zw[s][c]), S[m], 0, 0, 0);
+                        S[m + 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yt[i & 1][1], __builtin_bit_cast(bf16x8, zw[s][c]), S[m + 1], 0, 0, 0);
+                        if (ADV && s == 0 && c < 2) {
+#pragma unroll
+                            for (int e = 0; e < 4 / MT; ++e) weigh(1, (2 * i + c) * (4 / MT) + e);   // 4 words over the first half's pairs
+                        }
+                        if (ADV || c == 2) __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
-                __builtin_amdgcn_sched_barrier(0);
             }
-        };
-        // (of several query heads the last one brings the state on)
-        if (SETS != ROWS || !OUT || r.set == a.sets - 1) {
-            Decay dec = whole;
-            if (part) {
-                int n = r.n;
-                asm volatile("" : "+s"(n));   // (a real branch)
-                dec = decay_of(n * ld);
-            }
-            advance(dec);
         }
         if constexpr (OUT) {
             if (SETS != KEYS || r.set == a.sets - 1) {
@@ -522,7 +534,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_kernel(const LinearArgs a) {
                         }
                 }
             }
-            if (r.last && r.own_last && a.state_out && jn == 0)
+            if (r.last && r.own_last && a.state_out && leads)
                 write_state(a.state_out + ((int64_t)(a.out_by_slot ? ld_uniform(a.slots, r.seq) : r.seq) * a.Hkv + kvh) * (D * D),
                             a.out_scale);
         } else if (r.last) {
@@ -535,81 +547,93 @@ __global__ __launch_bounds__(2 * D, 2) void linear_kernel(const LinearArgs a) {
     // step c - 1, whose row stage the loads of step c + 2 take.  (Two key stages: the
     // loads of the next chunk's keys stand at least one step behind this chunk's
     // first, after every wave's last read of the chunk before.)
+    // The head's kind of decay is outside the loop, so that the state keeps its
+    // registers.
     auto inc = [](int i, int n) -> int { return i + 1 == n ? 0 : i + 1; };
-    Step r0 = walk.next(), r1 = walk.next();
-    int x0 = 0, k0 = 0, k1 = loads_keys(r1) ? inc(0, NYZ) : 0;   // stages of r0 and r1
-    issue(r0, 0, 0);
-    if (r1.live) issue(r1, 1, k1);
-    while (r0.live) {
-        if (!r1.live) wait_vm_lgkm<0>();
-        else if (loads_keys(r1)) wait_vm_lgkm<(OUT ? 3 : 2) * NI>();
-        else wait_vm_lgkm<NI>();
-        wg_barrier();
-        if constexpr (OUT) {
-            store_held();
-            held_n = 0;
+    auto run = [&](auto slow_) {
+        Step r0 = walk.next(), r1 = walk.next();
+        int x0 = 0, k0 = 0, k1 = loads_keys(r1) ? inc(0, NYZ) : 0;   // stages of r0 and r1
+        issue(r0, 0, 0);
+        if (r1.live) issue(r1, 1, k1);
+        while (r0.live) {
+            if (!r1.live) wait_vm_lgkm<0>();
+            else if (loads_keys(r1)) wait_vm_lgkm<(OUT ? 3 : 2) * NI>();
+            else wait_vm_lgkm<NI>();
+            wg_barrier();
+            if constexpr (OUT) {
+                store_held();
+                held_n = 0;
+            }
+            const Step r2 = walk.next();   // (not live past the end)
+            const int k2 = loads_keys(r2) ? inc(k1, NYZ) : k1;
+            if (r2.live) issue(r2, x0 == 0 ? 2 : x0 - 1, k2);
+            compute(r0, x0, k0, slow_);
+            r0 = r1;
+            r1 = r2;
+            k0 = k1;
+            k1 = k2;
+            x0 = inc(x0, 3);
         }
-        const Step r2 = walk.next();   // (not live past the end)
-        const int k2 = loads_keys(r2) ? inc(k1, NYZ) : k1;
-        if (r2.live) issue(r2, x0 == 0 ? 2 : x0 - 1, k2);
-        compute(r0, x0, k0);
-        r0 = r1;
-        r1 = r2;
-        k0 = k1;
-        k1 = k2;
-        x0 = inc(x0, 3);
+        if constexpr (OUT) store_held();
+    };
+    if constexpr (SETS == ONE) {
+        if (head_slow) run(std::true_type{});
+        else run(std::false_type{});
+    } else {
+        run(head_slow);
     }
-    if constexpr (OUT) store_held();
 }
 
 // Joins the cells' states: where the sequence at a cell's edge began before the
 // whole cell, the state there is the cell's own plus g^cell_len times the one at
-// its other edge.  A work-group takes 256 elements of a KV head's states, edge
-// by edge.
+// its other edge.  A wave takes 128 elements of a KV head's states, edge by edge
+// (bound by latency, so half of 64 cells' loads are in flight; only states that are
+// joined, or joined to, are read).
 template <bool REV>
 __global__ __launch_bounds__(64) void linear_scan_kernel(const LinearArgs a, int elems) {
-    __shared__ uint8_t kind[LIN_MAX_CELLS];   // of each cell's state: 0 none, 1 the neighbour cell's alone, 2 joined
-    const int kvh = blockIdx.y;
-    for (int c = threadIdx.x; c < a.ncells; c += 64) {
-        int k = 0;
-        // the edge this cell's state stands at, and the far edge of the neighbour it came over
-        const int64_t edge = REV ? (int64_t)(c + 1) * a.cell_len : (int64_t)c * a.cell_len;
-        const int64_t far = REV ? edge + a.cell_len : edge - a.cell_len;
-        if (edge > 0 && edge < a.T) {
-            int lo = 0, hi = a.S;   // the sequence of token edge
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (a.seqs[mid] <= edge) lo = mid;
-                else hi = mid;
-            }
-            const int begin = a.seqs[lo], end = a.seqs[lo + 1];
-            if (begin < edge) k = (REV ? end > far : begin < far) ? 2 : 1;
-        }
-        kind[c] = (uint8_t)k;
-    }
-    __syncthreads();
+    const int kvh = blockIdx.y, lane = threadIdx.x;
     const float full = expf(a.cell_len * log_decay_of(a.log_decay, kvh));
-    float *p = a.cells + (int64_t)kvh * elems + (int64_t)blockIdx.x * 256 + 4 * threadIdx.x;
-    const int64_t stride = (int64_t)a.Hkv * elems;
-    constexpr int AHEAD = 16;
-    f32x4 run = {0.f, 0.f, 0.f, 0.f};
-    for (int c0 = 0; c0 < a.ncells; c0 += AHEAD) {
-        f32x4 x[AHEAD];
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int c = REV ? a.ncells - 1 - c0 - i : c0 + i;
-            if (c0 + i < a.ncells && kind[c]) x[i] = *(const f32x4 *)(p + c * stride);
+    const int64_t stride = (REV ? -1 : 1) * (int64_t)a.Hkv * elems;
+    float *p = a.cells + (REV ? (int64_t)(a.ncells - 1) * a.Hkv * elems : 0) + (int64_t)kvh * elems + (int64_t)blockIdx.x * 128 + 2 * lane;
+    const int few = a.S < 64 ? a.seqs[min(lane, a.S)] : 0;   // the offsets, where lanes hold them all
+    auto offset = [&](int i) -> int { return a.S < 64 ? __shfl(few, i) : a.seqs[i]; };
+    f32x2 run = {0.f, 0.f};
+    for (int c0 = 0; c0 < a.ncells; c0 += 64, p += 64 * stride) {
+        // lane i: the state of the i-th cell from here, whose edge is where it stands
+        // and whose far edge is that of the neighbour it came over
+        const int c = REV ? a.ncells - 1 - c0 - lane : c0 + lane;
+        const int64_t edge = (int64_t)(REV ? c + 1 : c) * a.cell_len;
+        const int64_t far = REV ? edge + a.cell_len : edge - a.cell_len, next = REV ? edge - a.cell_len : edge + a.cell_len;
+        int lo = 0, hi = a.S;   // the sequence of token edge
+        while (__any(hi - lo > 1)) {
+            const int mid = (lo + hi) >> 1;
+            if (offset(mid) <= edge) lo = mid;
+            else hi = mid;
         }
+        const int begin = offset(lo), end = offset(lo + 1);
+        const bool over = c0 + lane < a.ncells && edge > 0 && edge < a.T && begin < edge;   // a sequence goes on over the edge
+        const bool join = over && (REV ? end > far : begin < far);
+        const uint64_t joined = __builtin_amdgcn_ballot_w64(join);
+        const uint64_t read = joined | __builtin_amdgcn_ballot_w64(over && (REV ? begin < next : end > next));
+        constexpr int AHEAD = 32;
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int c = REV ? a.ncells - 1 - c0 - i : c0 + i;
-            if (c0 + i >= a.ncells || !kind[c]) continue;
-            if (kind[c] == 2) {
+        for (int h = 0; h < 64; h += AHEAD) {
+            if (!(read >> h)) break;
+            f32x2 x[AHEAD];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[i][e] = __builtin_fmaf(run[e], full, x[i][e]);
-                *(f32x4 *)(p + c * stride) = x[i];
+            for (int i = 0; i < AHEAD; ++i)
+                if (read >> (h + i) & 1) x[i] = *(const f32x2 *)(p + (h + i) * stride);
+            __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): a wait behind each branch would be for the stores too
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                if (!(read >> (h + i) & 1)) continue;
+                if (joined >> (h + i) & 1) {
+                    x[i][0] = __builtin_fmaf(run[0], full, x[i][0]);
+                    x[i][1] = __builtin_fmaf(run[1], full, x[i][1]);
+                    *(f32x2 *)(p + (h + i) * stride) = x[i];
+                }
+                run = x[i];
             }
-            run = x[i];
         }
     }
 }
@@ -630,74 +654,105 @@ __global__ __launch_bounds__(256) void linear_commit_kernel(const float *from, f
     t[i] = f[i];
 }
 
+// The lane's value plus another's of its row of 16: rotations by 8 and 4 add what
+// stands there, and lanes 2 apart of four.
+template <int CTRL>
+__device__ __forceinline__ float plus_dpp(float x) {
+    return x + __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), CTRL, 0xF, 0xF, true));
+}
+
 // A few new tokens against the states in memory, one after the other: with S
-// the state's D x 32 columns of a wave in registers,
+// the state's D x CW columns of a wave in registers,
 //   S = g S + k v^T,   o = scale q S   for each query head.
 // Bound by reading and writing the states, 4 D^2 bytes each, while a token
 // takes (2 + G) D^2 FMAs per KV head.  A lane holds 4 neighbouring columns of
-// every eighth row, so a load instruction covers eight 128-byte pieces, and the
-// rows' sums meet in three lane exchanges; no barrier, no LDS.
-template <int D, bool F32>
+// every (256 / CW)-th row; its partial sums of 4 columns become the whole sum of
+// one by exchanging halves twice and rotations, no barrier, no LDS.
+// CW: 32, whose loads are of whole cache lines, where there are waves enough;
+// 8 for a few, whose tokens' instructions come to a quarter.
+template <int D, int CW, bool F32>
 __global__ __launch_bounds__(64) void linear_step_kernel(const LinearStepArgs a) {
-    constexpr int NR = D / 8;
-    const int lane = threadIdx.x, cg = lane & 7, rg = lane >> 3;
-    const int part = blockIdx.x % (D / 32);
-    const uint32_t bh = blockIdx.x / (D / 32);
+    constexpr int LPR = CW / 4, RPL = 64 / LPR, NR = D / RPL;   // lanes per row, rows per load, loads
+    const int lane = threadIdx.x, cg = lane % LPR, rg = lane / LPR;
+    const int part = blockIdx.x % (D / CW);
+    const uint32_t bh = blockIdx.x / (D / CW);
     const int b = (int)fastdiv(bh, a.fd_hkv), kvh = (int)(bh - (uint32_t)b * (uint32_t)a.Hkv);
     const int n = a.new_lens ? ld_uniform(a.new_lens, b) : a.Ln;
     if (n == 0) return;
-    const int col = 32 * part + 4 * cg;
+    const int col = CW * part + 4 * cg;
     float *p = a.pool + ((int64_t)ld_uniform(a.slots, b) * a.Hkv + kvh) * (D * D) + rg * D + col;
     f32x4 S[NR];
 #pragma unroll
-    for (int i = 0; i < NR; ++i) S[i] = *(const f32x4 *)(p + 8 * i * D);
-    const Decay dec = decay_of(log_decay_of(a.log_decay, kvh));
-    const uint32_t keep = dec.slow ? ~0u : 0u;
+    for (int i = 0; i < NR; ++i) S[i] = *(const f32x4 *)(p + RPL * i * D);
+    const float ld = log_decay_of(a.log_decay, kvh);
+    const bool slow = is_slow(ld);
+    const float by = slow ? expm1f(ld) : expf(ld);
+    const uint32_t keep = slow ? ~0u : 0u;
     const uint16_t *q = a.q + b * a.q_sb + (int64_t)kvh * a.G * a.q_sh + rg;
     const uint16_t *k = a.k + b * a.k_sb + kvh * a.k_sh + rg;
     const uint16_t *v = a.v + b * a.v_sb + kvh * a.v_sh + col;
+    // the column whose sum the lane ends with
+    const int mine = 2 * (lane >> 4 & 1) + (lane >> 5);
+    const bool writes = (lane & 15) < LPR;
+    // rows as they lie in memory, one token (of the queries: one head) ahead
+    u32x2 vr;
+    uint16_t kr[NR], qr[NR];
+    auto read_key = [&](int t) {
+        vr = *(const u32x2 *)(v + t * a.v_st);
+#pragma unroll
+        for (int i = 0; i < NR; ++i) kr[i] = k[t * a.k_st + RPL * i];
+    };
+    auto read_query = [&](int t, int g) {
+#pragma unroll
+        for (int i = 0; i < NR; ++i) qr[i] = q[t * a.q_st + g * a.q_sh + RPL * i];
+    };
+    read_key(0);
+    read_query(0, 0);
     for (int t = 0; t < n; ++t) {
-        const u32x2 vr = *(const u32x2 *)(v + t * a.v_st);
         const f32x4 vv = {__uint_as_float(vr[0] << 16), __uint_as_float(vr[0] & 0xFFFF0000u), __uint_as_float(vr[1] << 16),
                           __uint_as_float(vr[1] & 0xFFFF0000u)};
         float kf[NR];
 #pragma unroll
-        for (int i = 0; i < NR; ++i) kf[i] = __uint_as_float((uint32_t)k[t * a.k_st + 8 * i] << 16);
+        for (int i = 0; i < NR; ++i) kf[i] = __uint_as_float((uint32_t)kr[i] << 16);
+        if (t + 1 < n) read_key(t + 1);
 #pragma unroll
         for (int i = 0; i < NR; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float kept = __uint_as_float(__float_as_uint(S[i][e]) & keep);   // S of a slow head, else 0
-                S[i][e] = __builtin_fmaf(kf[i], vv[e], __builtin_fmaf(S[i][e], dec.by, kept));
+                S[i][e] = __builtin_fmaf(kf[i], vv[e], __builtin_fmaf(S[i][e], by, kept));
             }
         for (int g = 0; g < a.G; ++g) {
             f32x4 o = {0.f, 0.f, 0.f, 0.f};
+            float x[NR];
 #pragma unroll
-            for (int i = 0; i < NR; ++i) {
-                const float x = __uint_as_float((uint32_t)q[t * a.q_st + g * a.q_sh + 8 * i] << 16);
+            for (int i = 0; i < NR; ++i) x[i] = __uint_as_float((uint32_t)qr[i] << 16);
+            if (g + 1 < a.G) read_query(t, g + 1);
+            else if (t + 1 < n) read_query(t + 1, 0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(x, S[i][e], o[e]);
+            for (int i = 0; i < NR; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(x[i], S[i][e], o[e]);
+            // lanes past 32: columns 1 and 3; of every 32 the upper 16: columns 2 and 3
+            float half[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const u32x2 y = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[2 * h]), __float_as_uint(o[2 * h + 1]), false, false);
+                half[h] = __uint_as_float(y[0]) + __uint_as_float(y[1]);
             }
-#pragma unroll
-            for (int m = 8; m < 64; m *= 2)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], m);
-            if (rg == 0) {
-                const int64_t at = b * a.o_sb + t * a.o_st + (int64_t)(kvh * a.G + g) * a.o_sh + col;
-                if constexpr (F32) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[e] *= a.scale;
-                    *(f32x4 *)((float *)a.out + at) = o;
-                } else {
-                    *(u32x2 *)((uint16_t *)a.out + at) = u32x2{pack_bf16x2(o[0] * a.scale, o[1] * a.scale),
-                                                              pack_bf16x2(o[2] * a.scale, o[3] * a.scale)};
-                }
+            const u32x2 y = __builtin_amdgcn_permlane16_swap(__float_as_uint(half[0]), __float_as_uint(half[1]), false, false);
+            float sum = plus_dpp<0x128>(__uint_as_float(y[0]) + __uint_as_float(y[1]));   // (lanes 8 apart)
+            if constexpr (LPR == 2) sum = plus_dpp<0x4E>(plus_dpp<0x124>(sum));           // (4 and 2 apart)
+            if (writes) {
+                const int64_t at = b * a.o_sb + t * a.o_st + (int64_t)(kvh * a.G + g) * a.o_sh + col + mine;
+                if constexpr (F32) ((float *)a.out)[at] = sum * a.scale;
+                else ((uint16_t *)a.out)[at] = (uint16_t)pack_bf16x2(sum * a.scale, 0.f);
             }
         }
     }
     if (a.commit)
 #pragma unroll
-        for (int i = 0; i < NR; ++i) *(f32x4 *)(p + 8 * i * D) = S[i];
+        for (int i = 0; i < NR; ++i) *(f32x4 *)(p + RPL * i * D) = S[i];
 }
 
 template <int D, bool REV>
@@ -715,16 +770,29 @@ int linear_t(const LinearArgs &a, hipStream_t st) {
     return (int)hipGetLastError();
 }
 
+constexpr int64_t FULL = 1024;   // waves of the wide step from which every SIMD has one
+
+template <int D, bool F32>
+int step_t(const LinearStepArgs &a, hipStream_t st) {
+    const int64_t heads = (int64_t)a.B * a.Hkv;
+    if (heads * (D / 32) >= FULL) hipLaunchKernelGGL((linear_step_kernel<D, 32, F32>), dim3((unsigned)(heads * (D / 32))), dim3(64), 0, st, a);
+    else hipLaunchKernelGGL((linear_step_kernel<D, 8, F32>), dim3((unsigned)(heads * (D / 8))), dim3(64), 0, st, a);
+    return (int)hipGetLastError();
+}
+
 template <int D, bool REV>
 int cells_t(LinearArgs a, hipStream_t st) {
+    // (forwards the states do not depend on the row heads)
+    a.head_rows = 1;
+    a.fd_rows = fastdiv_make(1);
+    a.fd_heads = fastdiv_make((uint32_t)a.Hkv);
     a.n_work = a.ncells * a.Hkv;
     a.per_xcd = (a.n_work + NUM_XCD - 1) / NUM_XCD;
     const dim3 grid(a.per_xcd * NUM_XCD), block(2 * D);
-    // (forwards the states do not depend on the row heads)
     if (REV && a.sets > 1) hipLaunchKernelGGL((linear_kernel<D, REV, false, false, REV ? KEYS : ONE>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((linear_kernel<D, REV, false, false, ONE>), grid, block, 0, st, a);
     if (int e = (int)hipGetLastError()) return e;
-    hipLaunchKernelGGL((linear_scan_kernel<REV>), dim3(D * D / 256, a.Hkv), dim3(64), 0, st, a, D * D);
+    hipLaunchKernelGGL((linear_scan_kernel<REV>), dim3(D * D / 128, a.Hkv), dim3(64), 0, st, a, D * D);
     return (int)hipGetLastError();
 }
 
@@ -758,15 +826,8 @@ int launch_linear_commit(const float *from, float *pool, const int32_t *slots, i
 
 int launch_linear_step(const LinearStepArgs &a, int head_dim, void *stream) {
     hipStream_t st = (hipStream_t)stream;
-    const dim3 grid((unsigned)a.B * a.Hkv * (head_dim / 32)), block(64);
-    if (head_dim == 128) {
-        if (a.out_f32) hipLaunchKernelGGL((linear_step_kernel<128, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((linear_step_kernel<128, false>), grid, block, 0, st, a);
-    } else {
-        if (a.out_f32) hipLaunchKernelGGL((linear_step_kernel<64, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((linear_step_kernel<64, false>), grid, block, 0, st, a);
-    }
-    return (int)hipGetLastError();
+    if (head_dim == 128) return a.out_f32 ? step_t<128, true>(a, st) : step_t<128, false>(a, st);
+    return a.out_f32 ? step_t<64, true>(a, st) : step_t<64, false>(a, st);
 }
 
 }  // namespace ws
