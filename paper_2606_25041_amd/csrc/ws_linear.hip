@@ -668,14 +668,19 @@ __device__ __forceinline__ float plus_dpp(float x) {
 // takes (2 + G) D^2 FMAs per KV head.  A lane holds 4 neighbouring columns of
 // every (256 / CW)-th row; its partial sums of 4 columns become the whole sum of
 // one by exchanging halves twice and rotations, no barrier, no LDS.
-// CW: 32, whose loads are of whole cache lines, where there are waves enough;
-// 8 for a few, whose tokens' instructions come to a quarter.
+// CW: 32, whose loads are of whole cache lines, where every SIMD has such a wave;
+// 8 below, whose tokens' instructions come to a quarter (24 heads of 128, us for 1
+// and 8 tokens: 3 sequences 4.6 and 8.4 against 5.0 and 12.6, 8: 7.9 and 12.2
+// against 7.4 and 15.0, 16: 17.1 and 22.7 against 13.0 and 23.0).
 template <int D, int CW, bool F32>
 __global__ __launch_bounds__(64) void linear_step_kernel(const LinearStepArgs a) {
     constexpr int LPR = CW / 4, RPL = 64 / LPR, NR = D / RPL;   // lanes per row, rows per load, loads
     const int lane = threadIdx.x, cg = lane % LPR, rg = lane / LPR;
-    const int part = blockIdx.x % (D / CW);
-    const uint32_t bh = blockIdx.x / (D / CW);
+    // (narrow parts of a state share its cache lines: on one XCD)
+    const uint32_t w = CW < 32 ? blockIdx.x % NUM_XCD * (gridDim.x / NUM_XCD) + blockIdx.x / NUM_XCD : blockIdx.x;
+    const int part = w % (D / CW);
+    const uint32_t bh = w / (D / CW);
+    if (bh >= (uint32_t)a.B * (uint32_t)a.Hkv) return;
     const int b = (int)fastdiv(bh, a.fd_hkv), kvh = (int)(bh - (uint32_t)b * (uint32_t)a.Hkv);
     const int n = a.new_lens ? ld_uniform(a.new_lens, b) : a.Ln;
     if (n == 0) return;
@@ -770,13 +775,13 @@ int linear_t(const LinearArgs &a, hipStream_t st) {
     return (int)hipGetLastError();
 }
 
-constexpr int64_t FULL = 1024;   // waves of the wide step from which every SIMD has one
+constexpr int64_t FULL = 1024;   // wide waves of a step that give every SIMD one
 
 template <int D, bool F32>
 int step_t(const LinearStepArgs &a, hipStream_t st) {
     const int64_t heads = (int64_t)a.B * a.Hkv;
     if (heads * (D / 32) >= FULL) hipLaunchKernelGGL((linear_step_kernel<D, 32, F32>), dim3((unsigned)(heads * (D / 32))), dim3(64), 0, st, a);
-    else hipLaunchKernelGGL((linear_step_kernel<D, 8, F32>), dim3((unsigned)(heads * (D / 8))), dim3(64), 0, st, a);
+    else hipLaunchKernelGGL((linear_step_kernel<D, 8, F32>), dim3((unsigned)((heads * (D / 8) + NUM_XCD - 1) / NUM_XCD * NUM_XCD)), dim3(64), 0, st, a);
     return (int)hipGetLastError();
 }
 
