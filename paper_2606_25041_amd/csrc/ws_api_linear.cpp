@@ -151,8 +151,9 @@ size_t ws_linear_workspace_bytes(int32_t num_seqs, int32_t total_tokens, int32_t
     if (num_seqs <= 0 || total_tokens < 0 || total_tokens > MAX_TOKENS || num_q_heads <= 0 || num_kv_heads <= 0 ||
         num_q_heads % num_kv_heads || (head_dim != 64 && head_dim != 128))
         return 0;
-    return cells_bytes(total_tokens, num_kv_heads, head_dim) +
-           (size_t)num_seqs * num_kv_heads * head_dim * head_dim * sizeof(float);
+    // (the gradients' two passes have cells of their own, the forward's sequences their last states)
+    const size_t cells = cells_bytes(total_tokens, num_kv_heads, head_dim);
+    return cells + std::max(cells, (size_t)num_seqs * num_kv_heads * head_dim * head_dim * sizeof(float));
 }
 
 int ws_linear_attn_prefill(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const float *log_decay, const int32_t *off_host,
@@ -205,9 +206,9 @@ int ws_linear_attn_prefill(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const float
     a.state_out = !writes ? nullptr : late ? after : state->pool;
     a.out_by_slot = !late;
     if (edges)
-        if (int e = launch_linear_cells(a, false, head_dim, stream)) return fail(WS_ERR_HIP, "launch failed (hip error %d)", e);
+        if (int e = launch_linear_cells(a, head_dim, stream)) return fail(WS_ERR_HIP, "launch failed (hip error %d)", e);
     if (tokens > 0)
-        if (int e = launch_linear(a, false, head_dim, stream)) return fail(WS_ERR_HIP, "launch failed (hip error %d)", e);
+        if (int e = launch_linear(a, head_dim, stream)) return fail(WS_ERR_HIP, "launch failed (hip error %d)", e);
     if (writes && any_empty(off_host, num_seqs) && (late || !reads))
         if (int e = launch_linear_empty(a, head_dim, stream)) return fail(WS_ERR_HIP, "launch failed (hip error %d)", e);
     if (late)
@@ -265,6 +266,7 @@ int ws_linear_attn_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tens
     a.slots = state ? state->slots_dev : nullptr;
     // dV and dK: backwards, the states of Q dO^T summed over a KV head's query heads
     LinearArgs r = a;
+    r.cells = (float *)((char *)workspace + cells_bytes(tokens, num_kv_heads, head_dim));
     r.job[0] = job_of(k, q, dout, dv, false, false);
     r.job[1] = job_of(v, dout, q, dk, true, true);
     r.njobs = 2;
@@ -275,11 +277,9 @@ int ws_linear_attn_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tens
     r.out_scale = scale;
     if (tokens > 0) {
         if (!plan_pass(a, false, head_dim) || !plan_pass(r, true, head_dim)) return fail(WS_ERR_SHAPE, "too many work items");
-        for (LinearArgs *p : {&a, &r}) {
-            if (crosses(off_host, num_seqs, p->cell_len))
-                if (int e = launch_linear_cells(*p, p == &r, head_dim, stream)) return fail(WS_ERR_HIP, "launch failed (hip error %d)", e);
-            if (int e = launch_linear(*p, p == &r, head_dim, stream)) return fail(WS_ERR_HIP, "launch failed (hip error %d)", e);
-        }
+        const LinearPair p{a, r};
+        if (int e = launch_linear_pair(p, crosses(off_host, num_seqs, a.cell_len), crosses(off_host, num_seqs, r.cell_len), head_dim, stream))
+            return fail(WS_ERR_HIP, "launch failed (hip error %d)", e);
     }
     if (dstate0 && any_empty(off_host, num_seqs))
         if (int e = launch_linear_empty(r, head_dim, stream)) return fail(WS_ERR_HIP, "launch failed (hip error %d)", e);

@@ -1,7 +1,8 @@
 // Internal interface between the host-side validation/planning code
-// (ws_api.cpp and ws_api4.cpp, no HIP headers) and the gfx950 kernels
-// (ws_kernels.hip for attention, merge and append; ws_cache4.hip for the 4-bit
-// cache; ws_bwd.hip for the gradients).
+// (ws_api.cpp, ws_api4.cpp and ws_api_pack.cpp, no HIP headers) and the gfx950
+// kernels (ws_kernels.hip for attention, merge and append; ws_cache4.hip for the
+// 4-bit cache; ws_bwd.hip for the gradients).  Linear attention has an interface
+// of its own (ws_linear.h).
 #pragma once
 
 #include <stddef.h>

@@ -5,7 +5,8 @@
 // a token-causal segment (the thinker's language and state slots, Sec. 1 and
 // Sec. 2.4) whose tokens see the segment only up to themselves.  The step
 // kernel runs the current unit against its full-history cache (Sec. 2.4);
-// the prefill kernel covers whole sequences (Sec. 2.4, system prefill); the
+// the prefill kernel covers whole sequences (Sec. 2.4, system prefill), of equal
+// length or packed one behind the other; the
 // append kernel commits a KV slice to the paged cache (Sec. 2.4).  Both take a
 // sliding window with sinks, and the step a cache held in 4 bits, whose append,
 // read-back and steps of few rows are in ws_cache4.hip.  The gradient kernels,

@@ -50,6 +50,11 @@ struct LinearArgs {
     int32_t n_work, per_xcd;
 };
 
+// The passes of the gradients, dQ's and that of dV and dK.
+struct LinearPair {
+    LinearArgs forwards, backwards;
+};
+
 struct LinearStepArgs {
     const uint16_t *q, *k, *v;
     int64_t q_sb, q_st, q_sh, k_sb, k_st, k_sh, v_sb, v_st, v_sh;
@@ -67,9 +72,11 @@ struct LinearStepArgs {
 
 #define WS_HIDDEN __attribute__((visibility("hidden")))
 // Each returns 0 or a HIP error code.
-// the states at the cells' edges (pass 1 and the scan that joins them)
-WS_HIDDEN int launch_linear_cells(const LinearArgs &a, bool backwards, int head_dim, void *stream);
-WS_HIDDEN int launch_linear(const LinearArgs &a, bool backwards, int head_dim, void *stream);
+// the states at the cells' edges of a pass forwards (pass 1 and the scan that joins them)
+WS_HIDDEN int launch_linear_cells(const LinearArgs &a, int head_dim, void *stream);
+WS_HIDDEN int launch_linear(const LinearArgs &a, int head_dim, void *stream);
+// both passes of the gradients, with their cells' states where a sequence crosses an edge
+WS_HIDDEN int launch_linear_pair(const LinearPair &p, bool cells, bool cells_backwards, int head_dim, void *stream);
 // states of sequences without tokens: in (scaled) or zero to out
 WS_HIDDEN int launch_linear_empty(const LinearArgs &a, int head_dim, void *stream);
 // [S][Hkv][D][D] states to their slots in the pool

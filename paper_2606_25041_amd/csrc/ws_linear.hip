@@ -145,29 +145,33 @@ __device__ __forceinline__ int sequence_of(const int32_t *off, int S, int t, int
 // after the other; ROWS, its query heads are taken after each other against the
 // same keys, whose products with the state (24 of the 44 MFMAs) are then formed
 // once.
+//
+// A tile's rows lie in groups of 1 KiB, what one wave-wide load brings, 16 bytes
+// apart; in a group 16-byte chunk c of row r is in slot c ^ turn(r), so that of
+// chunk indices only the upper bits are in an XOR and the rest of a read's address
+// is a constant.
+constexpr int GROUPB = 1024 + 16;
+constexpr int tile_bytes(int D) { return C * 2 * D / 1024 * GROUPB; }
+// rings of the keys and values and, behind them, of the rows, three stages each
+// (two of keys where several steps share them)
+constexpr int key_stages(int sets) { return sets == ROWS ? 2 : 3; }
+constexpr int lds_bytes(int D, bool out, int sets) { return (2 * key_stages(sets) + (out ? 3 : 0)) * tile_bytes(D); }
+
 template <int D, bool REV, bool F32, bool OUT, int SETS>
-__global__ __launch_bounds__(2 * D, 2) void linear_kernel(const LinearArgs a) {
+__device__ __forceinline__ void linear_pass(const LinearArgs &a, const uint32_t block, char *smem) {
     constexpr int NW = D / 32, MT = D / 32, KS = D / 16;
     constexpr int PP = F32 ? 3 : 2, PS = F32 ? 3 : 1;   // bf16 parts of P . W and of S as operands
-    // A tile's rows lie in groups of 1 KiB, what one wave-wide load brings, 16
-    // bytes apart; in a group 16-byte chunk c of row r is in slot c ^ turn(r), so
-    // that of chunk indices only the upper bits are in an XOR and the rest of a
-    // read's address is a constant.
-    constexpr int ROWB = 2 * D, GROUPB = 1024 + 16, TILEB = C * ROWB / 1024 * GROUPB;
-    // rings of the keys and values and, behind them, of the rows, three stages each
-    // (two of keys where several steps share them)
-    constexpr int NYZ = SETS == ROWS ? 2 : 3, NX = OUT ? 3 : 0, XRING = NYZ * 2 * TILEB;
+    constexpr int ROWB = 2 * D, TILEB = tile_bytes(D), NYZ = key_stages(SETS), XRING = NYZ * 2 * TILEB;
     constexpr int LPR = ROWB / 16, RPW = 64 / LPR;   // lanes per row, rows per wave-wide load
     constexpr int NI = C / (NW * RPW);               // loads per wave and tile
     static_assert(NI == 2, "two loads a tile");
-    __shared__ __attribute__((aligned(1024))) char smem[XRING + NX * TILEB];
 
     const int lane = threadIdx.x & 63, hf = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
     // ---- work item: (cell, head, job), the heads being KV heads or, with
     // head_rows of them to a KV head, query heads ---------------------------------
-    const uint32_t w = (blockIdx.x % NUM_XCD) * (uint32_t)a.per_xcd + blockIdx.x / NUM_XCD;
+    const uint32_t w = (block % NUM_XCD) * (uint32_t)a.per_xcd + block / NUM_XCD;
     if (w >= (uint32_t)a.n_work) return;
     uint32_t item = w;
     int jn = 0;
@@ -584,13 +588,32 @@ __global__ __launch_bounds__(2 * D, 2) void linear_kernel(const LinearArgs a) {
     }
 }
 
+template <int D, bool F32, bool OUT, int SETS>
+__global__ __launch_bounds__(2 * D, 2) void linear_kernel(const LinearArgs a) {
+    __shared__ __attribute__((aligned(1024))) char smem[lds_bytes(D, OUT, SETS)];
+    linear_pass<D, false, F32, OUT, SETS>(a, blockIdx.x, smem);
+}
+
+// The two passes of the gradients, which do not depend on each other, in one
+// launch: the one backwards in time, whose work-groups have the most to do, first.
+// (8192 tokens of 32/8 heads of 128 with the forward: 330 us apart, 292 together;
+// 2 x 16384 of 24 heads: 1105 and 1022.)
+template <int D, bool OUT, int SETS, int REV_SETS>
+__global__ __launch_bounds__(2 * D, 2) void linear_pair_kernel(const LinearPair p) {
+    constexpr int A = lds_bytes(D, OUT, SETS), B = lds_bytes(D, OUT, REV_SETS);
+    __shared__ __attribute__((aligned(1024))) char smem[A > B ? A : B];
+    const uint32_t first = (uint32_t)p.backwards.per_xcd * NUM_XCD;
+    if (blockIdx.x < first) linear_pass<D, true, false, OUT, REV_SETS>(p.backwards, blockIdx.x, smem);
+    else linear_pass<D, false, false, OUT, SETS>(p.forwards, blockIdx.x - first, smem);
+}
+
 // Joins the cells' states: where the sequence at a cell's edge began before the
 // whole cell, the state there is the cell's own plus g^cell_len times the one at
 // its other edge.  A wave takes 128 elements of a KV head's states, edge by edge
 // (bound by latency, so half of 64 cells' loads are in flight; only states that are
 // joined, or joined to, are read).
 template <bool REV>
-__global__ __launch_bounds__(64) void linear_scan_kernel(const LinearArgs a, int elems) {
+__device__ __forceinline__ void linear_scan(const LinearArgs &a, int elems) {
     const int kvh = blockIdx.y, lane = threadIdx.x;
     const float full = expf(a.cell_len * log_decay_of(a.log_decay, kvh));
     const int64_t stride = (REV ? -1 : 1) * (int64_t)a.Hkv * elems;
@@ -636,6 +659,13 @@ __global__ __launch_bounds__(64) void linear_scan_kernel(const LinearArgs a, int
             }
         }
     }
+}
+
+__global__ __launch_bounds__(64) void linear_scan_kernel(const LinearArgs a, int elems) { linear_scan<false>(a, elems); }
+
+__global__ __launch_bounds__(64) void linear_pair_scan_kernel(const LinearPair p, int elems) {
+    if (blockIdx.z == 0) linear_scan<true>(p.backwards, elems);
+    else linear_scan<false>(p.forwards, elems);
 }
 
 __global__ __launch_bounds__(256) void linear_empty_kernel(const LinearArgs a, int elems) {
@@ -760,17 +790,15 @@ __global__ __launch_bounds__(64) void linear_step_kernel(const LinearStepArgs a)
         for (int i = 0; i < NR; ++i) *(f32x4 *)(p + RPL * i * D) = S[i];
 }
 
-template <int D, bool REV>
+template <int D>
 int linear_t(const LinearArgs &a, hipStream_t st) {
     const dim3 grid(a.per_xcd * NUM_XCD), block(2 * D);
-    // (gradients are bf16; backwards the sets are of keys, forwards of rows)
-    constexpr int MANY = REV ? KEYS : ROWS;
-    if (a.out_f32 && !REV) {
-        if (a.sets > 1) hipLaunchKernelGGL((linear_kernel<D, REV, !REV, true, MANY>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((linear_kernel<D, REV, !REV, true, ONE>), grid, block, 0, st, a);
+    if (a.out_f32) {
+        if (a.sets > 1) hipLaunchKernelGGL((linear_kernel<D, true, true, ROWS>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((linear_kernel<D, true, true, ONE>), grid, block, 0, st, a);
     } else {
-        if (a.sets > 1) hipLaunchKernelGGL((linear_kernel<D, REV, false, true, MANY>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((linear_kernel<D, REV, false, true, ONE>), grid, block, 0, st, a);
+        if (a.sets > 1) hipLaunchKernelGGL((linear_kernel<D, false, true, ROWS>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((linear_kernel<D, false, true, ONE>), grid, block, 0, st, a);
     }
     return (int)hipGetLastError();
 }
@@ -785,36 +813,67 @@ int step_t(const LinearStepArgs &a, hipStream_t st) {
     return (int)hipGetLastError();
 }
 
-template <int D, bool REV>
-int cells_t(LinearArgs a, hipStream_t st) {
-    // (forwards the states do not depend on the row heads)
+// The pass over a cell's states has a work-group per KV head.
+void of_cells(LinearArgs &a, bool any) {
     a.head_rows = 1;
     a.fd_rows = fastdiv_make(1);
     a.fd_heads = fastdiv_make((uint32_t)a.Hkv);
+    if (!any) a.ncells = 0;
     a.n_work = a.ncells * a.Hkv;
     a.per_xcd = (a.n_work + NUM_XCD - 1) / NUM_XCD;
-    const dim3 grid(a.per_xcd * NUM_XCD), block(2 * D);
-    if (REV && a.sets > 1) hipLaunchKernelGGL((linear_kernel<D, REV, false, false, REV ? KEYS : ONE>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((linear_kernel<D, REV, false, false, ONE>), grid, block, 0, st, a);
+}
+
+template <int D>
+int cells_t(LinearArgs a, hipStream_t st) {
+    of_cells(a, true);
+    // (the states do not depend on the row heads)
+    hipLaunchKernelGGL((linear_kernel<D, false, false, ONE>), dim3(a.per_xcd * NUM_XCD), dim3(2 * D), 0, st, a);
     if (int e = (int)hipGetLastError()) return e;
-    hipLaunchKernelGGL((linear_scan_kernel<REV>), dim3(D * D / 128, a.Hkv), dim3(64), 0, st, a, D * D);
+    hipLaunchKernelGGL(linear_scan_kernel, dim3(D * D / 128, a.Hkv), dim3(64), 0, st, a, D * D);
+    return (int)hipGetLastError();
+}
+
+template <int D>
+int pair_t(const LinearPair &p, bool cells, bool cells_backwards, hipStream_t st) {
+    const dim3 block(2 * D);
+    if (cells || cells_backwards) {
+        LinearPair c = p;
+        of_cells(c.forwards, cells);
+        of_cells(c.backwards, cells_backwards);
+        const dim3 grid((c.forwards.per_xcd + c.backwards.per_xcd) * NUM_XCD);
+        if (p.backwards.sets > 1) hipLaunchKernelGGL((linear_pair_kernel<D, false, ONE, KEYS>), grid, block, 0, st, c);
+        else hipLaunchKernelGGL((linear_pair_kernel<D, false, ONE, ONE>), grid, block, 0, st, c);
+        if (int e = (int)hipGetLastError()) return e;
+        hipLaunchKernelGGL(linear_pair_scan_kernel, dim3(D * D / 128, p.forwards.Hkv, 2), dim3(64), 0, st, c, D * D);
+        if (int e = (int)hipGetLastError()) return e;
+    }
+    const dim3 grid((p.forwards.per_xcd + p.backwards.per_xcd) * NUM_XCD);
+    if (p.forwards.sets > 1) hipLaunchKernelGGL((linear_pair_kernel<D, true, ROWS, KEYS>), grid, block, 0, st, p);
+    else if (p.backwards.sets > 1) hipLaunchKernelGGL((linear_pair_kernel<D, true, ONE, KEYS>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((linear_pair_kernel<D, true, ONE, ONE>), grid, block, 0, st, p);
     return (int)hipGetLastError();
 }
 
 }  // namespace
 
-int launch_linear(const LinearArgs &a, bool backwards, int head_dim, void *stream) {
+int launch_linear(const LinearArgs &a, int head_dim, void *stream) {
     hipStream_t st = (hipStream_t)stream;
-    if (head_dim == 128) return backwards ? linear_t<128, true>(a, st) : linear_t<128, false>(a, st);
-    if (head_dim == 64) return backwards ? linear_t<64, true>(a, st) : linear_t<64, false>(a, st);
+    if (head_dim == 128) return linear_t<128>(a, st);
+    if (head_dim == 64) return linear_t<64>(a, st);
     return (int)hipErrorInvalidValue;
 }
 
-int launch_linear_cells(const LinearArgs &a, bool backwards, int head_dim, void *stream) {
+int launch_linear_cells(const LinearArgs &a, int head_dim, void *stream) {
     hipStream_t st = (hipStream_t)stream;
-    if (a.ncells > LIN_MAX_CELLS) return (int)hipErrorInvalidValue;
-    if (head_dim == 128) return backwards ? cells_t<128, true>(a, st) : cells_t<128, false>(a, st);
-    if (head_dim == 64) return backwards ? cells_t<64, true>(a, st) : cells_t<64, false>(a, st);
+    if (head_dim == 128) return cells_t<128>(a, st);
+    if (head_dim == 64) return cells_t<64>(a, st);
+    return (int)hipErrorInvalidValue;
+}
+
+int launch_linear_pair(const LinearPair &p, bool cells, bool cells_backwards, int head_dim, void *stream) {
+    hipStream_t st = (hipStream_t)stream;
+    if (head_dim == 128) return pair_t<128>(p, cells, cells_backwards, st);
+    if (head_dim == 64) return pair_t<64>(p, cells, cells_backwards, st);
     return (int)hipErrorInvalidValue;
 }
 
