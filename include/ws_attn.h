@@ -634,7 +634,9 @@ int ws_block_causal_prefill_packed(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v,
  *               8 * num_q_heads * total_tokens bytes (rounded up to 256) + 8 *
  *               total_tokens are enough to run, unsplit
  * total_tokens must be below 2^30.  Deterministic, and as exact, as
- * ws_block_causal_prefill_bwd.
+ * ws_block_causal_prefill_bwd; rows with at most four tiles of 64 keys take
+ * <dout, o> from their scores instead of the rounded o.  What is not finite stays
+ * where the forward keeps it.
  */
 int ws_block_causal_prefill_packed_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 o,
                                        ws_tensor4 dout, const float *lse,
@@ -667,8 +669,8 @@ size_t ws_prefill_packed_bwd_workspace_bytes(int32_t total_tokens, int32_t num_q
  * copy, int32, the same values).  A call that writes states refuses slots that
  * repeat (WS_ERR_PAGE, as a slot outside the pool).
  * Outputs bf16 or f32.  States hold f32 accuracy over any number of tokens, f32
- * outputs too; in a bf16 output of several tokens' chunk two operands (the
- * scores and the state that a chunk of 32 tokens meets) are rounded to bf16.
+ * outputs too; in a bf16 output of packed sequences the state that a chunk of 32
+ * tokens meets enters rounded to bf16 and the scores as two bf16 values.
  * A query, key or value that is not finite may reach other tokens of its own
  * chunk of the sequence, and never another sequence.
  */

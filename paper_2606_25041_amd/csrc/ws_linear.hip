@@ -133,14 +133,22 @@ __device__ __forceinline__ int sequence_of(const int32_t *off, int S, int t, int
 //   O^T = S^T X^T       B operand of Z^T P^T under a fixed permutation of the
 //   O^T = g^(i+1) O^T + Z^T (P^T . W)   keys, and the state's those of S^T X^T
 //   S   = g^n S + Y^T (Z . w)             under one of the dims
-// Rounded to bf16 are the operands P . W and S (f32 output: three bf16 parts
-// each, 24 bits); the state's own sum takes Z . w in three parts, so that it
-// holds f32 accuracy over any number of tokens.
-// Per token and head 42 MFMAs a wave and chunk (24 of them the state's) against
-// 4 D bf16 of memory traffic: bound by HBM where the chip is full.
+// S enters its product rounded to bf16 (the output it becomes is, too) and P . W
+// as two bf16 parts (two more MFMAs; the output's error is 2.3e-3 of the norm, of which its
+// own rounding is 1.7e-3); f32 outputs take
+// three parts of each, 24 bits.  The state's own sum takes Z . w in three parts, so
+// that it holds f32 accuracy over any number of tokens.
+// A chunk takes a wave 44 MFMAs at D = 128 (24 of them the state's; 62 for f32
+// outputs) against 4 x 32 rows of memory traffic per work-group.  2 x 16384 tokens
+// of 24 heads (805 MB) take 213 us, 3.8 TB/s: the loads and stores alone 168 us,
+// everything else 172, so neither hides all of the other with the two work-groups
+// that registers and LDS leave a CU.  One query head per KV head: the vector work
+// stands between MFMAs that do not need it (231 us one after the other); with
+// several the state's part is not in every step, and straight code was faster.
 // Tiles go global -> LDS, three stages, one barrier a chunk.
 // OUT = false: the state alone, of the sequence that goes on past the cell's
-// edge, written to `cells`.
+// edge, written to `cells` (at D = 128: 110 us of those 2 x 16384 tokens, whose y and
+// z are 403 MB).
 // SETS: KEYS, the key sets of a KV head's query heads are summed, a chunk of each
 // after the other; ROWS, its query heads are taken after each other against the
 // same keys, whose products with the state (24 of the 44 MFMAs) are then formed
