@@ -49,8 +49,14 @@ static int seen(int kind, const LinearArgs *a) {
     g_seen.order[g_seen.norder++] = kind;
     return 0;
 }
-int launch_linear_cells(const LinearArgs &a, bool back, int, void *) { return seen(back ? 11 : 1, &a); }
-int launch_linear(const LinearArgs &a, bool back, int, void *) { return seen(back ? 12 : 2, &a); }
+int launch_linear_cells(const LinearArgs &a, int, void *) { return seen(1, &a); }
+int launch_linear(const LinearArgs &a, int, void *) { return seen(2, &a); }
+int launch_linear_pair(const LinearPair &p, bool cells, bool cells_backwards, int, void *) {   // (as if one after the other)
+    if (cells) seen(1, &p.forwards);
+    seen(2, &p.forwards);
+    if (cells_backwards) seen(11, &p.backwards);
+    return seen(12, &p.backwards);
+}
 int launch_linear_empty(const LinearArgs &a, int, void *) { return seen(3, &a); }
 int launch_linear_commit(const float *, float *, const int32_t *, int32_t, int32_t, int, void *) { return seen(4, nullptr); }
 int launch_linear_step(const LinearStepArgs &, int, void *) { return seen(5, nullptr); }
@@ -109,7 +115,8 @@ int probe_bwd(const int32_t *seqs, int n, const int32_t *blocks, int nb, const i
 }
 
 // A linear prefill (back: its gradients); out: launches' kinds (0-terminated), then of
-// every pass cell_len, ncells, n_work, per_xcd, sets; used: the workspace bytes
+// every pass cell_len, ncells, n_work, per_xcd, query heads per KV head (in a work-group
+// or of their own); used: the workspace bytes
 // that the kernels write
 int probe_linear(const int32_t *seqs, int n, int total, int hq, int hkv, int d, int back, int state, int flags, int *kinds, int *out,
                  int64_t *used) {
@@ -132,7 +139,7 @@ int probe_linear(const int32_t *seqs, int n, int total, int hq, int hkv, int d, 
     for (int i = 0; i < g_seen.nlinear; ++i) {
         const ws::LinearArgs &a = g_seen.linear[i];
         int *o = out + 5 * i;
-        o[0] = a.cell_len, o[1] = a.ncells, o[2] = a.n_work, o[3] = a.per_xcd, o[4] = a.sets;
+        o[0] = a.cell_len, o[1] = a.ncells, o[2] = a.n_work, o[3] = a.per_xcd, o[4] = a.sets * a.head_rows;
         const int64_t cells = (char *)(a.cells + (int64_t)a.ncells * hkv * d * d) - g_mem;
         if (a.ncells > 1 && cells > *used) *used = cells;
         const int64_t after = (char *)a.state_out - g_mem + (int64_t)n * hkv * d * d * 4;

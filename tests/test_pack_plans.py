@@ -148,7 +148,9 @@ def test_linear_plans(seed):
             assert (at > 0 and order[at - 1] == kind - 1) == crossing
         if not back:
             reads, writes = state and flags != 1, state and flags != 2
-            late = reads and writes and 1 in order
+            apart = out[2] > out[1] * hkv   # query heads with work-groups of their own
+            assert out[2] == out[1] * (hq if apart else hkv) and (not apart or out[2] <= (512 if d == 128 else 1024))
+            late = reads and writes and (1 in order or apart)
             assert (4 in order) == late and (3 in order) == (bool(empty) and writes and (late or not reads))
         else:
             assert (3 in order) == (bool(empty) and bool(state))
