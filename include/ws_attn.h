@@ -739,7 +739,7 @@ int ws_linear_attn_step(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const float *l
  *   dq: bf16 [total_tokens][num_q_heads][head_dim], dk, dv: bf16
  *            [..][num_kv_heads][..], written; rows behind the last sequence are not
  *   workspace: ws_linear_workspace_bytes(...) bytes, 16-byte aligned
- * Deterministic.  dstate and dstate0 must not overlap.
+ * Deterministic.  dstate0 must not overlap dstate or the pool.
  */
 int ws_linear_attn_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 dout,
                                const float *log_decay, const int32_t *seq_offsets_host,

@@ -12,7 +12,7 @@
 namespace ws {
 namespace {
 
-constexpr int32_t MAX_TOKENS = INT32_MAX - 256;   // (the ends of cells stay below 2^31)
+constexpr int32_t MAX_TOKENS = INT32_MAX - 256;
 
 // Work-groups that run at once on the chip: two a compute unit (four of head
 // dim 64) by LDS and registers.  Not asked of the device, so that a workspace
@@ -238,6 +238,10 @@ int ws_linear_attn_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tens
     const size_t states = (size_t)num_seqs * num_kv_heads * head_dim * head_dim;
     if (dstate && dstate0 && dstate < dstate0 + states && dstate0 < dstate + states)
         return fail(WS_ERR_SHAPE, "dstate and dstate0 overlap");
+    if (state && dstate0) {   // (the passes run at once)
+        const float *end = state->pool + (size_t)state->num_slots * num_kv_heads * head_dim * head_dim;
+        if (state->pool < dstate0 + states && dstate0 < end) return fail(WS_ERR_SHAPE, "the state pool and dstate0 overlap");
+    }
     const int32_t tokens = off_host[num_seqs];
     if (tokens > 0) {
         if (int rc = check_kv_tensor("q", q)) return rc;

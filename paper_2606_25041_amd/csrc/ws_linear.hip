@@ -197,7 +197,7 @@ __device__ __forceinline__ void linear_pass(const LinearArgs &a, const uint32_t 
     Walk<REV> walk;
     walk.off = a.seqs;
     walk.t0 = cell * a.cell_len;
-    walk.t1 = min(walk.t0 + a.cell_len, a.T);
+    walk.t1 = a.T - walk.t0 > a.cell_len ? walk.t0 + a.cell_len : a.T;   // (their sum may be 2^31)
     walk.sets = SETS == ONE || (SETS == ROWS && !OUT) ? 1 : a.sets;
     walk.set = 0;
     if constexpr (OUT) {

@@ -128,7 +128,7 @@ int probe_linear(const int32_t *seqs, int n, int total, int hq, int hkv, int d, 
     const size_t bytes = ws_linear_workspace_bytes(n, total, hq, hkv, d);
     const int rc = back ? ws_linear_attn_prefill_bwd(tensor(1, hq, d), tensor(1, hkv, d), tensor(1, hkv, d), tensor(1, hq, d), (const float *)g_mem,
                                                      seqs, dev, n, total, hq, hkv, d, 0.1f, state ? &st : nullptr, nullptr,
-                                                     state ? (float *)g_mem : nullptr, tensor(1, hq, d), tensor(1, hkv, d), tensor(1, hkv, d),
+                                                     state ? (float *)g_mem + ((int64_t)1 << 40) : nullptr, tensor(1, hq, d), tensor(1, hkv, d), tensor(1, hkv, d),
                                                      g_mem, bytes, nullptr)
                         : ws_linear_attn_prefill(tensor(1, hq, d), tensor(1, hkv, d), tensor(1, hkv, d), (const float *)g_mem, seqs, dev, n,
                                                  total, hq, hkv, d, 0.1f, state ? &st : nullptr, flags, tensor(1, hq, d), g_mem, bytes, nullptr);

@@ -123,6 +123,14 @@ def test_bwd_refusals(lib):
     assert c(wsp=None) == WORKSPACE and c(size=8) == WORKSPACE
 
 
+def test_first_states_and_their_gradients_apart(lib):
+    """Both passes run at once: dstate0 may not be written over states that dQ's reads."""
+    room = 8 * 2 * 128 * 128 * 4   # the pool's bytes; dstate0's are 2 / 8 of them
+    for at, rc in ((0, SHAPE), (room - 16, SHAPE), (room, HIP), (16 - room // 4, SHAPE), (-room // 4, HIP)):
+        assert bwd(lib, st=state((0, 1), pool=64 * FAKE), ds0=64 * FAKE + at) == rc, at
+    assert bwd(lib, ds0=FAKE) == HIP
+
+
 def test_workspace_bytes(lib):
     f = lib.ws_linear_workspace_bytes
     for bad in ((0, 9, 4, 2, 128), (2, -1, 4, 2, 128), (2, 9, 0, 2, 128), (2, 9, 4, 0, 128), (2, 9, 5, 2, 128), (2, 9, 4, 2, 96)):
