@@ -710,7 +710,9 @@ __device__ __forceinline__ float plus_dpp(float x) {
 // 8 below, whose tokens' instructions come to a quarter (24 heads of 128, us for 1
 // and 8 tokens: 3 sequences 4.6 and 8.4 against 5.0 and 12.6, 8: 7.9 and 12.2
 // against 7.4 and 15.0, 16: 17.1 and 22.7 against 13.0 and 23.0).
-template <int D, int CW, bool F32>
+// QA: query heads read ahead (narrow waves: 4 of several, 32/8 heads of 128 12.1 -> 9.5 us for
+// 8 tokens; one has nothing to gain, 6.5 -> 7.6).
+template <int D, int CW, int QA, bool F32>
 __global__ __launch_bounds__(64) void linear_step_kernel(const LinearStepArgs a) {
     constexpr int LPR = CW / 4, RPL = 64 / LPR, NR = D / RPL;   // lanes per row, rows per load, loads
     const int lane = threadIdx.x, cg = lane % LPR, rg = lane / LPR;
@@ -737,9 +739,9 @@ __global__ __launch_bounds__(64) void linear_step_kernel(const LinearStepArgs a)
     // the column whose sum the lane ends with
     const int mine = 2 * (lane >> 4 & 1) + (lane >> 5);
     const bool writes = (lane & 15) < LPR;
-    // rows as they lie in memory, one token (of the queries: one head) ahead
+    // rows as they lie in memory, one token (of the queries: QA heads) ahead
     u32x2 vr;
-    uint16_t kr[NR], qr[NR];
+    uint16_t kr[NR], qr[QA][NR];
     auto read_key = [&](int t) {
         vr = *(const u32x2 *)(v + t * a.v_st);
 #pragma unroll
@@ -747,7 +749,11 @@ __global__ __launch_bounds__(64) void linear_step_kernel(const LinearStepArgs a)
     };
     auto read_query = [&](int t, int g) {
 #pragma unroll
-        for (int i = 0; i < NR; ++i) qr[i] = q[t * a.q_st + g * a.q_sh + RPL * i];
+        for (int j = 0; j < QA; ++j)
+            if (g + j < a.G) {
+#pragma unroll
+                for (int i = 0; i < NR; ++i) qr[j][i] = q[t * a.q_st + (g + j) * a.q_sh + RPL * i];
+            }
     };
     read_key(0);
     read_query(0, 0);
@@ -765,31 +771,37 @@ __global__ __launch_bounds__(64) void linear_step_kernel(const LinearStepArgs a)
                 const float kept = __uint_as_float(__float_as_uint(S[i][e]) & keep);   // S of a slow head, else 0
                 S[i][e] = __builtin_fmaf(kf[i], vv[e], __builtin_fmaf(S[i][e], by, kept));
             }
-        for (int g = 0; g < a.G; ++g) {
-            f32x4 o = {0.f, 0.f, 0.f, 0.f};
-            float x[NR];
+        for (int g = 0; g < a.G; g += QA) {
+            float x[QA][NR];
 #pragma unroll
-            for (int i = 0; i < NR; ++i) x[i] = __uint_as_float((uint32_t)qr[i] << 16);
-            if (g + 1 < a.G) read_query(t, g + 1);
+            for (int j = 0; j < QA; ++j)
+#pragma unroll
+                for (int i = 0; i < NR; ++i) x[j][i] = __uint_as_float((uint32_t)qr[j][i] << 16);
+            if (g + QA < a.G) read_query(t, g + QA);
             else if (t + 1 < n) read_query(t + 1, 0);
 #pragma unroll
-            for (int i = 0; i < NR; ++i)
+            for (int j = 0; j < QA; ++j) {
+                if (g + j >= a.G) break;
+                f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(x[i], S[i][e], o[e]);
-            // lanes past 32: columns 1 and 3; of every 32 the upper 16: columns 2 and 3
-            float half[2];
+                for (int i = 0; i < NR; ++i)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const u32x2 y = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[2 * h]), __float_as_uint(o[2 * h + 1]), false, false);
-                half[h] = __uint_as_float(y[0]) + __uint_as_float(y[1]);
-            }
-            const u32x2 y = __builtin_amdgcn_permlane16_swap(__float_as_uint(half[0]), __float_as_uint(half[1]), false, false);
-            float sum = plus_dpp<0x128>(__uint_as_float(y[0]) + __uint_as_float(y[1]));   // (lanes 8 apart)
-            if constexpr (LPR == 2) sum = plus_dpp<0x4E>(plus_dpp<0x124>(sum));           // (4 and 2 apart)
-            if (writes) {
-                const int64_t at = b * a.o_sb + t * a.o_st + (int64_t)(kvh * a.G + g) * a.o_sh + col + mine;
-                if constexpr (F32) ((float *)a.out)[at] = sum * a.scale;
-                else ((uint16_t *)a.out)[at] = (uint16_t)pack_bf16x2(sum * a.scale, 0.f);
+                    for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(x[j][i], S[i][e], o[e]);
+                // lanes past 32: columns 1 and 3; of every 32 the upper 16: columns 2 and 3
+                float half[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const u32x2 y = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[2 * h]), __float_as_uint(o[2 * h + 1]), false, false);
+                    half[h] = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+                }
+                const u32x2 y = __builtin_amdgcn_permlane16_swap(__float_as_uint(half[0]), __float_as_uint(half[1]), false, false);
+                float sum = plus_dpp<0x128>(__uint_as_float(y[0]) + __uint_as_float(y[1]));   // (lanes 8 apart)
+                if constexpr (LPR == 2) sum = plus_dpp<0x4E>(plus_dpp<0x124>(sum));           // (4 and 2 apart)
+                if (writes) {
+                    const int64_t at = b * a.o_sb + t * a.o_st + (int64_t)(kvh * a.G + g + j) * a.o_sh + col + mine;
+                    if constexpr (F32) ((float *)a.out)[at] = sum * a.scale;
+                    else ((uint16_t *)a.out)[at] = (uint16_t)pack_bf16x2(sum * a.scale, 0.f);
+                }
             }
         }
     }
@@ -816,8 +828,10 @@ constexpr int64_t FULL = 1024;   // wide waves of a step that give every SIMD on
 template <int D, bool F32>
 int step_t(const LinearStepArgs &a, hipStream_t st) {
     const int64_t heads = (int64_t)a.B * a.Hkv;
-    if (heads * (D / 32) >= FULL) hipLaunchKernelGGL((linear_step_kernel<D, 32, F32>), dim3((unsigned)(heads * (D / 32))), dim3(64), 0, st, a);
-    else hipLaunchKernelGGL((linear_step_kernel<D, 8, F32>), dim3((unsigned)((heads * (D / 8) + NUM_XCD - 1) / NUM_XCD * NUM_XCD)), dim3(64), 0, st, a);
+    const dim3 narrow((unsigned)((heads * (D / 8) + NUM_XCD - 1) / NUM_XCD * NUM_XCD));
+    if (heads * (D / 32) >= FULL) hipLaunchKernelGGL((linear_step_kernel<D, 32, 1, F32>), dim3((unsigned)(heads * (D / 32))), dim3(64), 0, st, a);
+    else if (a.G > 1) hipLaunchKernelGGL((linear_step_kernel<D, 8, 4, F32>), narrow, dim3(64), 0, st, a);
+    else hipLaunchKernelGGL((linear_step_kernel<D, 8, 1, F32>), narrow, dim3(64), 0, st, a);
     return (int)hipGetLastError();
 }
 
