@@ -336,3 +336,39 @@ def test_gradients_of_few_keys(n):
     for name, got, want in (("dq", dq, ds @ x[1]), ("dk", dk, ds.transpose(2, 3).contiguous() @ x[0])):
         got = got.cpu().double().view(S, n, hq, d).transpose(1, 2)
         assert float((got - want).norm() / want.norm()) <= (2 / 3) ** 0.5 * 2.0 ** -8, name
+
+
+@pytest.mark.parametrize("bad", (float("nan"), float("inf")))
+def test_what_is_not_finite_stays_in_its_sequence(bad):
+    """Linear attention: every other sequence's outputs, states and gradients bit for
+    bit as without it, with sequences that share cells, chunks' tails and cell edges."""
+    hq, hkv, d = 4, 2, 64
+    lens, sick = [5, 90, 130, 1, 31, 260], (1, 4)
+    gs.say(f"[gpu] {bad} in two of {len(lens)} sequences")
+    T, S, seqs = sum(lens), len(lens), offsets(lens)
+    at = np.concatenate(([0], np.cumsum(lens)))
+    ld, start = decays(hkv), rnd32(9, S, hkv, d, d)
+
+    def run(x, before):
+        pool = before.clone()
+        st = ws.LinearState(pool, pair(list(range(S))))
+        q, k, v, do = x
+        grads = ws.linear_attn_prefill_bwd(q, k, v, do, ld, seqs, state=st, dstate=before, want_dstate0=True)
+        return ws.linear_attn_prefill(q, k, v, ld, seqs, state=st), pool, grads
+
+    x = [rnd(1, T, hq, d), rnd(2, T, hkv, d), rnd(3, T, hkv, d), rnd(4, T, hq, d)]
+    out, pool, grads = run(x, start)
+    for t in x:
+        for s in sick:
+            t[at[s] + lens[s] // 2] = bad
+    before = start.clone()
+    before[4, 0, 3] = bad
+    out2, pool2, grads2 = run(x, before)
+    torch.cuda.synchronize()
+    for s in range(S):
+        if s not in sick:
+            a, e = at[s], at[s + 1]
+            assert torch.equal(out[a:e], out2[a:e]) and torch.equal(pool[s], pool2[s]), s
+            assert all(torch.equal(g[a:e], h[a:e]) for g, h in zip(grads[:3], grads2[:3])), s
+            assert torch.equal(grads[3][s], grads2[3][s]), s
+    assert not torch.isfinite(out2[at[1]:at[2]].float()).all()
