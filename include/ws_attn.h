@@ -635,8 +635,8 @@ int ws_block_causal_prefill_packed(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v,
  *               total_tokens are enough to run, unsplit
  * total_tokens must be below 2^30.  Deterministic, and as exact, as
  * ws_block_causal_prefill_bwd; rows with at most four tiles of 64 keys take
- * <dout, o> from their scores instead of the rounded o.  What is not finite stays
- * where the forward keeps it.
+ * <dout, o> from their scores instead of the rounded o.  What is not finite in a
+ * sequence reaches no gradient of another.
  */
 int ws_block_causal_prefill_packed_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 o,
                                        ws_tensor4 dout, const float *lse,

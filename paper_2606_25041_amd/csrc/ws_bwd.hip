@@ -118,7 +118,10 @@ __device__ __forceinline__ void dma_rows(const char *g, int64_t st_bytes, int r0
 // row's window are never loaded, as in the forward; the first key of each
 // token's window goes to the dK/dV launch beside its key end.
 // WIN = 2: packed sequences; the rows' items come from a table, the key tiles are
-// counted from the first key of the first row's sequence, as in the forward.
+// counted from the first key of the first row's sequence, as in the forward.  As
+// there, in an item of several sequences a wave whose sums are not all finite does its
+// tiles again, with what is not finite in K as zeros, which the rows that see it add;
+// a masked gradient is then 0 whatever its dP is.
 template <int D, int WIN, bool BF16>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void bwd_dq_kernel(const BwdArgs a, const RowPlan<WIN> rp) {
     constexpr int ROWB = 2 * D, KK = D / 16, MD = D / 32;
@@ -159,8 +162,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int kfull = token_key_end(win, q0, lane);
     const int my_kend = lane_key_end(win, min(q0 + 32 * wave, rows - 1), rc, lane);
     int my_klo = 0, nst = 0, gap = 0, base = 0;   // (base: packed, the first row's first key)
+    bool apart = false;                           // (packed: rows of several sequences)
     if constexpr (WIN == 2) {
         const BlockWindow swin = block_window(a.seqs, nullptr, a.nseqs, q0, lane);
+        apart = window_block(swin, q0) != window_block(swin, min(q0 + 127, rows - 1));
         base = __builtin_amdgcn_readfirstlane(token_anchor(swin, q0, lane));
         my_klo = lane_anchor(swin, min(q0 + 32 * wave, rows - 1), rc, lane);
     } else if constexpr (WIN) {
@@ -383,6 +388,45 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         wait_vm_lgkm<0>();   // tile t + 1 landed (and this tile's LDS reads are done)
         wg_barrier();
     }
+    if constexpr (WIN == 2) {
+        if (apart && any_not_finite(acc)) {
+#pragma unroll
+            for (int md = 0; md < MD; ++md)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[md][v] = 0.f;
+            // (hidden from the optimiser, so that nothing derived here is held over the
+            // loop before)
+            int ln = lane, last = k_hi - 1;
+            asm volatile("" : "+v"(ln), "+s"(last));
+            const int lr = ln & 31, lh = ln >> 5;
+#pragma unroll 1
+            for (int k0 = base; k0 <= last; k0 += 32) {
+                const char *kr = kg + min(k0 + lr, last) * kst + 16 * lh, *vr = vg + min(k0 + lr, last) * vst + 16 * lh;
+                f32x16 S = {}, dPt = {};
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)(kr + 32 * kk), qf[kk], S, 0, 0, 0);
+                    dPt = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)(vr + 32 * kk), dof[kk], dPt, 0, 0, 0);
+                }
+                bf16x8 dsf[2];
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int key = k0 + 8 * (v >> 2) + 4 * lh + (v & 3);
+                    const float ds = fast_exp2(__builtin_fmaf(S[v], c2, -lse2)) * (dPt[v] + nD);
+                    dsf[v >> 3][v & 7] = (__bf16)((key >= my_kend) | (key < my_klo) ? 0.f : ds);
+                }
+                uint32_t odd = 0;
+#pragma unroll
+                for (int i = 0; i < 2 * MD; ++i)
+                    acc[i % MD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        finite_column(kg + 64 * (i % MD) + 2 * lr, kst, k0 + 16 * (i / MD) + 4 * lh, k0, last, odd), dsf[i / MD], acc[i % MD], 0, 0, 0);
+                if (!__builtin_amdgcn_ballot_w64(odd != 0)) continue;
+#pragma unroll 1
+                for (int k = k0; k < k0 + 32; ++k)
+                    add_not_finite<D>(kg + min(k, last) * kst + 8 * lh, (k >= my_klo) & (k < my_kend), acc);
+            }
+        }
+    }
     if (row < rows) {
         const int64_t ofs = b * a.dq_sb + (int64_t)row * a.dq_st + h * a.dq_sh;
 #pragma unroll
@@ -422,7 +466,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // are separate work-groups (BwdArgs), the heaviest, dispatched first.  It spills 7
 // scalars at D = 128 (none without) and 87 at 64 (26 without).
 // WIN = 2: packed sequences; the key tiles and the shares of their rows come from a
-// table, longest first.
+// table, longest first.  Of a tile with keys of several sequences a wave whose sums are
+// not all finite does its chunks again, as in dQ, with what is not finite in Q and dO
+// as zeros.
 template <int D, int WIN, bool BF16>
 __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a, const KeyPlan<WIN> rp) {
     constexpr int ROWB = 2 * D, KK = D / 16, MD = D / 32;
@@ -559,6 +605,9 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a, const Ke
         }
     }
     const int i0 = lo;
+    // packed: keys of several sequences (the first keys of the first and the last differ)
+    bool apart = false;
+    if constexpr (WIN == 2) apart = ld_uniform(kend_b + a.L, kw0) != ld_uniform(kend_b + a.L, min(kw0 + 127, keys - 1));
     // rows before these are no rows (packed: another sequence's, which may hold
     // anything)
     const int low = WIN == 2 ? i0 : 0;
@@ -783,6 +832,70 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(const BwdArgs a, const Ke
         r0 = rn;
         wait_vm_lgkm<0>();   // the next chunks landed; this step's LDS reads are done
         wg_barrier();
+    }
+    if constexpr (WIN == 2) {
+        if (apart && (any_not_finite(dk) || any_not_finite(dv))) {
+#pragma unroll
+            for (int md = 0; md < MD; ++md)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) dk[md][v] = dv[md][v] = 0.f;
+            // (hidden from the optimiser, so that nothing derived here is held over the
+            // loop before)
+            const auto &a = args_again<BwdArgs>();
+            int ln = lane, it = first + grp;
+            asm volatile("" : "+v"(ln), "+s"(it));
+            const int32_t *kend_b = a.kend;
+            const int64_t qst = 2 * a.q_st, dst = 2 * a.do_st;
+            const int lr = ln & 31, lh = ln >> 5, ky = kw0 + 32 * sub + lr;
+            const char *kr = (const char *)(a.k + kvh * a.k_sh + min(ky, keys - 1) * a.k_st) + 16 * lh;
+            const char *vr = (const char *)(a.v + kvh * a.v_sh + min(ky, keys - 1) * a.v_st) + 16 * lh;
+#pragma unroll 1
+            for (; it < total; it += 2) {
+                const int hq = kvh * a.G + it % a.G, r0 = last - 32 * (it / a.G + 1);
+                const char *qg = (const char *)(a.q + hq * a.q_sh), *dg = (const char *)(a.dout + hq * a.do_sh);
+                // (rows before `low` are another sequence's: their place is empty)
+                auto row_of = [&](int r) -> int { return max(r0 + r, low); };
+                // row lr's data; a lane takes that of its accumulators' rows from there
+                const float *rd = a.dl + 2 * (int64_t)hq * a.L + row_of(lr);
+                const float lse2 = rd[0], nD = rd[a.L];
+                const int ke = r0 + lr >= low ? kend_b[row_of(lr)] : 0, kl = kend_b[a.L + row_of(lr)];
+                f32x16 S = {}, dP = {};
+                const char *qr = qg + row_of(lr) * qst + 16 * lh, *dr = dg + row_of(lr) * dst + 16 * lh;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) dP[v] = __shfl(nD, 8 * (v >> 2) + 4 * lh + (v & 3));
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk) {
+                    S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)(qr + 32 * kk), *(const bf16x8 *)(kr + 32 * kk), S, 0, 0, 0);
+                    dP = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)(dr + 32 * kk), *(const bf16x8 *)(vr + 32 * kk), dP, 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                bf16x8 pf[2], dsf[2];
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int r = 8 * (v >> 2) + 4 * lh + (v & 3);
+                    const float p = fast_exp2(__builtin_fmaf(S[v], c2, -__shfl(lse2, r))), ds = p * dP[v];
+                    const bool in = (ky < __shfl(ke, r)) & (ky >= __shfl(kl, r));
+                    pf[v >> 3][v & 7] = (__bf16)(in ? p : 0.f);
+                    dsf[v >> 3][v & 7] = (__bf16)(in ? ds : 0.f);
+                }
+                uint32_t odd = 0;
+#pragma unroll
+                for (int i = 0; i < 2 * MD; ++i) {
+                    const int md = i % MD, rr = r0 + 16 * (i / MD) + 4 * lh;
+                    dv[md] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(finite_column(dg + 64 * md + 2 * lr, dst, rr, low, last - 1, odd), pf[i / MD], dv[md], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    dk[md] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(finite_column(qg + 64 * md + 2 * lr, qst, rr, low, last - 1, odd), dsf[i / MD], dk[md], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (!__builtin_amdgcn_ballot_w64(odd != 0)) continue;
+#pragma unroll 1
+                for (int r = 0; r < 32; ++r) {
+                    const bool in = (ky < __shfl(ke, r)) & (ky >= __shfl(kl, r));
+                    add_not_finite<D>(dg + row_of(r) * dst + 8 * lh, in, dv);
+                    add_not_finite<D>(qg + row_of(r) * qst + 8 * lh, in, dk);
+                }
+            }
+        }
     }
     // group 1 -> LDS -> group 0, in register order (conflict-free)
     float *part = (float *)smem;

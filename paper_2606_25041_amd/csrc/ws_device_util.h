@@ -165,6 +165,63 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, b16x2));
 }
 
+// ---- sums that a value of another sequence may not reach (packed calls) ----------
+// An operand whose masked terms are zeros still makes NaN of 0 times an infinity or
+// NaN.  These serve the rare second pass of a wave in which that has happened: operands
+// straight from memory, what is not finite as zero, then added to those that see it.
+
+// The kernel's first argument, read again: what a rare path behind the loop needs of it
+// is then not held over the loop.
+template <class A>
+__device__ __forceinline__ const __attribute__((address_space(4))) A &args_again() {
+    auto *p = (const __attribute__((address_space(4))) A *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *p;
+}
+
+// Eight rows of one column as an operand: rows r0 + 8 (e / 4) + e % 4 (4 hf in r0),
+// those outside [first, last] as the nearest in it, byte stride st.  What is not finite (an exponent of ones) is zero there
+// and makes odd other than 0.
+__device__ __forceinline__ bf16x8 finite_column(const char *p, int64_t st, int r0, int first, int last, uint32_t &odd) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = r0 + 8 * (i >> 1) + 2 * (i & 1);
+        w[i] = *(const uint16_t *)(p + min(max(r, first), last) * st) | (uint32_t)*(const uint16_t *)(p + min(max(r + 1, first), last) * st) << 16;
+        // (an exponent of ones carries into the sign's place, none beyond it)
+        const uint32_t bad = ((w[i] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+        w[i] &= ~((bad - (bad >> 15)) | bad);
+        odd |= bad;
+    }
+    return __builtin_bit_cast(bf16x8, w);
+}
+// What is not finite in a row of D values, added where `to` holds to a lane's sums:
+// accumulator 4 g + e of block md is dim 32 md + 8 g + 4 hf + e (hf in p).
+template <int D>
+__device__ __forceinline__ void add_not_finite(const char *p, bool to, f32x16 (&acc)[D / 32]) {
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+        const u32x2 x = *(const u32x2 *)(p + 16 * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t bits = e & 1 ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16;
+            const float was = acc[c >> 2][4 * (c & 3) + e];
+            acc[c >> 2][4 * (c & 3) + e] = to & ((bits & 0x7F800000u) == 0x7F800000u) ? was + __uint_as_float(bits) : was;
+        }
+    }
+}
+// Whether a sum of some lane is not finite.
+template <int MD>
+__device__ __forceinline__ bool any_not_finite(const f32x16 (&acc)[MD]) {
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int md = 0; md < MD; ++md)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[v & 3] = __builtin_fmaf(acc[md][v], 0.f, x[v & 3]);   // (infinity times 0 is NaN)
+    const float s = (x[0] + x[1]) + (x[2] + x[3]);
+    return __builtin_amdgcn_ballot_w64(s != s) != 0;
+}
+
 // s_waitcnt with vector-memory count <= N and LDS/scalar count = 0 (the export
 // count is not waited on).  gfx9 encoding: vmcnt[3:0], expcnt[6:4],
 // lgkmcnt[11:8], vmcnt[5:4] in bits [15:14].
