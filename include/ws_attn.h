@@ -607,10 +607,7 @@ size_t ws_step_workspace_bytes_4bit(int32_t batch, int32_t num_q_heads, int32_t 
  *         f32 [num_q_heads][total_tokens]; rows behind the last sequence are left as
  *         they were
  * f32 outputs hold f32 accuracy (as ws_block_causal_attn_fwd_window's).
- * A key or value that is not finite reaches no sequence of more than 256 tokens but
- * its own; sequences of up to 256 tokens that are neighbours may share a tile.
- * (Past 512 tiles of 256 tokens, or 2^24 tokens, tiles may be shared by any
- * neighbours.)
+ * What is not finite in a sequence reaches no row of another.
  * total_tokens must not exceed 2^31 - 257 (WS_ERR_SHAPE).
  * Errors: WS_ERR_NULL, WS_ERR_SHAPE, WS_ERR_UNSUPPORTED, WS_ERR_ALIGN,
  * WS_ERR_HEADS, WS_ERR_OFFSETS, WS_ERR_HIP.

@@ -160,7 +160,18 @@ using Plan = std::conditional_t<WIN == 2, PackPlan, std::conditional_t<RAGGED, R
 // sequence of more than a tile holds rows of that sequence alone; its key tiles are
 // counted from its first row's klo, so that it loads no key of another sequence
 // and masks none.  Only the rows of short sequences that share an item have
-// different klo; a wave skips the tiles before its first row's.
+// different klo; a wave skips the tiles before its first row's.  The weight of
+// another sequence's key is an exact zero, which times an infinity or NaN of its V
+// is NaN: in an item of several sequences a wave whose sums are not all finite does
+// its tiles again, by itself, with such values as zeros, and its rows take those
+// that they see themselves.
+// The arguments that the epilogue takes.
+template <bool AGAIN>
+__device__ __forceinline__ auto &epilogue_args(const AttnArgs &a) {
+    if constexpr (AGAIN) return args_again<AttnArgs>();
+    else return a;
+}
+
 template <int D, int NW, int NB, int KIND, bool F32, int KG, int WIN = 0>
 __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const Plan<is_ragged(KIND), WIN> rp) {
     constexpr bool C4 = is_cache4(KIND);
@@ -367,10 +378,12 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     // window: the first row's klo, at least 0 (it is not past the row's own key),
     // the live tiles and their mapping
     int lo_min = 0, nst = 0, gap = 0;
-    BlockWindow swin;   // (packed: the sequences around the rows)
+    BlockWindow swin;     // (packed: the sequences around the rows)
+    bool apart = false;   // (packed: rows of several of them)
     if constexpr (WIN == 2) {
         swin = block_window(a.seqs, nullptr, a.nseqs, q0, lane);
         lo_min = __builtin_amdgcn_readfirstlane(token_anchor(swin, q0, lane));
+        apart = window_block(swin, q0) != window_block(swin, min(q0 + QT, (int)nrows) - 1);
     } else if constexpr (WIN) {
         if (step) {
             const int t0 = (int)fastdiv((uint32_t)q0, fd_gq);
@@ -843,6 +856,18 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
 #pragma unroll
         for (int n = 0; n < NB; ++n) l[n] += ls[n];
     };
+    // eight weights as the sums of three bf16 values each
+    auto split_weights = [](const float *p, bf16x8 (&part)[3]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float x = p[e];
+#pragma unroll
+            for (int c = 0; c < 3; ++c) {
+                part[c][e] = (__bf16)x;
+                x -= (float)part[c][e];
+            }
+        }
+    };
     // O^T[d][query] += V^T P^T from the V tile of a stage; V reads RAHEAD
     // steps ahead of their MFMAs
     auto pv = [&](uint32_t soff, const Weights &pf) {
@@ -857,17 +882,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
                 if constexpr (P3) {
-                    if (i % MD == 0) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float x = pf[n][8 * (i / MD) + e];
-#pragma unroll
-                            for (int c = 0; c < 3; ++c) {
-                                p3[n][c][e] = (__bf16)x;
-                                x -= (float)p3[n][c][e];
-                            }
-                        }
-                    }
+                    if (i % MD == 0) split_weights(&pf[n][8 * (i / MD)], p3[n]);
 #pragma unroll
                     for (int c = 0; c < 3; ++c)
                         o[n][i % MD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % (RAHEAD + 1)], p3[n][c], o[n][i % MD], 0, 0, 0);
@@ -996,6 +1011,60 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     } else {
         wait_vm_lgkm<0>();   // (the query loads)
     }
+    // Packed, rows of several sequences, sums that are not all finite: this wave's
+    // tiles once more, with the queries that it holds, straight from memory.
+    auto again = [&]() {
+        if (!apart || !busy || !any_not_finite(o[0])) return;
+        m[0] = -INFINITY;
+        l[0] = 0.f;
+#pragma unroll
+        for (int md = 0; md < MD; ++md)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[0][md][v] = 0.f;
+        // (hidden from the optimiser, so that nothing derived here is computed before
+        // the loop and held in registers)
+        const auto &a = args_again<AttnArgs>();
+        int ln = lane, lo = lo_min, last = k_hi - 1;
+        asm volatile("" : "+v"(ln), "+s"(lo), "+s"(last));
+        const int lr = ln & 31, lh = ln >> 5;
+        const char *kb = (const char *)(a.kc + kvh * a.kc_sh), *vb = (const char *)(a.vc + kvh * a.vc_sh);
+        const int64_t ks = 2 * a.kc_st, vs = 2 * a.vc_st;
+#pragma unroll 1
+        for (int t = t_begin + kg; t < t_end; t += KG) {
+            if (t < skip) continue;
+            const int k0 = lo + t * KT;
+#pragma unroll
+            for (int mb = 0; mb < 2; ++mb) {
+                const char *kr = kb + min(k0 + 32 * mb + lr, last) * ks + 16 * lh;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) S[0][mb][v] = 0.f;
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk)
+                    S[0][mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)(kr + 32 * kk), qf[0][kk], S[0][mb], 0, 0, 0);
+            }
+            softmax(t, S, pf);
+            uint32_t odd = 0;
+#pragma unroll
+            for (int ks4 = 0; ks4 < 4; ++ks4) {
+                bf16x8 part[P3 ? 3 : 1];
+                if constexpr (P3) split_weights(&pf[0][8 * ks4], part);
+                else part[0] = pf[0][ks4];
+#pragma unroll
+                for (int md = 0; md < MD; ++md) {
+                    const bf16x8 vt = finite_column(vb + 64 * md + 2 * lr, vs, k0 + 16 * ks4 + 4 * lh, k0, last, odd);
+#pragma unroll
+                    for (int c = 0; c < (P3 ? 3 : 1); ++c)
+                        o[0][md] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, part[c], o[0][md], 0, 0, 0);
+                }
+            }
+            if (!__builtin_amdgcn_ballot_w64(odd != 0)) continue;
+            // (whatever their weight, which is above 0 but for underflow)
+#pragma unroll 1
+            for (int k = k0; k < k0 + KT; ++k)
+                add_not_finite<D>(vb + min(k, last) * vs + 8 * lh, (k >= klo[0]) & (k < kend[0]), o[0]);
+        }
+    };
+    if constexpr (WIN == 2 && KG == 1) again();
 
     // Two key groups.  Phase p (between two barriers) is the leading waves'
     // MFMA block of step p / 2 (p even) or the trailing waves' (p odd), while
@@ -1042,6 +1111,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
             wait_vm_lgkm<0>();   // (the query loads)
             wg_barrier();
         }
+        if constexpr (WIN == 2) again();
         // The odd tiles' sums go to the leading wave of the same rows, in
         // register order; every tile and query read is behind the last barrier.
         char *xch = smem + VRING + rblk * (32 * D * 4 + 512);
@@ -1102,6 +1172,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
     // direct; f32 30.3 and 29.4; 64 rows 10.4 and 9.8, 128 rows 10.8 and 12.0).
     const bool whole = KIND != STEP_SPLIT && (!step || nsplit == 1);   // this item's rows are final
     const bool direct = KIND == STEP && a.nrows <= 64;
+    auto &ea = epilogue_args<WIN == 2>(a);
     if (whole && busy && !direct) {
         // (the lane is hidden from the optimiser, so that nothing derived from
         // it here is computed ahead of the loop and held in registers there)
@@ -1122,7 +1193,7 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
                 const u32x4 val = *(const u32x4 *)(stage + rr * ROWB + 16 * (c ^ swz<D>(rr)));
                 if (p < (int)nrows) {
                     const int t = row_token(p), h = row_head(p, t);
-                    *(u32x4 *)((char *)((E *)a.out + b * a.o_sb + (int64_t)t * a.o_st + h * a.o_sh) + ofs + 16 * c) = val;
+                    *(u32x4 *)((char *)((E *)ea.out + b * ea.o_sb + (int64_t)t * ea.o_st + h * ea.o_sh) + ofs + 16 * c) = val;
                 }
             }
         };
@@ -1180,8 +1251,8 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
                         }
                     }
             }
-            if (a.lse && hf == 0)
-                a.lse[((int64_t)b * a.Hq + h) * a.Lq + t] = (m[n] + __builtin_amdgcn_logf(lt)) * 0.69314718055994531f;
+            if (ea.lse && hf == 0)
+                ea.lse[((int64_t)b * ea.Hq + h) * ea.Lq + t] = (m[n] + __builtin_amdgcn_logf(lt)) * 0.69314718055994531f;
         } else if constexpr (!F32) {
             // bf16 output: o / l rounded to bf16 and the split's log2-domain
             // lse; register order, two accumulator groups (16 bytes) per

@@ -1,5 +1,6 @@
-"""What is not finite stays in its own sequence of a packed call, also past the tables
-of a launch (512 items of rows, 320 of keys).  Everything of the other sequences, outputs,
+"""What is not finite stays in its own sequence of a packed call, at any lengths: of
+neighbours that share a work-group's rows or keys, and past the tables of a launch
+(512 items of rows, 320 of keys).  Everything of the other sequences, outputs,
 log-sum-exps and gradients, is what it is without it, bit for bit; what sees it is
 not finite."""
 import numpy as np
@@ -69,7 +70,67 @@ def check(hq, hkv, d, lens, bad, blocks=None, text=None, f32=False, bf16=False, 
             assert not dv[a:at + 1, 0, dim].isfinite().any() and not dq[at, 0].isfinite().any()
 
 
+SHORT = [5, 33, 1, 64, 100, 20, 0, 30, 3]
+ALL = tuple((n, v) for n in ("q", "k", "v", "do") for v in (NAN, INF, -INF))
+
+
+@pytest.mark.parametrize("f32,bf16", ((False, True), (True, False)))
+@pytest.mark.parametrize("hq,hkv,d", ((4, 2, 64), (2, 2, 128), (8, 1, 128)))
+@pytest.mark.parametrize("bad", (0, 1, 4, 8))
+def test_short_neighbours(hq, hkv, d, bad, f32, bf16):
+    """All in one 256-row tile, two of keys; some in a wave's 32 rows together."""
+    check(hq, hkv, d, SHORT, bad, f32=f32, bf16=bf16, poison=ALL)
+
+
+def test_many_short_sequences():
+    """More work-groups than run at once: tiles of 256 rows."""
+    for bad in (0, 151, 152, 299):
+        check(32, 8, 128, [100, 7, 30] * 100, bad, bf16=True)
+
+
+@pytest.mark.parametrize("d", (64, 128))
+def test_short_beside_long(d):
+    """A long sequence's work-groups in the same launch, 128 rows each (two key groups)."""
+    for bad in (0, 1, 3, 4):
+        check(4, 2, d, [700, 30, 31, 90, 120], bad)
+
+
+@pytest.mark.parametrize("d", (64, 128))
+def test_short_neighbours_with_blocks(d):
+    """By blocks, with token-causal segments."""
+    lens = [40, 25, 60, 3, 70]
+    blocks = [0, 10, 40, 65, 65, 90, 125, 128, 160, 198]
+    text = [5, 30, 41, 65, 90, 100, 125, 150, 160]
+    for bad in range(5):
+        check(4, 2, d, lens, bad, blocks=blocks)
+        check(4, 2, d, lens, bad, blocks=blocks, text=text)
+
+
 @pytest.mark.parametrize("lens,bad", (([260] * 107, 50), ([260] * 171, 80), ([20500, 20500], 0), ([20500, 20500], 1), ([700] * 58, 29)))
 def test_past_the_tables_of_the_gradients(lens, bad):
     """More key or row items than a launch's table holds: tiles of any neighbours."""
     check(2, 1, 64, lens, bad, bf16=True)
+
+
+@pytest.mark.parametrize("lens,bad", (([300] * 450, 211), ([7] * 20000, 9000), ([3, 500] * 300, 301)))
+def test_past_the_tables_of_the_forward(lens, bad):
+    check(1, 1, 128, lens, bad)
+    check(2, 2, 64, lens, bad, f32=True)
+
+
+def test_a_sequence_all_bad():
+    """Every value of a sequence, and of several, in all inputs at once."""
+    gs.say("[gpu] packed, whole sequences not finite")
+    hq, hkv, d = 4, 2, 64
+    seqs = np.concatenate(([0], np.cumsum(SHORT)))
+    T = int(seqs[-1])
+    x = [rnd(1, T, hq, d), rnd(2, T, hkv, d), rnd(3, T, hkv, d), rnd(4, T, hq, d)]
+    clean = calls(*x, pair(seqs), None, None, False, False)
+    gone = [1, 3, 8]
+    rows = torch.cat([torch.arange(int(seqs[s]), int(seqs[s + 1])) for s in gone]).to(DEV)
+    rest = torch.tensor([i for i in range(T) if not any(seqs[s] <= i < seqs[s + 1] for s in gone)], device=DEV)
+    for t in x:
+        t[rows] = NAN
+    got = calls(*x, pair(seqs), None, None, False, False)
+    for p, c in zip(got, clean):
+        assert torch.equal(p[rest], c[rest]) and not p[rows].isfinite().any()
