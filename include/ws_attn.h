@@ -666,8 +666,10 @@ size_t ws_prefill_packed_bwd_workspace_bytes(int32_t total_tokens, int32_t num_q
  * copy, int32, the same values).  A call that writes states refuses slots that
  * repeat (WS_ERR_PAGE, as a slot outside the pool).
  * Outputs bf16 or f32.  States hold f32 accuracy over any number of tokens, f32
- * outputs too; in a bf16 output of packed sequences the state that a chunk of 32
- * tokens meets enters rounded to bf16 and the scores as two bf16 values.
+ * outputs too (a head that loses some, but less than 2^-20, of its state a token, in
+ * packed calls in 32 tokens, is off by up to 2^-24 of it each time: f32 has too few
+ * places for the difference); in a bf16 output of packed sequences the state that a
+ * chunk of 32 tokens meets enters rounded to bf16 and the scores as two bf16 values.
  * A query, key or value that is not finite may reach other tokens of its own
  * chunk of the sequence, and never another sequence.
  */

@@ -54,3 +54,34 @@ def test_many_cells_join(d, n):
         off("out", out[-1, 0], scale * (q[-1, 0].double() @ want), ref.bound(2 * cells + 2 * 8) * 2)
         ds0 = ws.linear_attn_prefill_bwd(q, k, v, do, decay, pair([0, n]), state=state, want_dstate0=True)[3]
         off("dstate0", ds0[0, 0], scale * np.exp(ld) * exact(q[:, 0].flip(0), do[:, 0].flip(0), ld), limit + 2.0 ** -22)
+
+
+@pytest.mark.parametrize("d,n,heads", ((128, 16384, 512), (64, 16384, 1024)))
+def test_many_chunks_of_a_cell(d, n, heads):
+    """So many KV heads that a sequence is one cell: 512 chunks, of heads whose g^32
+    rounds badly."""
+    gs.say(f"[gpu] linear, {n // 32} chunks, {heads} heads x {d}")
+    q, k, v = (rnd(i, n, 1, d).expand(n, heads, d) for i in range(3))
+    lds = (ref.decays(32, 16) * (heads // 16))[:heads]
+    state = ws.LinearState(torch.zeros(1, heads, d, d, device=DEV), pair([0]))
+    ws.linear_attn_prefill(q, k, v, torch.tensor(lds, device=DEV), pair([0, n]), state=state)
+    for h in range(0, heads, heads // 16 + 1):
+        off(f"state, {lds[h]:.3e}", state.pool[0, h], exact(k[:, 0], v[:, 0], lds[h]), ref.bound(8 * n // 32))
+
+
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("batch", (1, 64))
+def test_many_steps(batch, d):
+    """Token by token in place, by narrow waves and by wide ones."""
+    n, heads = 4096, 8
+    gs.say(f"[gpu] linear step, {batch} x {n} tokens, {heads} heads x {d}")
+    q, k, v = (rnd(i, 1, n, heads, d).expand(batch, n, heads, d) for i in range(3))
+    lds = ref.decays(1, heads, 1e-4, 2.0 ** -20)   # (below, f32 has too few places for S - (1 - g) S)
+    state = ws.LinearState(torch.zeros(batch, heads, d, d, device=DEV), pair(list(range(batch))))
+    out = torch.empty(batch, n, heads, d, device=DEV)
+    ws.linear_attn_step(q, k, v, torch.tensor(lds, device=DEV), state, out=out)
+    for h in range(heads):
+        want = exact(k[0, :, h], v[0, :, h], lds[h])
+        for b in (0, batch - 1):
+            off(f"state {b}, {lds[h]:.3e}", state.pool[b, h], want, ref.bound(2 * n))
+            off(f"out {b}", out[b, -1, h], d ** -0.5 * (q[0, -1, h].double() @ want), 2 * ref.bound(2 * n))

@@ -21,3 +21,15 @@ def test_a_decay_rounded_by_itself_is_out_of_bounds():
     x = np.random.default_rng(1).standard_normal((1024, 4096)).astype(np.float32)
     assert ref.error(*ref.recurrence(x, -1e-9, 64, "twice")) > ref.bound(2 * 1024)
     assert ref.error(*ref.recurrence(x, -1e-9, 64, "once")) <= ref.bound(2 * 1024)
+
+
+def test_steps_of_products_of_bf16():
+    """Token by token the decay is rounded by itself: from 2^-20 a token on within the
+    bound, a rounded factor is not."""
+    import torch
+    g = torch.Generator().manual_seed(1)
+    k, v = (torch.randn(4096, 64, generator=g).to(torch.bfloat16).float().numpy() for _ in range(2))
+    x = (k[:, :, None] * v[:, None, :]).reshape(4096, -1)
+    for ld in ref.decays(1, 3, 1e-4, 2.0 ** -20):
+        assert ref.error(*ref.recurrence(x, ld, 1, "factor")) > ref.bound(2 * 4096)
+        assert ref.error(*ref.recurrence(x, ld, 1, "twice")) <= ref.bound(2 * 4096)
