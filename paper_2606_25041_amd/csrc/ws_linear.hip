@@ -692,10 +692,10 @@ __global__ __launch_bounds__(256) void linear_empty_kernel(const LinearArgs a, i
 }
 
 __global__ __launch_bounds__(256) void linear_commit_kernel(const float *from, float *pool, const int32_t *slots, int hkv, int elems) {
-    const int per = elems / 1024, s = blockIdx.x / per, kvh = blockIdx.y;
+    const int s = blockIdx.x, kvh = blockIdx.y;
     const f32x4 *f = (const f32x4 *)(from + ((int64_t)s * hkv + kvh) * elems);
     f32x4 *t = (f32x4 *)(pool + ((int64_t)slots[s] * hkv + kvh) * elems);
-    const int i = blockIdx.x % per * 256 + threadIdx.x;
+    const int i = blockIdx.z * 256 + threadIdx.x;
     t[i] = f[i];
 }
 
@@ -913,7 +913,9 @@ int launch_linear_empty(const LinearArgs &a, int head_dim, void *stream) {
 
 int launch_linear_commit(const float *from, float *pool, const int32_t *slots, int32_t S, int32_t hkv, int head_dim, void *stream) {
     const int elems = head_dim * head_dim;
-    hipLaunchKernelGGL(linear_commit_kernel, dim3((unsigned)(elems / 1024) * S, hkv), dim3(256), 0, (hipStream_t)stream, from, pool, slots, hkv, elems);
+    // (a sequence's parts in a dimension of their own: a launch has fewer than 2^32
+    // threads in one, and 2^24 sequences' states fit no memory)
+    hipLaunchKernelGGL(linear_commit_kernel, dim3(S, hkv, elems / 1024), dim3(256), 0, (hipStream_t)stream, from, pool, slots, hkv, elems);
     return (int)hipGetLastError();
 }
 
