@@ -733,7 +733,7 @@ int ws_linear_attn_step(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, const float *l
  *   dout:    bf16, as q
  *   state_or_null: the states the sequences began with (read only); NULL: zero
  *   dstate:  NULL (zero) or f32 [num_seqs][num_kv_heads][head_dim][head_dim], the
- *            gradient of the final states
+ *            gradient of the final states (1 / scale must be finite then)
  *   dstate0: NULL or the same shape, written: the gradient of the first states
  *   dq: bf16 [total_tokens][num_q_heads][head_dim], dk, dv: bf16
  *            [..][num_kv_heads][..], written; rows behind the last sequence are not

@@ -234,6 +234,8 @@ int ws_linear_attn_prefill_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tens
     if (int rc = check_scalars(log_decay, scale)) return rc;
     if (state)
         if (int rc = check_state(state, num_seqs, false)) return rc;
+    // (the backward passes carry dstate / scale)
+    if (dstate && !std::isfinite(1.f / scale)) return fail(WS_ERR_UNSUPPORTED, "1 / scale must be finite with dstate");
     if (!aligned16(dstate) || !aligned16(dstate0)) return fail(WS_ERR_ALIGN, "dstate and dstate0 must be 16-byte aligned");
     const size_t states = (size_t)num_seqs * num_kv_heads * head_dim * head_dim;
     if (dstate && dstate0 && dstate < dstate0 + states && dstate0 < dstate + states)
