@@ -631,9 +631,10 @@ int ws_block_causal_prefill_packed(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v,
  *               8 * num_q_heads * total_tokens bytes (rounded up to 256) + 8 *
  *               total_tokens are enough to run, unsplit
  * total_tokens must be below 2^30.  Deterministic, and as exact, as
- * ws_block_causal_prefill_bwd; rows with at most four tiles of 64 keys take
- * <dout, o> from their scores instead of the rounded o.  What is not finite in a
- * sequence reaches no gradient of another.
+ * ws_block_causal_prefill_bwd; where up to 128 rows that are taken together see at
+ * most 256 keys, <dout, o> comes from their scores instead of the rounded o (so the
+ * last bits of a row's gradients depend on the rows and sequences beside it).  What is
+ * not finite in a sequence reaches no gradient of another.
  */
 int ws_block_causal_prefill_packed_bwd(ws_tensor4 q, ws_tensor4 k, ws_tensor4 v, ws_tensor4 o,
                                        ws_tensor4 dout, const float *lse,

@@ -21,8 +21,10 @@ int resident(int head_dim) { return head_dim == 128 ? 512 : 1024; }
 
 // Cells of the token axis, each a work-group of every KV head: as many as fill
 // the chip once, none shorter than 64 tokens (two chunks: the states of its edges
-// cost as much as eight).  With half of them the states' pass leaves CUs empty
-// (gradients of 8192 tokens of 32/8 heads of 128: 236 us, 260 with half the cells).
+// cost as much as eight).  Half of them, and so half of the work-groups, leave CUs
+// empty in the states' pass (gradients of 8192 tokens of 32/8 heads of 128: 236 us,
+// 260 so); longer cells with as many work-groups were not tried.  Neither the states'
+// traffic nor the launches are weighed: few KV heads pay for their many cells.
 int32_t plan_cell_len(int32_t tokens, int64_t rows, int head_dim) {
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(resident(head_dim) / rows, LIN_MAX_CELLS));
     const int64_t len = (tokens + most - 1) / most;

@@ -276,10 +276,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         // arithmetic, from a pass of its own over their tiles.  <dO, O> is off by
         // the bf16 roundings of O and of the forward's weights, which are not small
         // beside a dS where |O| is not below |v| (by sqrt of the keys): relative
-        // errors of dQ and dK for causal sequences of 4 / 64 / 1500 random tokens are
-        // 4.0e-3 / 2.8e-3 / 2.6e-3 with it everywhere, 2.4e-3 each (what the
-        // roundings of dS and of the result leave) with this for rows of up to 128
-        // keys; beyond FEW tiles nothing is left to gain.
+        // errors of dQ and dK for causal sequences of 4 / 64 / 256 / 1500 tokens (unit
+        // normals, 4 heads of 128) are 3.4e-3 / 2.6e-3 / 2.5e-3 / 2.4e-3 with it
+        // everywhere, 2.3e-3 to 2.4e-3 (what the roundings of dS and of the result
+        // leave) with this for items of up to FEW tiles, of which two measure the same
+        // as four.  The tiles are the item's: whether a row's D comes from here depends
+        // on the rows beside it.
         constexpr int FEW = 4;
         if (ntile <= FEW) {
             float sum = 0.f;

@@ -716,9 +716,12 @@ __device__ __forceinline__ float plus_dpp(float x) {
 // CW: 32, whose loads are of whole cache lines, where every SIMD has such a wave;
 // 8 below, whose tokens' instructions come to a quarter (24 heads of 128, us for 1
 // and 8 tokens: 3 sequences 4.6 and 8.4 against 5.0 and 12.6, 8: 7.9 and 12.2
-// against 7.4 and 15.0, 16: 17.1 and 22.7 against 13.0 and 23.0).
-// QA: query heads read ahead (narrow waves: 4 of several, 32/8 heads of 128 12.1 -> 9.5 us for
-// 8 tokens; one has nothing to gain, 6.5 -> 7.6).
+// against 7.4 and 15.0, 16: 17.1 and 22.7 against 13.0 and 23.0; the rule goes by the
+// waves alone, which costs one token of the 8 its 0.5 us).
+// QA: query heads read ahead, 4 in narrow waves of several to a KV head (8 tokens, us
+// with 1 and 4: 3 sequences of 8/4 heads of 128 7.9 and 7.7, 8 of 24/12 10.6 and 11.0,
+// 3 of 12/4 9.9 and 8.6, 4 of 32/8 13.0 and 10.7, of 40/8 15.3 and 13.4, of 64/8 22.3
+// and 17.0; one token of 64/8 4.3 and 3.75); one head has nothing to gain, 6.5 -> 7.6.
 template <int D, int CW, int QA, bool F32>
 __global__ __launch_bounds__(64) void linear_step_kernel(const LinearStepArgs a) {
     constexpr int LPR = CW / 4, RPL = 64 / LPR, NR = D / RPL;   // lanes per row, rows per load, loads
