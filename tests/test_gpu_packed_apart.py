@@ -134,3 +134,47 @@ def test_a_sequence_all_bad():
     got = calls(*x, pair(seqs), None, None, False, False)
     for p, c in zip(got, clean):
         assert torch.equal(p[rest], c[rest]) and not p[rows].isfinite().any()
+
+
+@pytest.mark.parametrize("d", (64, 128))
+def test_views(d):
+    """Heads of one fused projection, outputs and gradients into views, tokens behind the
+    last sequence, captured into a graph and replayed on other values."""
+    gs.say(f"[gpu] packed, views, x {d}")
+    hq, hkv, tail = 4, 2, 9
+    lens = [*SHORT, 300]
+    seqs = pair(np.concatenate(([0], np.cumsum(lens))))
+    T = int(seqs[0][-1])
+    fused, do = rnd(1, T + tail, hq + 2 * hkv, d), rnd(2, T + tail, hq, d)
+    fused[T:], do[T:] = NAN, NAN
+    first = fused.clone()
+    q, k, v = fused[:, :hq], fused[:, hq:hq + hkv], fused[:, hq + hkv:]
+    wide = torch.full((T + tail, 2 * hq, d), 7.0, dtype=torch.bfloat16, device=DEV)
+    dfused = torch.full((T + tail, hq + 2 * hkv, d), 7.0, device=DEV)
+    lse = torch.full((hq, T + tail), 7.0, device=DEV)
+    space = torch.empty(ws.prefill_packed_bwd_workspace_bytes(T + tail, hq, hkv), dtype=torch.uint8, device=DEV)
+
+    def run():
+        ws.block_causal_prefill_packed(q, k, v, seqs, out=wide[:, 1::2], lse=lse)
+        ws.block_causal_prefill_packed_bwd(q, k, v, wide[:, 1::2], do, lse, seqs, dq=dfused[:, :hq], dk=dfused[:, hq:hq + hkv],
+                                           dv=dfused[:, hq + hkv:], workspace=space)
+
+    run()
+    clean = [t.clone() for t in (wide, dfused, lse)]
+    assert all(t.isfinite().all() for t in clean) and (wide[:, ::2] == 7).all() and (wide[T:] == 7).all() and (dfused[T:] == 7).all()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.stream(stream), torch.cuda.graph(graph, stream=stream):
+        run()
+    torch.cuda.synchronize()
+    for bad in (1, 4, 8, 9, None):
+        fused.copy_(first)
+        rest = torch.ones(T + tail, dtype=torch.bool, device=DEV)
+        if bad is not None:
+            a, e = seqs[0][bad:bad + 2].tolist()
+            fused[(a + e) // 2, :, 5] = INF
+            rest[a:e] = False
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip((wide, dfused, lse.T), (clean[0], clean[1], clean[2].T)):
+            assert torch.equal(got[rest], want[rest]), bad
+            assert bad is None or not got[~rest].isfinite().all()
