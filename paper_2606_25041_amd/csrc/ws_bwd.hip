@@ -160,14 +160,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const BlockWindow win = block_window(offs, text, a.nb, q0, lane);
     const int k_hi = token_key_end(win, min(q0 + 127, rows - 1), lane);
     const int kfull = token_key_end(win, q0, lane);
-    const int my_kend = lane_key_end(win, min(q0 + 32 * wave, rows - 1), rc, lane);
+    const int my_kend = WIN == 2 ? packed_key_end(win, min(q0 + 32 * wave, rows - 1), rc, lane)
+                                 : lane_key_end(win, min(q0 + 32 * wave, rows - 1), rc, lane);
     int my_klo = 0, nst = 0, gap = 0, base = 0;   // (base: packed, the first row's first key)
     bool apart = false;                           // (packed: rows of several sequences)
     if constexpr (WIN == 2) {
         const BlockWindow swin = block_window(a.seqs, nullptr, a.nseqs, q0, lane);
         apart = window_block(swin, q0) != window_block(swin, min(q0 + 127, rows - 1));
         base = __builtin_amdgcn_readfirstlane(token_anchor(swin, q0, lane));
-        my_klo = lane_anchor(swin, min(q0 + 32 * wave, rows - 1), rc, lane);
+        my_klo = packed_anchor(swin, min(q0 + 32 * wave, rows - 1), rc, lane);
     } else if constexpr (WIN) {
         const int first = max(token_anchor(win, q0, lane) - a.window, 0) / 64;
         my_klo = lane_anchor(win, min(q0 + 32 * wave, a.L - 1), rc, lane) - a.window;

@@ -135,6 +135,14 @@ struct NoPlan {};
 template <bool RAGGED, int WIN = 0>
 using Plan = std::conditional_t<WIN == 2, PackPlan, std::conditional_t<RAGGED, RaggedPlan, NoPlan>>;
 
+// The arguments that the epilogue takes (packed: read again, as the rare second pass
+// leaves no scalars to hold them over the loop).
+template <bool AGAIN>
+__device__ __forceinline__ auto &epilogue_args(const AttnArgs &a) {
+    if constexpr (AGAIN) return args_again<AttnArgs>();
+    else return a;
+}
+
 //
 // KG = 2 (prefill): the work-group takes 128 query rows, and its two halves of
 // four waves the even and the odd key tiles of the same rows, merged through
@@ -165,13 +173,6 @@ using Plan = std::conditional_t<WIN == 2, PackPlan, std::conditional_t<RAGGED, R
 // is NaN: in an item of several sequences a wave whose sums are not all finite does
 // its tiles again, by itself, with such values as zeros, and its rows take those
 // that they see themselves.
-// The arguments that the epilogue takes.
-template <bool AGAIN>
-__device__ __forceinline__ auto &epilogue_args(const AttnArgs &a) {
-    if constexpr (AGAIN) return args_again<AttnArgs>();
-    else return a;
-}
-
 template <int D, int NW, int NB, int KIND, bool F32, int KG, int WIN = 0>
 __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const Plan<is_ragged(KIND), WIN> rp) {
     constexpr bool C4 = is_cache4(KIND);
@@ -437,11 +438,13 @@ __global__ __launch_bounds__(NW * 64) void attn_kernel(const AttnArgs a, const P
         tok[n] = row_token(pc);
         hqr[n] = row_head(pc, tok[n]);
         if constexpr (step) kend[n] = n_new + min(nl, max(ts, tok[n] + 1));
+        else if constexpr (WIN == 2)
+            kend[n] = packed_key_end(win, min(q0 + rblk * 32 * NB + 32 * n, (int)nrows - 1), tok[n], lane);
         else kend[n] = lane_key_end(win, min(q0 + rblk * 32 * NB + 32 * n, (int)nrows - 1), tok[n], lane);
         klo[n] = 0;
         if constexpr (WIN && step) klo[n] = n_pool + (tok[n] >= ts ? tok[n] : 0) - a.window;
         else if constexpr (WIN == 2)
-            klo[n] = lane_anchor(swin, min(q0 + rblk * 32 * NB + 32 * n, (int)nrows - 1), tok[n], lane);
+            klo[n] = packed_anchor(swin, min(q0 + rblk * 32 * NB + 32 * n, (int)nrows - 1), tok[n], lane);
         else if constexpr (WIN)
             klo[n] = lane_anchor(win, min(q0 + rblk * 32 * NB + 32 * n, (int)nrows - 1), tok[n], lane) - a.window;
     }
